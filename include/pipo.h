@@ -385,6 +385,110 @@ PIPO_API pipo_status pipo_op_lm_head_argmax_noalloc(int32_t dtype, const void *d
                                                     const float *d_h, const void *d_gamma, float eps, int32_t B,
                                                     int32_t *d_tokens, float *d_logits, void *stream);
 
+/* ---- attention over a paged cache that the caller owns ------------------
+ * The attention half of a decoder layer as kernel-level calls: append the new
+ * tokens' keys and values (pipo_op_kv_append), attend to everything cached
+ * (pipo_op_attn_paged), or score the pages (pipo_op_page_scores) and attend
+ * to the best ones only (pipo_op_attn_pages).  For serving; no gradients.
+ *
+ * Layout, as in a context's caches: entry j of sequence b is slot j % 64 of
+ * block table[b][j / 64]; the pools are [n_blocks][n_kv][64][d_h].
+ *
+ * A call works on the new tokens of a ragged batch: those of sequence b are
+ * rows q_start[b] .. q_start[b+1]-1 of its token arrays (none is allowed), and
+ * kv_len[b] counts the cached entries of b INCLUDING them, so that token i of
+ * n_b new ones has position kv_len[b] - n_b + i.  A token with a negative
+ * position (more new tokens than entries) has no entry: nothing is appended
+ * for it and its outputs are zero.  Rows outside every sequence's range are
+ * not touched.  The lengths are read on the device: a captured graph stays
+ * valid while they grow.
+ *
+ * q_start must not decrease; kv_len is clamped to [0, 64 max_pages].  Only
+ * table entries of pages below kv_len are read; a block outside [0, n_blocks)
+ * is not followed (an append skips it, a read takes block 0 or n_blocks - 1).
+ * Cache slots at and past kv_len may hold anything, also NaN; those below it
+ * must be finite.
+ *
+ * Common to the calls: device pointers, no host synchronisation, nothing
+ * allocated, everything enqueued on `stream` (NULL = the legacy default
+ * stream) and capturable.  EINVAL for bad shapes, pointers that are NULL or not
+ * 16-byte aligned (the int arrays: 4), strides below a row or not a
+ * multiple of 16 bytes, or a short scratch buffer; batch 0 or n_tokens 0 is
+ * a no-op. */
+typedef struct {
+    int32_t dtype;       /* 0: fp32, 1: bf16: pools, page means, gains, queries and outputs */
+    int32_t n_q_heads;
+    int32_t n_kv_heads;  /* n_q_heads / n_kv_heads a whole number of at most 16 */
+    int32_t head_dim;    /* d_h: 64 or 128 */
+    int32_t page_size;   /* 64 */
+    int32_t n_blocks;    /* blocks of the pools */
+    int32_t max_pages;   /* row length of the table; a sequence holds at most 64 * max_pages entries */
+    int32_t batch;       /* sequences, at most 4096 */
+    void *k;             /* [n_blocks][n_kv][64][d_h] */
+    void *v;             /* [n_blocks][n_kv][64][d_h] */
+    void *means;         /* [n_blocks][n_kv][d_h] mean key of the entries a block holds, or NULL */
+    const int32_t *table;    /* [batch][max_pages] */
+    const int32_t *q_start;  /* [batch + 1] */
+    const int32_t *kv_len;   /* [batch] */
+} pipo_paged;
+
+/* Norm, rotation and append in one launch.  d_q, d_k, d_v: the projections'
+ * outputs, fp32 (in_dtype 0) or bf16 (1), token t's heads back to back at
+ * d_q + t * ld_q elements (ld_k, ld_v likewise; slices of one fused row are
+ * fine).  Per head of q and k: RMSNorm over d_h with the gains d_q_gain /
+ * d_k_gain [d_h] (NULL: no norm; eps inside the root), then the rotate-half
+ * rotation of pairs (i, i + d_h/2) by d_rope[position][i] = (cos, sin), fp32
+ * [n_rope][d_h/2][2] with n_rope >= 64 max_pages (NULL: none).  k and v are rounded to the
+ * pools' type and written at their positions; the queries go to d_q_out
+ * [n_tokens][n_q * d_h] in the pools' type.  d_q and d_q_out may both be NULL
+ * (no queries).  With c->means, the means of the pages that received an entry
+ * are set to the mean of their entries below kv_len, as stored. */
+PIPO_API pipo_status pipo_op_kv_append(const pipo_paged *c, int32_t n_tokens, int32_t in_dtype, const void *d_q,
+                                       int64_t ld_q, const void *d_k, int64_t ld_k, const void *d_v, int64_t ld_v,
+                                       const void *d_q_gain, const void *d_k_gain, float eps, const float *d_rope,
+                                       int32_t n_rope, void *d_q_out, void *stream);
+
+/* Causal attention of the new tokens over the cache (their own entries
+ * appended before): out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over
+ * the entries j <= position, and with window > 0 only j > position - window.
+ * d_q at ld_q elements per token, d_out at ld_out, both in the pools' type.
+ * scale > 0.  d_scratch: pipo_op_attn_paged_scratch(c, n_tokens) bytes, 16-byte
+ * aligned, overwritten; not shared with a call that may overlap. */
+PIPO_API pipo_status pipo_op_attn_paged(const pipo_paged *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
+                                        float scale, int32_t window, void *d_out, int64_t ld_out, void *d_scratch,
+                                        size_t scratch_bytes, void *stream);
+
+/* Scratch bytes of pipo_op_attn_paged and pipo_op_attn_pages on the current
+ * device (0 for arguments they reject or when no device is usable). */
+PIPO_API size_t pipo_op_attn_paged_scratch(const pipo_paged *c, int32_t n_tokens);
+
+/* The cheap score of every page a token sees: d_scores[t][g][p] = scale *
+ * sum over the query heads h of kv head g of q[t, h] . means[table[b][p]][g],
+ * fp32 [n_tokens][n_kv][max_pages]; -infinity for pages past the token's
+ * position.  Needs c->means (k and v may be NULL). */
+PIPO_API pipo_status pipo_op_page_scores(const pipo_paged *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
+                                         float scale, float *d_scores, void *stream);
+
+/* Causal attention over selected pages.  Of the position / 64 + 1 pages that
+ * a token sees, every kv head reads the first n_sink, the last n_local and then
+ * those with the largest d_scores[t][g][p] (ties go to the lower page, NaN
+ * comes last) until it has n_top, or all of them; d_pages[t][g][n_top] (int32)
+ * receives them in ascending order, -1 behind the last.  n_sink, n_local >= 0,
+ * n_sink + n_local <= n_top, 1 <= n_top <= 4096.  d_scores is
+ * [n_tokens][n_kv][max_pages] as pipo_op_page_scores writes it (what it holds
+ * past a token's pages is not read); any values will do, e.g. those of a
+ * learned indexer.  Otherwise as pipo_op_attn_paged. */
+PIPO_API pipo_status pipo_op_attn_pages(const pipo_paged *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
+                                        float scale, const float *d_scores, int32_t n_top, int32_t n_sink,
+                                        int32_t n_local, void *d_out, int64_t ld_out, int32_t *d_pages,
+                                        void *d_scratch, size_t scratch_bytes, void *stream);
+
+/* Whether a device-side wait of the calls above has given up since the last
+ * check (their outputs are then incomplete): synchronises the current device, reads and clears
+ * the error word.  PIPO_ECUDA with the wait site in the message, else PIPO_OK.
+ * h_info[4] (host, may be NULL): {site, block, iteration, parity} of the first. */
+PIPO_API pipo_status pipo_op_paged_check(uint32_t *h_info);
+
 /* Kernel timing of one decode step run eagerly (no graph) on the context
  * stream, with CUDA events recorded around every launch.  For launch i in step
  * order: h_kind[i] (0 weight-streaming GEMV, 1 attention, 2 other), h_bytes[i]

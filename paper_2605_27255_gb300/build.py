@@ -17,12 +17,14 @@ LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libpipo.so")
 # the host code first (the longest units start first)
 SOURCES = ["k_gemv_bf16.cu", "k_gemv_f32.cu", "k_attn.cu", "pipo_capi.cu", "k_tc.cu"]
+# the operators on caller-owned paged caches
+PAGED_SOURCES = ["paged/k_paged.cu", "paged/paged_capi.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
 def _digest() -> str:
     h = hashlib.sha256()
-    for d in (CSRC, INCLUDE):
+    for d in (CSRC, os.path.join(CSRC, "paged"), INCLUDE):
         for name in sorted(os.listdir(d)):
             p = os.path.join(d, name)
             if os.path.isfile(p):
@@ -57,16 +59,18 @@ def build(force: bool = False, verbose: bool = False) -> str:
     flags = ["-O3", "-std=c++17", "-lineinfo", *ARCH, "-Xcompiler", "-fPIC,-fvisibility=hidden",
              "-I", INCLUDE, "-I", CSRC] + extra_flags() + (["-Xptxas=-v"] if verbose else [])
 
+    units = SOURCES + PAGED_SOURCES
+
     def compile_unit(src: str) -> str:
-        obj = os.path.join(LIBDIR, os.path.splitext(src)[0] + tag + ".o")
+        obj = os.path.join(LIBDIR, os.path.splitext(os.path.basename(src))[0] + tag + ".o")
         cmd = [nvcc(), *flags, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), file=sys.stderr)
         subprocess.check_call(cmd)
         return obj
 
-    with concurrent.futures.ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as pool:
-        objs = list(pool.map(compile_unit, SOURCES))
+    with concurrent.futures.ThreadPoolExecutor(max_workers=min(len(units), os.cpu_count() or 1)) as pool:
+        objs = list(pool.map(compile_unit, units))
     tmp = LIB + tag
     try:
         subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs])

@@ -67,6 +67,16 @@ class pipo_debug(C.Structure):
                 ("x_b", _IP), ("x_d", _IP)]
 
 
+class pipo_paged(C.Structure):
+    """A paged cache that the caller owns and a ragged batch of new tokens
+    (include/pipo.h); pointers are device addresses."""
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_blocks",
+                                         "max_pages", "batch")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "means", "table", "q_start", "kv_len")]
+
+
+_PG = C.POINTER(pipo_paged)
+
 # name -> (restype, argtypes): every entry point declared in include/pipo.h
 SIGNATURES = {
     "pipo_init": (C.c_int, [C.POINTER(pipo_config), C.POINTER(pipo_weights), C.POINTER(C.c_void_p)]),
@@ -103,6 +113,17 @@ SIGNATURES = {
     "pipo_op_gemm_tc_norm": (C.c_int, [C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p,
                                        C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_int32,
                                        C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "pipo_op_kv_append": (C.c_int, [_PG, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                    C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int32,
+                                    C.c_void_p, C.c_void_p]),
+    "pipo_op_attn_paged": (C.c_int, [_PG, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_int32, C.c_void_p,
+                                     C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "pipo_op_attn_paged_scratch": (C.c_size_t, [_PG, C.c_int32]),
+    "pipo_op_page_scores": (C.c_int, [_PG, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p]),
+    "pipo_op_attn_pages": (C.c_int, [_PG, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int32,
+                                     C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t,
+                                     C.c_void_p]),
+    "pipo_op_paged_check": (C.c_int, [C.POINTER(C.c_uint32)]),
     "pipo_describe_step": (C.c_int, [C.c_void_p, C.c_char_p, C.c_size_t]),
     "pipo_replay_family": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_double), _IP]),
     "pipo_selftest_wait": (C.c_int, [C.c_int32, C.c_uint64, C.POINTER(C.c_uint32)]),
@@ -329,6 +350,47 @@ def pipo_op_lm_head_argmax_noalloc(dtype: int, E: int, V: int, H: int, h: int, g
     _check(load().pipo_op_lm_head_argmax_noalloc(dtype, C.c_void_p(E), V, H, C.c_void_p(h),
                                                  C.c_void_p(gamma or None), float(eps), B, C.c_void_p(tokens),
                                                  C.c_void_p(logits or None), C.c_void_p(stream or None)), None)
+
+
+def pipo_op_kv_append(c: pipo_paged, n_tokens: int, in_dtype: int, q: int, ld_q: int, k: int, ld_k: int, v: int,
+                      ld_v: int, q_gain: int, k_gain: int, eps: float, rope: int, n_rope: int, q_out: int,
+                      stream: int = 0) -> None:
+    """Norm, rotation and append of new tokens (device pointers as ints, 0 for NULL); see include/pipo.h."""
+    _check(load().pipo_op_kv_append(c, n_tokens, in_dtype, q or None, ld_q, k or None, ld_k, v or None, ld_v,
+                                    q_gain or None, k_gain or None, eps, rope or None, n_rope, q_out or None,
+                                    stream or None), None)
+
+
+def pipo_op_attn_paged_scratch(c: pipo_paged, n_tokens: int) -> int:
+    """Scratch bytes of pipo_op_attn_paged and pipo_op_attn_pages (0: rejected arguments)."""
+    return load().pipo_op_attn_paged_scratch(c, n_tokens)
+
+
+def pipo_op_attn_paged(c: pipo_paged, n_tokens: int, q: int, ld_q: int, scale: float, window: int, out: int,
+                       ld_out: int, scratch: int, scratch_bytes: int, stream: int = 0) -> None:
+    """Causal attention of new tokens over a paged cache; see include/pipo.h."""
+    _check(load().pipo_op_attn_paged(c, n_tokens, q or None, ld_q, scale, window, out or None, ld_out,
+                                     scratch or None, scratch_bytes, stream or None), None)
+
+
+def pipo_op_page_scores(c: pipo_paged, n_tokens: int, q: int, ld_q: int, scale: float, scores: int,
+                        stream: int = 0) -> None:
+    """Score of every page for every new token and kv head; see include/pipo.h."""
+    _check(load().pipo_op_page_scores(c, n_tokens, q or None, ld_q, scale, scores or None, stream or None), None)
+
+
+def pipo_op_attn_pages(c: pipo_paged, n_tokens: int, q: int, ld_q: int, scale: float, scores: int, n_top: int,
+                       n_sink: int, n_local: int, out: int, ld_out: int, pages: int, scratch: int, scratch_bytes: int,
+                       stream: int = 0) -> None:
+    """Causal attention over the pages the scores select; see include/pipo.h."""
+    _check(load().pipo_op_attn_pages(c, n_tokens, q or None, ld_q, scale, scores or None, n_top, n_sink, n_local,
+                                     out or None, ld_out, pages or None, scratch or None, scratch_bytes,
+                                     stream or None), None)
+
+
+def pipo_op_paged_check():
+    """Raises when a device-side wait of the paged-cache calls has given up (synchronises)."""
+    _check(load().pipo_op_paged_check(None), None)
 
 
 def pipo_profile_step(ctx, cap: int = 4096):

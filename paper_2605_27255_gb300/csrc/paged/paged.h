@@ -1,0 +1,70 @@
+// Paged-cache operators: what the host code (paged_capi.cu) and the kernel
+// units share.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace pipo {
+
+constexpr int kPage = 64;            // entries per block
+constexpr int kPagedMaxBatch = 4096;
+constexpr int kPagedMaxGroup = 16;   // query heads per kv head
+constexpr int kPagedMaxTop = 4096;
+
+// the cache and the ragged batch of new tokens (pipo_paged)
+struct PagedArgs {
+    void *k, *v, *means;
+    const int32_t *table, *q_start, *kv_len;
+    int dtype, n_q, n_kv, G, dh;
+    int n_blocks, max_pages, batch, n_tokens;
+};
+
+struct AppendArgs {
+    PagedArgs c;
+    const void *q, *kn, *vn;      // fp32 or bf16, token t at q + t * ld_q
+    long long ld_q, ld_k, ld_v;
+    const void *q_gain, *k_gain;  // [dh] in the pools' type, or nullptr
+    const float* rope;            // [position][dh / 2][2], or nullptr
+    float eps;
+    int in_bf16;
+    void* q_out;                  // [n_tokens][n_q * dh] or nullptr
+};
+
+struct AttnPagedArgs {
+    PagedArgs c;
+    const void* q;
+    long long ld_q;
+    void* out;
+    long long ld_out;
+    float scale;
+    int window;             // 0: none
+    const int32_t* pages;   // [token][n_kv][n_top] kept pages, ascending, -1 behind the last; nullptr: every page
+    int n_top;
+    unsigned char* scratch;
+};
+
+struct ScoreArgs {
+    PagedArgs c;
+    const void* q;
+    long long ld_q;
+    float scale;
+    float* scores;  // [token][n_kv][max_pages]
+};
+
+struct SelectArgs {
+    PagedArgs c;
+    const float* scores;
+    int n_top, n_sink, n_local;
+    int32_t* pages;
+};
+
+// k_paged.cu
+cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
+cudaError_t launch_page_scores(const ScoreArgs& a, cudaStream_t s);
+cudaError_t launch_page_select(const SelectArgs& a, cudaStream_t s);
+cudaError_t launch_attn_plain(const AttnPagedArgs& a, cudaStream_t s);
+cudaError_t take_error_paged(unsigned* code, unsigned* info);
+
+}  // namespace pipo

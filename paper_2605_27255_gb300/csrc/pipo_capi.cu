@@ -219,6 +219,16 @@ struct pipo_ctx {
 };
 
 // ------------------------------------------------------------------ helpers
+namespace pipo {
+// the message of a failed call of another unit's pipo_op_* entry points
+void set_op_error(const char* msg) {
+    try {
+        g_init_error = msg;
+    } catch (...) {  // no memory for the message: the status stands
+    }
+}
+}  // namespace pipo
+
 namespace {
 
 pipo_status fail(pipo_ctx* c, pipo_status s, const char* fmt, ...) {

@@ -1,0 +1,187 @@
+"""The paged-cache operators of ``include/pipo.h`` on torch tensors.
+
+``PagedCache`` describes pools and a block table that the caller owns and
+makes the four calls of an attention layer on the current CUDA stream:
+
+    cache = PagedCache(k_pool, v_pool, table, n_q=32, means=means)
+    q = cache.append(q, k, v, q_start, kv_len, q_gain=..., k_gain=..., rope=...)
+    out = cache.attend(q, q_start, kv_len)
+    scores = cache.page_scores(q, q_start, kv_len)
+    out, pages = cache.attend_pages(q, scores, q_start, kv_len, top=32, sink=1, local=2)
+
+The new tokens of sequence b are rows ``q_start[b] .. q_start[b+1]-1`` of the
+token tensors ``[tokens, heads, d_h]`` (any token stride; the heads of a token
+back to back), and ``kv_len[b]`` counts its cached entries, the new ones
+included.  ``q_start`` and ``kv_len`` are int32 tensors on the device and are
+read there: the calls neither synchronise nor depend on host copies, and a
+captured graph follows their values.  Shapes and types are checked here,
+everything else by the library (``capi.PipoError``).
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import capi
+
+PAGE = 64
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def rope_table(n: int, d_h: int, theta: float, device="cuda") -> torch.Tensor:
+    """(cos, sin) of every position and pair, angle ``position * theta^(-2i/d_h)``,
+    computed in fp64 and rounded once: fp32 [n, d_h/2, 2]."""
+    i = torch.arange(0, d_h, 2, device=device, dtype=torch.float64)
+    a = torch.arange(n, device=device, dtype=torch.float64)[:, None] * theta ** (-i / d_h)
+    return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+
+
+class PagedCache:
+    """Pools ``k``, ``v`` [n_blocks, n_kv, 64, d_h] (bf16 or fp32), the block
+    table [batch, max_pages] (int32) and, for the page scores, the mean keys
+    ``means`` [n_blocks, n_kv, d_h] that ``append`` maintains.  The tensors stay
+    the caller's; nothing is copied.  ``attend`` and ``attend_pages`` keep one
+    scratch buffer per object, so calls of one object that may overlap on the
+    device (other streams) need objects of their own."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_q: int,
+                 means: Optional[torch.Tensor] = None):
+        if k.dtype not in _TYPES or v.dtype != k.dtype or k.dim() != 4 or k.shape != v.shape or k.shape[2] != PAGE \
+                or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("pools must be contiguous [n_blocks, n_kv, 64, d_h] of one type (float32 or bfloat16)")
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("the block table must be a contiguous int32 [batch, max_pages]")
+        if means is not None and (means.dtype != k.dtype or not means.is_contiguous() or
+                                  means.shape != (k.shape[0], k.shape[1], k.shape[3])):
+            raise ValueError("means must be contiguous [n_blocks, n_kv, d_h] of the pools' type")
+        if not k.is_cuda or any(t.device != k.device for t in (v, table) + (() if means is None else (means,))):
+            raise ValueError("pools, table and means must be on one CUDA device")
+        self.k, self.v, self.table, self.means = k, v, table, means
+        self.n_q, self.n_kv, self.d_h, self.dtype, self.device = n_q, k.shape[1], k.shape[3], k.dtype, k.device
+        self._c = capi.pipo_paged(_TYPES[k.dtype], n_q, k.shape[1], k.shape[3], PAGE, k.shape[0], table.shape[1],
+                                  table.shape[0], k.data_ptr(), v.data_ptr(),
+                                  None if means is None else means.data_ptr(), table.data_ptr())
+        self._scratch: Optional[torch.Tensor] = None
+        self._scratch_for = -1
+
+    # ---- arguments
+
+    def _batch(self, q_start: torch.Tensor, kv_len: torch.Tensor) -> None:
+        n = self.table.shape[0]
+        if q_start.dtype != torch.int32 or kv_len.dtype != torch.int32 or q_start.shape != (n + 1,) or \
+                kv_len.shape != (n,) or not q_start.is_contiguous() or not kv_len.is_contiguous() or \
+                q_start.device != self.device or kv_len.device != self.device:
+            raise ValueError(f"q_start [{n + 1}] and kv_len [{n}] must be contiguous int32 on the pools' device")
+        self._c.q_start, self._c.kv_len = q_start.data_ptr(), kv_len.data_ptr()
+
+    def _rows(self, x: torch.Tensor, heads: int, name: str, like: Optional[torch.dtype] = None) -> int:
+        """Token stride of [tokens, heads, d_h] with the heads back to back."""
+        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.d_h or x.device != self.device or \
+                x.dtype != (like or self.dtype) or \
+                (x.shape[0] and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.d_h))):
+            raise ValueError(f"{name} must be [tokens, {heads}, {self.d_h}] {like or self.dtype} with whole rows")
+        return x.stride(0) if x.shape[0] > 1 else heads * self.d_h
+
+    def _work(self, tokens: int) -> torch.Tensor:
+        if self._scratch_for != tokens:
+            need = capi.pipo_op_attn_paged_scratch(self._c, tokens)
+            if self._scratch is None or self._scratch.numel() < need:
+                self._scratch = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
+            self._scratch_for = tokens
+        return self._scratch
+
+    # ---- the calls
+
+    def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor,
+               kv_len: torch.Tensor, *, q_gain: Optional[torch.Tensor] = None,
+               k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, rope: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Normalise (where a gain is given) and rotate (where a table is) the
+        new queries and keys, append keys and values, update the page means.
+        Returns the queries [tokens, n_q, d_h] in the pools' type (None without q)."""
+        self._batch(q_start, kv_len)
+        if k.dtype not in _TYPES:
+            raise ValueError("keys must be float32 or bfloat16")
+        tokens = k.shape[0]
+        ld_k, ld_v = self._rows(k, self.n_kv, "k", k.dtype), self._rows(v, self.n_kv, "v", k.dtype)
+        ld_q = self._rows(q, self.n_q, "q", k.dtype) if q is not None else 0
+        if v.shape[0] != tokens or (q is not None and q.shape[0] != tokens):
+            raise ValueError("q, k and v must have the same number of tokens")
+        for gain in (q_gain, k_gain):
+            if gain is not None and (gain.dtype != self.dtype or gain.shape != (self.d_h,) or
+                                     not gain.is_contiguous() or gain.device != self.device):
+                raise ValueError("gains must be [d_h] of the pools' type")
+        if rope is not None and (rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1] != self.d_h // 2 or
+                                 rope.shape[2] != 2 or not rope.is_contiguous() or rope.device != self.device):
+            raise ValueError("rope must be a contiguous float32 [positions, d_h / 2, 2]")
+        if q is None:
+            out = None
+        elif out is None:
+            out = torch.empty((tokens, self.n_q, self.d_h), dtype=self.dtype, device=self.device)
+        elif out.shape != (tokens, self.n_q, self.d_h) or out.dtype != self.dtype or not out.is_contiguous() or \
+                out.device != self.device:
+            raise ValueError("out must be a contiguous [tokens, n_q, d_h] of the pools' type")
+        p = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
+        capi.pipo_op_kv_append(self._c, tokens, _TYPES[k.dtype], p(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
+                               p(q_gain), p(k_gain), eps, p(rope), 0 if rope is None else rope.shape[0], p(out),
+                               torch.cuda.current_stream(self.device).cuda_stream)
+        return out
+
+    def _out(self, q: torch.Tensor, out: Optional[torch.Tensor]) -> Tuple[torch.Tensor, int]:
+        if out is None:
+            out = torch.empty((q.shape[0], self.n_q, self.d_h), dtype=self.dtype, device=self.device)
+            return out, self.n_q * self.d_h
+        if out.shape[0] != q.shape[0]:
+            raise ValueError("out must have a row for every token")
+        return out, self._rows(out, self.n_q, "out")
+
+    def attend(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
+               scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Causal attention of the new tokens over the cache; ``window`` > 0
+        keeps the last ``window`` entries of every token.  scale: 1/sqrt(d_h)
+        unless given."""
+        self._batch(q_start, kv_len)
+        ld_q = self._rows(q, self.n_q, "q")
+        out, ld_out = self._out(q, out)
+        w = self._work(q.shape[0])
+        capi.pipo_op_attn_paged(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
+                                window, out.data_ptr(), ld_out, w.data_ptr(), w.numel(),
+                                torch.cuda.current_stream(self.device).cuda_stream)
+        return out
+
+    def page_scores(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """fp32 [tokens, n_kv, max_pages]: the score of every page a token sees,
+        -inf for the others."""
+        if self.means is None:
+            raise ValueError("page scores need a cache with means")
+        self._batch(q_start, kv_len)
+        ld_q = self._rows(q, self.n_q, "q")
+        shape = (q.shape[0], self.n_kv, self.table.shape[1])
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=self.device)
+        elif out.shape != shape or out.dtype != torch.float32 or not out.is_contiguous() or out.device != self.device:
+            raise ValueError("out must be a contiguous float32 [tokens, n_kv, max_pages]")
+        capi.pipo_op_page_scores(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
+                                 out.data_ptr(), torch.cuda.current_stream(self.device).cuda_stream)
+        return out
+
+    def attend_pages(self, q: torch.Tensor, scores: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
+                     top: int, sink: int = 1, local: int = 1, scale: Optional[float] = None,
+                     out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Causal attention over ``top`` pages per token and kv head: the first
+        ``sink``, the last ``local`` and the best scored.  Returns the outputs
+        and the pages, int32 [tokens, n_kv, top], ascending, -1 behind the last."""
+        self._batch(q_start, kv_len)
+        ld_q = self._rows(q, self.n_q, "q")
+        if scores.shape != (q.shape[0], self.n_kv, self.table.shape[1]) or scores.dtype != torch.float32 or \
+                not scores.is_contiguous() or scores.device != self.device:
+            raise ValueError("scores must be a contiguous float32 [tokens, n_kv, max_pages]")
+        out, ld_out = self._out(q, out)
+        pages = torch.empty((q.shape[0], self.n_kv, top), dtype=torch.int32, device=self.device)
+        w = self._work(q.shape[0])
+        capi.pipo_op_attn_pages(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
+                                scores.data_ptr(), top, sink, local, out.data_ptr(), ld_out, pages.data_ptr(),
+                                w.data_ptr(), w.numel(), torch.cuda.current_stream(self.device).cuda_stream)
+        return out, pages

@@ -187,3 +187,37 @@ def test_header_compiles_as_cplusplus():
     """The header also compiles as C++ (its extern "C" block), with warnings as errors."""
     import subprocess
     subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsyntax-only", "-x", "c++", HEADER])
+
+
+def test_paged_layout_matches_header():
+    assert [f for f, _ in capi.pipo_paged._fields_] == struct_fields("pipo_paged")
+
+
+def test_paged_units_are_built():
+    """Every .cu file of csrc/paged is a unit of the library build."""
+    import glob
+    csrc = os.path.join(ROOT, "paper_2605_27255_gb300", "csrc")
+    units = sorted(os.path.relpath(p, csrc) for p in glob.glob(os.path.join(csrc, "paged", "*.cu")))
+    assert units == sorted(build.PAGED_SOURCES)
+
+
+def test_paged_calls_reject_bad_descriptions_without_a_gpu(lib):
+    """EINVAL before any CUDA call, with a message; batch 0 is a no-op."""
+    L = capi.load()
+    ok = dict(dtype=1, n_q_heads=8, n_kv_heads=2, head_dim=64, page_size=64, n_blocks=4, max_pages=2, batch=0)
+    c = capi.pipo_paged(**ok)
+    assert L.pipo_op_attn_paged(c, 5, None, 0, 1.0, 0, None, 0, None, 0, None) == capi.PIPO_OK
+    for key, bad in (("dtype", 2), ("n_q_heads", 9), ("n_q_heads", 34), ("head_dim", 96), ("page_size", 32),
+                     ("n_blocks", 0), ("max_pages", 0), ("batch", -1), ("batch", 5000)):
+        c = capi.pipo_paged(**{**ok, key: bad})
+        assert L.pipo_op_attn_paged(c, 5, None, 0, 1.0, 0, None, 0, None, 0, None) == capi.PIPO_EINVAL, key
+        assert L.pipo_op_kv_append(c, 5, 0, None, 0, None, 0, None, 0, None, None, 0.0, None, 0, None,
+                                   None) == capi.PIPO_EINVAL, key
+        assert L.pipo_op_page_scores(c, 5, None, 0, 1.0, None, None) == capi.PIPO_EINVAL, key
+        assert L.pipo_op_attn_pages(c, 5, None, 0, 1.0, None, 1, 0, 1, None, 0, None, None, 0, None) == \
+            capi.PIPO_EINVAL, key
+        assert L.pipo_op_attn_paged_scratch(c, 5) == 0, key
+        assert capi.pipo_last_error(None)
+    c = capi.pipo_paged(**{**ok, "batch": 1})
+    assert L.pipo_op_attn_paged(c, 5, None, 0, 1.0, 0, None, 0, None, 0, None) == capi.PIPO_EINVAL  # null pointers
+    assert L.pipo_op_attn_paged(None, 5, None, 0, 1.0, 0, None, 0, None, 0, None) == capi.PIPO_EINVAL
