@@ -18,7 +18,7 @@ LIB = os.path.join(LIBDIR, "libpipo.so")
 # the host code first (the longest units start first)
 SOURCES = ["k_gemv_bf16.cu", "k_gemv_f32.cu", "k_attn.cu", "pipo_capi.cu", "k_tc.cu"]
 # the operators on caller-owned paged caches
-PAGED_SOURCES = ["paged/k_paged.cu", "paged/paged_capi.cu"]
+PAGED_SOURCES = ["paged/k_paged.cu", "paged/k_paged_tc.cu", "paged/paged_capi.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -1,0 +1,477 @@
+// Attention of ragged chunks over a paged bf16 cache on the tensor cores
+// (tcgen05, sm_103a).
+//
+// out = softmax(scale Q K^T) V for row tiles of 128 rows (tokens times the query
+// heads of one kv head), the rows of the MMAs, over 128 cache entries at a time:
+//   S = Q K^T   fp32 in TMEM, Q and K from shared memory (K-major);
+//   softmax     one thread per row: it reads the row's 128 scores, keeps the
+//               running maximum and sum in fp32, and writes exp2 of the scores back over
+//               them as bf16 (the A operand of the next MMAs, from TMEM).  bf16
+//               weights carry 2^-9 of a weight, about the output's own
+//               rounding; their sum is taken before the rounding;
+//   O += P V    fp32 in TMEM over the whole item; V is the [entry][dim] tile as it
+//               lies in the cache (MN-major).  The reference that the
+//               exponents are taken against moves only when the running maximum
+//               has passed it by 2^8: until then the weights are at most 256 and
+//               neither O nor the sum is touched; when it moves the row's
+//               thread rescales its row of O in TMEM.
+//
+// A CTA runs two such pipelines side by side, so that the MMAs of one run under
+// the softmax of the other:
+//   PAIR    the two halves of a 256-row tile: both read each K and V tile
+//           (one copy, two uses).  Chunks of many rows.
+//   single  two workers with items of their own (work.cuh), 128 rows each, and a
+//           ring of copies each.  Few rows per sequence, listed pages.
+//
+// Roles (384 threads): warps 0 and 2 copy K and V tiles (TMA boxes of one page x
+// 64 dims, 128-byte swizzle) and warps 1 and 3 issue the MMAs (PAIR: warps 0
+// and 1 alone), warps 4-7 and 8-11 are the two softmax warpgroups, which also
+// load the queries and write the outputs.  Cache slots past a sequence's end may hold
+// anything: their scores are masked, and the MMA warp clears their values in
+// shared memory (0 times NaN would be NaN).
+//
+// Every wait is bounded; when one gives up the error word is set, every role
+// stops, and the copies and commits in flight are waited for before the CTA ends.
+#pragma once
+
+#include "../attn_prefill.cuh"
+#include "work.cuh"
+
+namespace pipo {
+
+constexpr int kAtThreads = 384;
+constexpr int kAtRegsIo = 56, kAtRegsSoft = 224;
+static_assert(kAtRegsIo + 2 * kAtRegsSoft <= 3 * 168, "register shares must fit the launch's registers");
+constexpr int kAtHalf = 128 * 128;  // 64 dims of a tile: 128 rows of 128 bytes
+constexpr float kAtSlack = 8.f;     // exponents above the reference before it moves
+
+__host__ __device__ constexpr int at_tile_bytes(int dh) { return dh / 64 * kAtHalf; }
+// stages of one ring
+__host__ __device__ constexpr int at_stages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
+    return 1024 + (size_t)at_tile_bytes(dh) * (2 + at_stages(dh, pair) * (pair ? 1 : 2));
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// 32 consecutive fp32 columns of this thread's TMEM lane, without the wait
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,"
+        "%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// the loaded values exist from here on: nothing may use them before the wait
+__device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+}
+
+template <int DH, bool PAIR>
+__global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs p, ItemShape shape, int S,
+                                                                  int part_rows, size_t part_off,
+                                                                  const __grid_constant__ CUtensorMap tmK,
+                                                                  const __grid_constant__ CUtensorMap tmV) {
+    constexpr int kTile = at_tile_bytes(DH), ST = at_stages(DH, PAIR), NR = PAIR ? 1 : 2;  // NR: rings
+    constexpr int kPageHalf = kPage * 128;  // 64 dims of a page
+    extern __shared__ __align__(1024) unsigned char at_smem_raw[];
+    __shared__ uint32_t tmem_base;
+    __shared__ __align__(8) uint64_t full[NR][ST], empty[NR][ST];
+    __shared__ __align__(8) uint64_t q_full[2], s_full[2], p_full[2], o_full[2], drained[2];
+    __shared__ Piece pieces[NR];
+    __shared__ int give_up;
+
+    unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* q_s = sm;              // two query tiles
+    unsigned char* ring_s = sm + 2 * kTile;  // NR rings of ST stages
+
+    const PagedArgs& c = p.c;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == 0) tmem_alloc(&tmem_base, 512);
+    if (threadIdx.x == 32) {
+        prefetch_tmap(&tmK);
+        prefetch_tmap(&tmV);
+        for (int r = 0; r < NR; ++r)
+            for (int i = 0; i < ST; ++i) {
+                mbar_init(&full[r][i], 1);
+                mbar_init(&empty[r][i], 1);
+            }
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(q_full + w, 4);  // softmax warps
+            mbar_init(s_full + w, 1);
+            mbar_init(p_full + w, 4);
+            mbar_init(o_full + w, 1);
+            mbar_init(drained + w, 1);
+        }
+        give_up = 0;
+        mbar_init_fence();
+    }
+    // (the sequences' tile counts use the ring's memory before any copy)
+    find_pieces<kAtThreads, NR>(c, shape, (int)blockIdx.x * NR, S, reinterpret_cast<int*>(ring_s), pieces,
+                                reinterpret_cast<int*>(p.scratch));
+    fence_proxy_async();  // those generic accesses, before the copies into the ring
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_launch();  // after the allocation: a dependent CTA must not take this SM's TMEM first
+    const uint32_t tmem = tmem_base;
+
+    // bounded wait of a whole warp that stops every role of the CTA once it gives up
+    auto wait = [&](uint64_t* bar, uint32_t parity, unsigned site, int it) -> bool {
+        bool got = mbar_try_wait(bar, parity);
+        if (!got && !*(volatile int*)&give_up) got = mbar_wait(bar, parity, site, (unsigned)it);
+        got = __all_sync(0xffffffffu, got);
+        if (!got) *(volatile int*)&give_up = 1;
+        return got;
+    };
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtRegsIo));
+        const int ring = warp >> 1;  // PAIR: warps 2 and 3 have nothing to do
+        if (!(PAIR && ring == 1)) {
+            ItemWalk it;
+            it.start(c, shape, pieces[PAIR ? 0 : ring], (int)blockIdx.x * NR + ring);
+            uint64_t* fu = full[PAIR ? 0 : ring];
+            uint64_t* em = empty[PAIR ? 0 : ring];
+            unsigned char* rs = ring_s + (size_t)(PAIR ? 0 : ring) * ST * kTile;
+            if ((warp & 1) == 0) {
+                // ---- copies: K then V of every unit
+                int k = 0;  // copies issued
+                bool ok = true;
+                for (; it.more() && ok; it.next()) {
+                    const int32_t* list =
+                        shape.n_top > 0 ? p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top : nullptr;
+                    const int seen = (it.len + kPage - 1) / kPage;  // pages with entries
+                    int held = -32, mine = -1;                      // lane l holds page held + l
+                    for (int u = it.kv0; u < it.kv1 && ok; ++u) {
+                        const int pg = (it.t0 + u) * 2;  // index in the cache or the list
+                        if (pg >= held + 32) {
+                            held = pg;
+                            const int i = pg + lane;
+                            if (list) {
+                                const int q = i < shape.n_top ? list[i] : -1;
+                                mine = q >= 0 ? page_block(c, it.b, q) : -1;
+                            } else {
+                                mine = i < seen ? page_block(c, it.b, i) : -1;
+                            }
+                        }
+                        int blk[2];
+                        blk[0] = __shfl_sync(0xffffffffu, mine, pg - held);
+                        blk[1] = __shfl_sync(0xffffffffu, mine, pg - held + 1);
+                        const int np = blk[0] < 0 ? 0 : blk[1] < 0 ? 1 : 2;
+#pragma unroll
+                        for (int v = 0; v < 2 && ok; ++v, ++k) {
+                            const int st = k % ST;
+                            ok = k < ST || wait(em + st, (uint32_t)(((k / ST) & 1) ^ 1), 51, k);
+                            if (!ok) break;
+                            if (lane == 0) {
+                                if (np == 0) mbar_arrive(fu + st);
+                                else mbar_arrive_expect_tx(fu + st, (uint32_t)(np * (DH / 64) * kPageHalf));
+                                for (int i = 0; i < np; ++i)
+                                    for (int d = 0; d < DH / 64; ++d)
+                                        tma_load_2d(rs + (size_t)st * kTile + d * kAtHalf + i * kPageHalf, v ? &tmV : &tmK,
+                                                    d * 64, (blk[i] * c.n_kv + it.g) * kPage, fu + st);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+                // no copy into this CTA's shared memory is in flight at its end
+                if (lane == 0) ring_drain<ST>(k, [&](int st, uint32_t ph, int i) { mbar_wait(fu + st, ph, 52, (unsigned)i); });
+            } else {
+                // ---- MMAs.  TMEM: scores / weights of pipeline w at w * 128, its output at 256 + w * 128
+                constexpr uint32_t id_s = umma_idesc_bf16(128, kTileEnt);
+                constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
+                int k = 0;                 // ring position
+                int qn[2] = {0, 0};        // items begun
+                int pn[2] = {0, 0};        // units of weights
+                bool ok = true;
+                auto scores = [&](int w, int st) {
+                    const uint32_t d = tmem + (uint32_t)(w * 128), qb = smem_u32(q_s) + w * kTile,
+                                   kb = smem_u32(rs) + st * kTile;
+                    if (lane == 0) {
+#pragma unroll
+                        for (int i = 0; i < DH / 16; ++i) {
+                            const uint32_t o = (i >> 2) * kAtHalf + (i & 3) * 32;
+                            umma_bf16(d, umma_desc_sw128(qb + o), umma_desc_sw128(kb + o), id_s, i > 0 ? 1u : 0u);
+                        }
+                        umma_commit(s_full + w);
+                    }
+                    __syncwarp();
+                };
+                auto values = [&](int w, int st, bool first) {
+                    const uint32_t a = tmem + (uint32_t)(w * 128), d = tmem + 256u + (uint32_t)(w * 128),
+                                   vb = smem_u32(rs) + st * kTile;
+                    if (lane == 0) {
+#pragma unroll
+                        for (int i = 0; i < kTileEnt / 16; ++i)
+                            umma_bf16_ta(d, a + i * 8, umma_desc_mn128(vb + i * 2048), id_o, !first || i > 0 ? 1u : 0u);
+                        umma_commit(o_full + w);
+                    }
+                    __syncwarp();
+                };
+                auto free_stage = [&](int st) {
+                    if (lane == 0) umma_commit(em + st);
+                };
+                const int w0 = PAIR ? 0 : ring;
+                for (; it.more() && ok; it.next()) {
+                    const int rows = it.tokens() * c.G;
+                    const bool two = PAIR && rows > 128;
+                    // entries whose values may be anything: those past the sequence's (or the list's) end
+                    int end = it.len;
+                    if (shape.n_top > 0) {
+                        const int pos = it.len - it.n + it.tile;
+                        const int kept = pos < 0 ? 0 : min(shape.n_top, pos / kPage + 1);
+                        const int32_t* list = p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top;
+                        end = kept == 0 ? 0 : (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage + 1 : kPage);
+                    }
+                    ok = wait(q_full + w0, (uint32_t)(qn[0] & 1), 53, qn[0]) &&
+                         (!two || wait(q_full + 1, (uint32_t)(qn[1] & 1), 53, qn[1])) &&
+                         wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k);
+                    if (!ok) break;
+                    ++qn[0];
+                    if (two) ++qn[1];
+                    tc_fence_after();
+                    scores(w0, k % ST);
+                    if (two) scores(1, k % ST);
+                    free_stage(k % ST);
+                    ++k;
+                    for (int u = it.kv0; u < it.kv1; ++u) {
+                        const int vst = k % ST;
+                        ok = wait(fu + vst, (uint32_t)((k / ST) & 1), 54, k);
+                        if (!ok) break;
+                        const int tail = end - (it.t0 + u) * kTileEnt;
+                        if (tail < kTileEnt) {  // (the generic stores are ordered before the MMAs that read them)
+                            const int r0 = max(0, tail);
+                            for (int i = lane; i < (kTileEnt - r0) * (DH / 8); i += 32) {
+                                const int r = r0 + i / (DH / 8), ch = i % (DH / 8);
+                                *reinterpret_cast<uint4*>(rs + (size_t)vst * kTile + (ch >> 3) * kAtHalf + r * 128 +
+                                                          (ch & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            fence_proxy_async();
+                            __syncwarp();
+                        }
+                        const bool last = u + 1 == it.kv1;
+                        const int kst = (k + 1) % ST;
+                        ok = wait(p_full + w0, (uint32_t)(pn[0] & 1), 55, pn[0]);
+                        if (!ok) break;
+                        tc_fence_after();
+                        values(w0, vst, u == it.kv0);
+                        if (!last) {
+                            ok = wait(fu + kst, (uint32_t)(((k + 1) / ST) & 1), 54, k + 1) &&
+                                 wait(o_full + w0, (uint32_t)(pn[0] & 1), 56, pn[0]);
+                            if (!ok) break;
+                            scores(w0, kst);
+                        }
+                        ++pn[0];
+                        if (two) {
+                            ok = wait(p_full + 1, (uint32_t)(pn[1] & 1), 55, pn[1]);
+                            if (!ok) break;
+                            tc_fence_after();
+                            values(1, vst, u == it.kv0);
+                            free_stage(vst);
+                            if (!last) {
+                                ok = wait(o_full + 1, (uint32_t)(pn[1] & 1), 56, pn[1]);
+                                if (!ok) break;
+                                scores(1, kst);
+                            }
+                            ++pn[1];
+                        } else {
+                            free_stage(vst);
+                        }
+                        if (!last) {
+                            free_stage(kst);
+                            ++k;
+                        }
+                        ++k;
+                    }
+                }
+                // commits arrive in order: after one more, none is in flight at the CTA's end
+                if (lane == 0) {
+                    umma_commit(drained + ring);
+                    mbar_wait(drained + ring, 0, 57);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kAtRegsSoft));
+        // ---- softmax warpgroup w: thread = row r of its tile
+        const int w = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane, wt = threadIdx.x - 128 - w * 128;
+        const uint32_t lane_addr = tmem + ((uint32_t)(quad * 32) << 16);
+        const uint32_t s_col = lane_addr + (uint32_t)(w * 128), o_col = lane_addr + 256u + (uint32_t)(w * 128);
+        const int me = (int)blockIdx.x * NR + (PAIR ? 0 : w);
+        const float c2 = p.scale * 1.4426950408889634f;  // exponents of two
+        ItemWalk it;
+        it.start(c, shape, pieces[PAIR ? 0 : w], me);
+        int sn = 0;  // units seen
+        bool ok = true;
+        for (; it.more() && ok; it.next()) {
+            const int rows = min(128, it.tokens() * c.G - (PAIR ? w * 128 : 0));
+            if (rows <= 0) continue;
+            const int row0 = PAIR ? w * 128 : 0, i0 = it.tile * shape.TP;
+            // the queries of this tile; rows past the last one are zero
+            {
+                const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)it.g * c.G * DH;
+                for (int i = wt; i < 128 * (DH / 8); i += 128) {
+                    const int v = i / (DH / 8), ch = i % (DH / 8);
+                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                    if (v < rows) {
+                        const int row = row0 + v, tok = it.q0 + i0 + row / c.G;
+                        x = *reinterpret_cast<const uint4*>(q + (size_t)tok * p.ld_q + (size_t)(row % c.G) * DH + ch * 8);
+                    }
+                    *reinterpret_cast<uint4*>(q_s + w * kTile + (ch >> 3) * kAtHalf + v * 128 + (((ch & 7) ^ (v & 7)) << 4)) = x;
+                }
+                fence_proxy_async();  // the generic stores above, before the MMAs read them
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full + w);
+            }
+            const bool live = quad * 32 < rows;  // this warp has rows at all
+            const int tok = i0 + (row0 + min(r, rows - 1)) / c.G;
+            int pos = it.len - it.n + tok, lo = p.window > 0 ? pos - p.window + 1 : 0;
+            if (shape.n_top > 0) {  // positions in the list's own order
+                const int kept = pos < 0 ? 0 : min(shape.n_top, pos / kPage + 1);
+                const int32_t* list = p.pages + ((size_t)(it.q0 + tok) * c.n_kv + it.g) * shape.n_top;
+                if (kept > 0) pos = (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage : kPage - 1);
+            }
+            float m_ref = -INFINITY, l = 0.f;
+            for (int u = it.kv0; u < it.kv1; ++u, ++sn) {
+                ok = wait(s_full + w, (uint32_t)(sn & 1), 58, sn);
+                if (!ok) break;
+                tc_fence_after();
+                if (live) {
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tmem_ld32_issue(s_col + 32 * i, s[i]);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pin32(s[i]);
+                    const int e0 = (it.t0 + u) * kTileEnt;
+                    if (e0 + kTileEnt - 1 > pos || e0 < lo) {
+#pragma unroll
+                        for (int i = 0; i < 128; ++i)
+                            if (e0 + i > pos || e0 + i < lo) s[i >> 5][i & 31] = 0xff800000u;
+                    }
+                    float mt[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mt[i] = __uint_as_float(s[i][0]);
+#pragma unroll
+                    for (int j = 1; j < 32; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mt[i] = fmaxf(mt[i], __uint_as_float(s[i][j]));
+                    const float top = fmaxf(fmaxf(mt[0], mt[1]), fmaxf(mt[2], mt[3])) * c2;
+                    // the reference moves when the maximum has passed it by the slack (or it is the first one)
+                    const bool move = top > m_ref + kAtSlack;
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float f = move ? (m_ref == -INFINITY ? 0.f : ex2(m_ref - top)) : 1.f;
+                        if (move) m_ref = top;
+                        l *= f;
+                        if (u > it.kv0) {  // the output so far, once the values of the unit before are in it
+                            ok = wait(o_full + w, (uint32_t)((sn - 1) & 1), 59, sn);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int h = 0; h < DH / 32; ++h) {
+                                uint32_t o[32];
+                                tmem_ld32_issue(o_col + 32 * h, o);
+                                tmem_ld_wait();
+                                pin32(o);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tmem_st32(o_col + 32 * h, o);
+                            }
+                        }
+                    }
+                    const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t pk[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const int e = h * 64 + 2 * i;
+                            const float p0 = ex2(fmaf(__uint_as_float(s[e >> 5][e & 31]), c2, neg));
+                            const float p1 = ex2(fmaf(__uint_as_float(s[e >> 5][(e & 31) + 1]), c2, neg));
+                            sum[(2 * i) & 3] += p0;
+                            sum[(2 * i + 1) & 3] += p1;
+                            pk[i] = pack_bf16x2(p0, p1);
+                        }
+                        tmem_st32(s_col + 32 * h, pk);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + w);
+            }
+            if (!ok) break;
+            ok = wait(o_full + w, (uint32_t)((sn - 1) & 1), 59, sn);
+            if (!ok) break;
+            tc_fence_after();
+            if (!live) {
+                // (row 0's warp writes the item's meta)
+            } else if (it.whole()) {
+                const float inv = l > 0.f ? 1.0f / l : 0.f;
+                bf16_t* o = static_cast<bf16_t*>(p.out) + (size_t)(it.q0 + tok) * p.ld_out +
+                            (size_t)(it.g * c.G + (row0 + min(r, rows - 1)) % c.G) * DH;
+#pragma unroll
+                for (int h = 0; h < DH / 32; ++h) {
+                    uint32_t v[32];
+                    tmem_ld32_issue(o_col + 32 * h, v);
+                    tmem_ld_wait();
+                    pin32(v);
+                    if (r < rows) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t x[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                x[e] = pack_bf16x2(__uint_as_float(v[i + 2 * e]) * inv, __uint_as_float(v[i + 2 * e + 1]) * inv);
+                            *reinterpret_cast<uint4*>(o + 32 * h + i) = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                    }
+                }
+            } else {
+                float* part = reinterpret_cast<float*>(p.scratch + part_off) +
+                              ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
+#pragma unroll
+                for (int h = 0; h < DH / 32; ++h) {
+                    uint32_t v[32];
+                    tmem_ld32_issue(o_col + 32 * h, v);
+                    tmem_ld_wait();
+                    pin32(v);
+                    if (r < rows) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<uint4*>(part + (size_t)(row0 + r) * DH + 32 * h + i) =
+                                make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    }
+                }
+                if (r < rows)
+                    *reinterpret_cast<float2*>(part + (size_t)part_rows * DH + 2 * (row0 + r)) = make_float2(m_ref, l);
+            }
+            if (it.kv0 == 0 && row0 + r == 0)
+                reinterpret_cast<ItemMeta*>(p.scratch + kScratchHead)[(size_t)it.index * c.n_kv + it.g] = {
+                    it.b, it.tile, me, it.whole() ? me : it.last_worker()};
+            tc_fence_before();  // the output is read, before the next item's values overwrite it
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+}  // namespace pipo

@@ -1,6 +1,5 @@
 // Paged-cache operators: append, page scores, selection, attention on the CUDA
 // cores (a translation unit of its own).
-#include "../tma.cuh"
 #include "append.cuh"
 #include "attn_plain.cuh"
 #include "select.cuh"
@@ -62,7 +61,5 @@ cudaError_t launch_attn_plain(const AttnPagedArgs& a, cudaStream_t s) {
     }
     return cudaGetLastError();
 }
-
-cudaError_t take_error_paged(unsigned* code, unsigned* info) { return take_unit_error(code, info); }
 
 }  // namespace pipo

@@ -1,0 +1,65 @@
+// Paged-cache attention on the tensor cores (a translation unit of its own).
+#include "attn_tile.cuh"
+
+namespace pipo {
+
+namespace {
+
+template <int DH, bool PAIR>
+cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
+                    cudaStream_t s) {
+    auto* fn = &attn_tile_kernel<DH, PAIR>;
+    static thread_local int ready_dev = -1;  // the shared-memory limit is set per device
+    if (ready_dev != pl.dev) {
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at_smem(DH, PAIR));
+        if (e != cudaSuccess) return e;
+        ready_dev = pl.dev;
+    }
+    const ItemShape shape{pl.TP, a.window, a.pages ? a.n_top : 0};
+    fn<<<pl.ctas, kAtThreads, at_smem(DH, PAIR), s>>>(a, shape, pl.workers, pl.part_rows, pl.part_off, tk, tv);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 3) / 4));
+    lc.blockDim = dim3(128);
+    lc.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, &combine_kernel<DH, bf16_t>, a, shape, pl.part_rows, pl.part_off);
+}
+
+}  // namespace
+
+// The plan of a bf16 launch.  Pairs of row tiles when the sequences of the batch
+// have more than 128 rows on average; scratch: see work.cuh.
+AttnPlan plan_attn_tile(const PagedArgs& c, bool listed, int dev, int sms) {
+    AttnPlan pl{};
+    pl.dev = dev;
+    pl.pair = !listed && (long long)c.n_tokens * c.G > 128LL * c.batch;
+    const int rows = pl.pair ? 256 : 128;
+    pl.TP = listed ? 1 : rows / c.G;
+    pl.tiles = tiles_bound(c.n_tokens, c.batch, pl.TP);
+    const long long most = pl.tiles * c.n_kv * ((c.max_pages + 1) / 2);  // units at most
+    const int per = pl.pair ? 1 : 2;
+    pl.ctas = (int)(most < (long long)sms * per ? (most + per - 1) / per : sms);
+    pl.workers = pl.ctas * per;
+    const long long mine = (long long)c.n_tokens * c.G;
+    pl.part_rows = (int)(mine < (long long)pl.TP * c.G ? mine : (long long)pl.TP * c.G);
+    pl.part_rows += pl.part_rows & 1;
+    pl.part_off = meta_bytes(pl.tiles * c.n_kv);
+    pl.scratch = pl.part_off + (size_t)pl.workers * 2 * part_floats(pl.part_rows, c.dh) * sizeof(float);
+    return pl;
+}
+
+cudaError_t launch_attn_tile(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
+                             cudaStream_t s) {
+    if (a.c.dh == 64) return pl.pair ? tile_as<64, true>(a, pl, tk, tv, s) : tile_as<64, false>(a, pl, tk, tv, s);
+    return pl.pair ? tile_as<128, true>(a, pl, tk, tv, s) : tile_as<128, false>(a, pl, tk, tv, s);
+}
+
+cudaError_t take_error_paged(unsigned* code, unsigned* info) { return take_unit_error(code, info); }
+
+}  // namespace pipo

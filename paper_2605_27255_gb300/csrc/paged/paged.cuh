@@ -4,20 +4,12 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include "../kernels.cuh"
 #include "paged.h"
 
 namespace pipo {
 
 using bf16_t = __nv_bfloat16;
-
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(bf16_t x) { return __bfloat162float(x); }
-template <typename T>
-__device__ __forceinline__ T from_f(float x);
-template <>
-__device__ __forceinline__ float from_f<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ bf16_t from_f<bf16_t>(float x) { return __float2bfloat16_rn(x); }
 
 // N consecutive values as fp32 (N * sizeof(T) a multiple of 4 bytes up to 16, aligned to it)
 template <typename T, int N>
@@ -40,12 +32,6 @@ __device__ __forceinline__ void store_f(T* p, const float (&x)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v.e[i] = from_f<T>(x[i]);
     *reinterpret_cast<Pack*>(p) = v;
-}
-
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
 }
 
 // entries of sequence b, its new ones included

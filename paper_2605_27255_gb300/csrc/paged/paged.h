@@ -2,6 +2,7 @@
 // units share.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -60,11 +61,28 @@ struct SelectArgs {
     int32_t* pages;
 };
 
+// How a tensor-core attention launch is laid out (plan_attn_tile)
+struct AttnPlan {
+    int dev;
+    bool pair;          // two 128-row tiles per item share the copies
+    int TP;             // tokens per row tile
+    long long tiles;    // row tiles at most
+    int ctas, workers;
+    int part_rows;      // rows of a partial
+    size_t part_off;    // partials in the scratch
+    size_t scratch;     // bytes in all
+};
+
+// k_paged_tc.cu
+AttnPlan plan_attn_tile(const PagedArgs& c, bool listed, int dev, int sms);
+cudaError_t launch_attn_tile(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
+                             cudaStream_t s);
+cudaError_t take_error_paged(unsigned* code, unsigned* info);
+
 // k_paged.cu
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
 cudaError_t launch_page_scores(const ScoreArgs& a, cudaStream_t s);
 cudaError_t launch_page_select(const SelectArgs& a, cudaStream_t s);
 cudaError_t launch_attn_plain(const AttnPagedArgs& a, cudaStream_t s);
-cudaError_t take_error_paged(unsigned* code, unsigned* info);
 
 }  // namespace pipo

@@ -1,7 +1,11 @@
 // C entry points of the paged-cache operators: argument checks and launches.
+#include <cudaTypedefs.h>
+
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <mutex>
 
 #include "paged.h"
 #include "pipo.h"
@@ -80,6 +84,58 @@ bool attn_args_ok(const pipo_paged* c, int32_t n_tokens, const void* d_q, int64_
            scale > 0.f && std::isfinite(scale);
 }
 
+// current device and its SMs
+cudaError_t device_of(int* dev, int* sms) {
+    static thread_local int have = -1, count = 0;
+    cudaError_t e = cudaGetDevice(dev);
+    if (e == cudaSuccess && have != *dev) {
+        e = cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, *dev);
+        if (e == cudaSuccess) have = *dev;
+    }
+    *sms = count;
+    return e;
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+std::mutex g_encode_lock;
+
+// a pool as [n_blocks * n_kv * 64][d_h] bf16: boxes of one page x 64 dims, 128-byte swizzle
+pipo_status pool_map(const char* who, CUtensorMap* tm, void* pool, const PagedArgs& a) {
+    {
+        std::lock_guard<std::mutex> lk(g_encode_lock);
+        if (!g_encode) {
+            void* fn = nullptr;
+            cudaDriverEntryPointQueryResult q{};
+            const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+            if (e != cudaSuccess) return cuda_status(who, e);
+            if (q != cudaDriverEntryPointSuccess || !fn) return fail(PIPO_ECUDA, "%s: no cuTensorMapEncodeTiled", who);
+            g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+        }
+    }
+    const cuuint64_t dims[2] = {(cuuint64_t)a.dh, (cuuint64_t)a.n_blocks * a.n_kv * kPage};
+    const cuuint64_t strides[1] = {(cuuint64_t)a.dh * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)kPage}, es[2] = {1, 1};
+    const CUresult r = g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, pool, dims, strides, box, es,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? PIPO_OK : fail(PIPO_ECUDA, "%s: cuTensorMapEncodeTiled: error %d", who, (int)r);
+}
+
+// Scratch and launch of the attention calls
+pipo_status run_attn(const char* who, const AttnPagedArgs& a, size_t scratch_bytes, cudaStream_t s) {
+    if (!a.c.dtype) return cuda_status(who, launch_attn_plain(a, s));
+    int dev = 0, sms = 0;
+    const cudaError_t e = device_of(&dev, &sms);
+    if (e != cudaSuccess) return cuda_status(who, e);
+    const AttnPlan pl = plan_attn_tile(a.c, a.pages != nullptr, dev, sms);
+    if (scratch_bytes < pl.scratch)
+        return fail(PIPO_EINVAL, "%s: scratch needs %zu bytes, got %zu", who, pl.scratch, scratch_bytes);
+    CUtensorMap tk, tv;
+    pipo_status st = pool_map(who, &tk, a.c.k, a.c);
+    if (st == PIPO_OK) st = pool_map(who, &tv, a.c.v, a.c);
+    return st == PIPO_OK ? cuda_status(who, launch_attn_tile(a, pl, tk, tv, s)) : st;
+}
+
 }  // namespace
 
 extern "C" {
@@ -119,8 +175,11 @@ pipo_status pipo_op_kv_append(const pipo_paged* c, int32_t n_tokens, int32_t in_
 }
 
 size_t pipo_op_attn_paged_scratch(const pipo_paged* c, int32_t n_tokens) {
-    if (!paged_ok(c, n_tokens)) return 0;
-    return 16;
+    int dev = 0, sms = 0;
+    if (!paged_ok(c, n_tokens) || device_of(&dev, &sms) != cudaSuccess) return 0;
+    if (!c->dtype || c->batch == 0 || n_tokens == 0) return 16;
+    const PagedArgs a = args_of(c, n_tokens);
+    return std::max(plan_attn_tile(a, false, dev, sms).scratch, plan_attn_tile(a, true, dev, sms).scratch);
 }
 
 pipo_status pipo_op_attn_paged(const pipo_paged* c, int32_t n_tokens, const void* d_q, int64_t ld_q, float scale,
@@ -143,7 +202,7 @@ pipo_status pipo_op_attn_paged(const pipo_paged* c, int32_t n_tokens, const void
     a.scale = scale;
     a.window = window;
     a.scratch = static_cast<unsigned char*>(d_scratch);
-    return cuda_status("pipo_op_attn_paged", launch_attn_plain(a, static_cast<cudaStream_t>(stream)));
+    return run_attn("pipo_op_attn_paged", a, scratch_bytes, static_cast<cudaStream_t>(stream));
 }
 
 pipo_status pipo_op_page_scores(const pipo_paged* c, int32_t n_tokens, const void* d_q, int64_t ld_q, float scale,
@@ -196,7 +255,7 @@ pipo_status pipo_op_attn_pages(const pipo_paged* c, int32_t n_tokens, const void
     a.pages = d_pages;
     a.n_top = n_top;
     a.scratch = static_cast<unsigned char*>(d_scratch);
-    return cuda_status("pipo_op_attn_pages", launch_attn_plain(a, static_cast<cudaStream_t>(stream)));
+    return run_attn("pipo_op_attn_pages", a, scratch_bytes, static_cast<cudaStream_t>(stream));
 }
 
 pipo_status pipo_op_paged_check(uint32_t* h_info) {

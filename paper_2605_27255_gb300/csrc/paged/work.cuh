@@ -1,0 +1,293 @@
+// How the attention kernels share a ragged batch.
+//
+// The rows of a sequence (its new tokens times the query heads of one kv head)
+// are cut into row tiles of TP tokens; a row tile with one kv head is an item, and
+// an item is nt units, one per tile of kTileEnt cache entries that its rows
+// see.  The units of all items lie on one line (row tiles in order, within a
+// tile head by head), which S workers (or as many as there are units) cut into equal pieces: worker i takes
+// the units [i W / S, (i + 1) W / S).  So every worker reads the same amount
+// whatever the lengths are, a long cache with few rows is split over all of
+// them, and with many rows at most one item at each end of a worker's piece
+// is shared.  Of a shared item each worker leaves the running output, maximum
+// and sum of its part in the scratch; combine_kernel joins them in order, so the
+// result depends on the lengths alone, not on who came first.
+#pragma once
+
+#include "paged.cuh"
+
+namespace pipo {
+
+constexpr int kTileEnt = 128;  // entries per unit (two pages)
+
+// What a launch needs of an item's shape
+struct ItemShape {
+    int TP;         // tokens per row tile
+    int window;     // 0: none
+    int n_top;      // > 0: the entries are those of listed pages, and TP = 1
+};
+
+// Row tile j of a sequence with n new tokens and len entries
+struct RowTile {
+    int t0, nt;     // first unit (in kTileEnt entries from the start of the cache or of the list), units
+};
+__device__ __forceinline__ RowTile row_tile(const ItemShape& s, int n, int len, int j) {
+    const int i0 = j * s.TP, i1 = min(n, i0 + s.TP);
+    const int first = len - n + i0, last = len - n + i1 - 1;
+    if (s.n_top > 0) {
+        const int kept = last < 0 ? 0 : min(s.n_top, last / kPage + 1);
+        return {0, max(1, (kept + 1) / 2)};
+    }
+    const int hi = max(0, last + 1), lo = s.window > 0 ? min(hi, max(0, first - s.window + 1)) : 0;
+    const int t0 = lo / kTileEnt;
+    return {t0, max(1, (hi + kTileEnt - 1) / kTileEnt - t0)};
+}
+
+__device__ __forceinline__ int seq_new(const PagedArgs& c, int b) { return max(0, q_row(c, b + 1) - q_row(c, b)); }
+
+// scratch header, then one ItemMeta per item, then the partials
+struct ItemMeta {
+    int b, tile;        // sequence and row tile
+    int first, last;    // the workers that share it (first == last: nobody)
+};
+constexpr size_t kScratchHead = 16;  // int: number of row tiles
+
+__host__ __device__ inline long long tiles_bound(int n_tokens, int batch, int TP) {
+    const long long a = n_tokens, b = n_tokens / TP + (long long)batch;
+    return a < b ? a : b;
+}
+__host__ __device__ inline size_t meta_bytes(long long items) {
+    return (kScratchHead + (size_t)items * sizeof(ItemMeta) + 255) / 256 * 256;
+}
+// floats of one partial: rows of DH outputs, then (maximum, sum) of every row; an even
+// number of rows keeps every partial 16-byte aligned
+__host__ __device__ inline size_t part_floats(int rows, int dh) { return (size_t)rows * (dh + 2); }
+
+// A worker's piece: where it starts, and how many units it has.
+struct Piece {
+    int b, tile, g, kv;  // sequence, row tile in it, head, unit within the item
+    int index;           // row tile in the whole batch
+    int units;
+    long long at, total;  // unit on the line, units in all
+    int workers;         // that have units: S, or as many as there are units
+};
+
+// All threads of a block (NT of them): the piece of each of its NW workers
+// (w0 .. w0 + NW - 1 of S), written to `out` in shared memory.  seq_tiles:
+// batch + 1 ints of shared memory.  Block 0 also leaves the number of row tiles.
+template <int NT, int NW>
+__device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape& s, int w0, int S, int* seq_tiles,
+                                            Piece* out, int* n_tiles_out) {
+    __shared__ long long warp_units[NT / 32 + 1];
+    __shared__ int warp_tiles[NT / 32];
+    __shared__ int tiles_before;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // row tiles before every sequence
+    if (tid == 0) tiles_before = 0;
+    __syncthreads();
+    for (int b0 = 0; b0 < c.batch; b0 += NT) {
+        const int b = b0 + tid;
+        const int n = b < c.batch ? (seq_new(c, b) + s.TP - 1) / s.TP : 0;
+        int incl = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) warp_tiles[warp] = incl;
+        __syncthreads();
+        int before = tiles_before;
+        for (int w = 0; w < warp; ++w) before += warp_tiles[w];
+        if (b < c.batch) seq_tiles[b] = before + incl - n;
+        __syncthreads();
+        if (tid == NT - 1) tiles_before = before + incl;
+        __syncthreads();
+    }
+    // (offsets that decrease could count rows twice: never more tiles than the scratch has room for)
+    const int tiles = (int)min((long long)tiles_before, tiles_bound(c.n_tokens, c.batch, s.TP));
+    if (tid == 0) seq_tiles[c.batch] = tiles;
+    __syncthreads();
+    // this thread's run of row tiles and its units
+    const int x0 = (int)((long long)tiles * tid / NT), x1 = (int)((long long)tiles * (tid + 1) / NT);
+    int lo = 0, hi = c.batch - 1;  // the last b with seq_tiles[b] <= x0 (it holds x0: an empty sequence's start is its successor's)
+    while (lo < hi) {
+        const int m = (lo + hi + 1) >> 1;
+        if (seq_tiles[m] <= x0) lo = m; else hi = m - 1;
+    }
+    const int bfirst = lo;
+    auto walk = [&](auto&& fn) {  // fn(b, tile, x, shape) -> stop
+        int b = bfirst, n = 0, len = 0, loaded = -1;
+        for (int x = x0; x < x1; ++x) {
+            while (x >= seq_tiles[b + 1]) ++b;
+            if (b != loaded) {
+                n = seq_new(c, b);
+                len = seq_len(c, b);
+                loaded = b;
+            }
+            if (fn(b, x - seq_tiles[b], x, row_tile(s, n, len, x - seq_tiles[b]))) return;
+        }
+    };
+    long long mine = 0;
+    walk([&](int, int, int, const RowTile& r) {
+        mine += (long long)r.nt * c.n_kv;
+        return false;
+    });
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) warp_units[warp] = incl;
+    __syncthreads();
+    if (tid == 0) {
+        long long sum = 0;
+        for (int w = 0; w < NT / 32; ++w) {
+            const long long v = warp_units[w];
+            warp_units[w] = sum;
+            sum += v;
+        }
+        warp_units[NT / 32] = sum;
+        if (n_tiles_out && blockIdx.x == 0) *n_tiles_out = tiles;
+    }
+    if (tid < NW) out[tid].units = 0;
+    __syncthreads();
+    const long long total = warp_units[NT / 32], before = warp_units[warp] + incl - mine;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const int Sw = (int)min((long long)S, total);
+        if (w0 + w >= Sw) break;
+        const long long u0 = (long long)(w0 + w) * total / Sw, u1 = (long long)(w0 + w + 1) * total / Sw;
+        if (u0 >= before && u0 < before + mine) {
+            long long at = before;
+            walk([&](int b, int j, int x, const RowTile& r) {
+                const long long n = (long long)r.nt * c.n_kv;
+                if (u0 >= at + n) {
+                    at += n;
+                    return false;
+                }
+                const int off = (int)(u0 - at);
+                out[w] = {b, j, off / r.nt, off % r.nt, x, (int)(u1 - u0), u0, total, Sw};
+                return true;
+            });
+        }
+    }
+    __syncthreads();
+}
+
+// the worker that holds unit u
+__device__ __forceinline__ int worker_of(long long u, long long total, int S) { return (int)(((u + 1) * S - 1) / total); }
+
+// One worker's items in turn.  Every thread of a role keeps its own.
+struct ItemWalk {
+    const PagedArgs* c;
+    ItemShape s;
+    int S, me;
+    int b, tile, g, index, left;
+    long long at, total;
+    // the present item
+    int n, len, q0;      // new tokens and entries of the sequence, row of its first new token
+    int t0, nt;          // first unit, units of the item
+    int kv0, kv1;        // this worker's units of it
+    __device__ __forceinline__ void start(const PagedArgs& cc, const ItemShape& ss, const Piece& p, int me_) {
+        c = &cc;
+        s = ss;
+        S = p.workers;
+        me = me_;
+        b = p.b;
+        tile = p.tile;
+        g = p.g;
+        index = p.index;
+        left = p.units;
+        at = p.at;
+        total = p.total;
+        kv0 = p.kv;
+        if (left > 0) load();
+    }
+    __device__ __forceinline__ void load() {
+        n = seq_new(*c, b);
+        len = seq_len(*c, b);
+        q0 = q_row(*c, b);
+        shape();
+    }
+    __device__ __forceinline__ void shape() {
+        const RowTile r = row_tile(s, n, len, tile);
+        t0 = r.t0;
+        nt = r.nt;
+        kv1 = min(nt, kv0 + left);
+    }
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ bool whole() const { return kv0 == 0 && kv1 == nt; }
+    __device__ __forceinline__ int tokens() const { return min(s.TP, n - tile * s.TP); }
+    __device__ __forceinline__ void next() {
+        left -= kv1 - kv0;
+        at += kv1 - kv0;
+        kv0 = 0;
+        if (left <= 0) return;
+        if (++g < c->n_kv) {
+            kv1 = min(nt, left);
+            return;
+        }
+        g = 0;
+        ++index;
+        if (++tile * s.TP < n) {
+            shape();
+            return;
+        }
+        tile = 0;
+        do ++b;
+        while (b + 1 < c->batch && seq_new(*c, b) == 0);
+        load();
+    }
+    // the last worker that holds a unit of this item (asked by the one with its first unit)
+    __device__ __forceinline__ int last_worker() const { return worker_of(at - kv0 + nt - 1, total, S); }
+};
+
+// Joins the parts of the shared items.  grid (items, row groups of 4): one warp per row.
+// out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the workers first .. last in
+// order; the first one's part is its second slot, the others' their first.
+template <int DH, typename T>
+__global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, ItemShape s, int part_rows, size_t part_off) {
+    constexpr int N = DH / 32;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const PagedArgs& c = a.c;
+    const int item = blockIdx.x, lane = threadIdx.x & 31;
+    if (item / c.n_kv >= *reinterpret_cast<const int*>(a.scratch)) return;
+    const ItemMeta m = reinterpret_cast<const ItemMeta*>(a.scratch + kScratchHead)[item];
+    if (m.first == m.last) return;
+    const int row = blockIdx.y * 4 + (threadIdx.x >> 5);
+    const int i = m.tile * s.TP + row / c.G;
+    if (row >= s.TP * c.G || i >= seq_new(c, m.b)) return;
+    const float* parts = reinterpret_cast<const float*>(a.scratch + part_off);
+    auto part = [&](int w) { return parts + ((size_t)w * 2 + (w == m.first ? 1 : 0)) * part_floats(part_rows, DH); };
+    float M = -INFINITY;
+    for (int w = m.first + lane; w <= m.last; w += 32) M = fmaxf(M, part(w)[(size_t)part_rows * DH + 2 * row]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    const float ref = M == -INFINITY ? 0.f : M;
+    float L = 0.f, o[N] = {};
+    for (int w0 = m.first; w0 <= m.last; w0 += 32) {
+        float wt = 0.f;
+        if (w0 + lane <= m.last) {
+            const float2 ml = *reinterpret_cast<const float2*>(part(w0 + lane) + (size_t)part_rows * DH + 2 * row);
+            wt = exp2f(ml.x - ref);
+            L += wt * ml.y;
+        }
+        const int k = min(32, m.last - w0 + 1);
+#pragma unroll 8
+        for (int j = 0; j < k; ++j) {
+            const float f = __shfl_sync(0xffffffffu, wt, j);
+            float x[N];
+            load_f<float, N>(part(w0 + j) + (size_t)row * DH + lane * N, x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] = fmaf(f, x[e], o[e]);
+        }
+    }
+    L = warp_sum(L);
+    const float inv = L > 0.f ? 1.0f / L : 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] *= inv;
+    const int g = item % c.n_kv, t = q_row(c, m.b) + i;
+    store_f<T, N>(static_cast<T*>(a.out) + (size_t)t * a.ld_out + (size_t)(g * c.G + row % c.G) * DH + lane * N, o);
+}
+
+}  // namespace pipo
