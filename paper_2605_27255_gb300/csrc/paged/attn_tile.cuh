@@ -58,6 +58,29 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// pairs of fp32 values, the first one in the low word
+__device__ __forceinline__ uint64_t u32x2(uint32_t a, uint32_t b) { return (uint64_t)b << 32 | a; }
+__device__ __forceinline__ uint64_t f32x2(float a, float b) { return u32x2(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// 16 consecutive 32-bit columns of this thread's TMEM lane
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+
 // 32 consecutive fp32 columns of this thread's TMEM lane, without the wait
 __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(
@@ -139,7 +162,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         const int ring = warp >> 1;  // PAIR: warps 2 and 3 have nothing to do
         if (!(PAIR && ring == 1)) {
             ItemWalk it;
-            it.start(c, shape, pieces[PAIR ? 0 : ring], (int)blockIdx.x * NR + ring);
+            it.start(c, shape, pieces[PAIR ? 0 : ring]);
             uint64_t* fu = full[PAIR ? 0 : ring];
             uint64_t* em = empty[PAIR ? 0 : ring];
             unsigned char* rs = ring_s + (size_t)(PAIR ? 0 : ring) * ST * kTile;
@@ -147,7 +170,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 // ---- copies: K then V of every unit
                 int k = 0;  // copies issued
                 bool ok = true;
-                for (; it.more() && ok; it.next()) {
+                for (; it.more() && ok; it.next(c, shape)) {
                     const int32_t* list =
                         shape.n_top > 0 ? p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top : nullptr;
                     const int seen = (it.len + kPage - 1) / kPage;  // pages with entries
@@ -192,29 +215,36 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 constexpr uint32_t id_s = umma_idesc_bf16(128, kTileEnt);
                 constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
                 int k = 0;                 // ring position
-                int qn[2] = {0, 0};        // items begun
-                int pn[2] = {0, 0};        // units of weights
+                int qn0 = 0, qn1 = 0;      // items begun
+                int pn0 = 0, pn1 = 0;      // units of weights
                 bool ok = true;
+                // descriptors count in 16 bytes: a step along a tile is an addition
+                const uint64_t dq = umma_desc_sw128(smem_u32(q_s)), dk = umma_desc_sw128(smem_u32(rs)),
+                               dv = umma_desc_mn128(smem_u32(rs));
                 auto scores = [&](int w, int st) {
-                    const uint32_t d = tmem + (uint32_t)(w * 128), qb = smem_u32(q_s) + w * kTile,
-                                   kb = smem_u32(rs) + st * kTile;
                     if (lane == 0) {
+                        uint32_t qb = (uint32_t)dq + (uint32_t)(w * (kTile >> 4)), kb = (uint32_t)dk + (uint32_t)(st * (kTile >> 4));
+                        const uint32_t d = tmem + (uint32_t)(w * 128);
+                        asm volatile("" : "+r"(qb), "+r"(kb));  // eight sums now, not sixteen kept over the loop
 #pragma unroll
                         for (int i = 0; i < DH / 16; ++i) {
-                            const uint32_t o = (i >> 2) * kAtHalf + (i & 3) * 32;
-                            umma_bf16(d, umma_desc_sw128(qb + o), umma_desc_sw128(kb + o), id_s, i > 0 ? 1u : 0u);
+                            const uint32_t o = ((i >> 2) * kAtHalf + (i & 3) * 32) >> 4;
+                            umma_bf16(d, u32x2(qb + o, (uint32_t)(dq >> 32)), u32x2(kb + o, (uint32_t)(dk >> 32)), id_s,
+                                      i > 0 ? 1u : 0u);
                         }
                         umma_commit(s_full + w);
                     }
                     __syncwarp();
                 };
                 auto values = [&](int w, int st, bool first) {
-                    const uint32_t a = tmem + (uint32_t)(w * 128), d = tmem + 256u + (uint32_t)(w * 128),
-                                   vb = smem_u32(rs) + st * kTile;
                     if (lane == 0) {
+                        uint32_t vb = (uint32_t)dv + (uint32_t)(st * (kTile >> 4)), a = tmem + (uint32_t)(w * 128);
+                        asm volatile("" : "+r"(vb), "+r"(a));
+                        const uint32_t d = a + 256u;
 #pragma unroll
                         for (int i = 0; i < kTileEnt / 16; ++i)
-                            umma_bf16_ta(d, a + i * 8, umma_desc_mn128(vb + i * 2048), id_o, !first || i > 0 ? 1u : 0u);
+                            umma_bf16_ta(d, a + i * 8, u32x2(vb + i * (2048 >> 4), (uint32_t)(dv >> 32)), id_o,
+                                         i > 0 || !first ? 1u : 0u);
                         umma_commit(o_full + w);
                     }
                     __syncwarp();
@@ -223,8 +253,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     if (lane == 0) umma_commit(em + st);
                 };
                 const int w0 = PAIR ? 0 : ring;
-                for (; it.more() && ok; it.next()) {
-                    const int rows = it.tokens() * c.G;
+                for (; it.more() && ok; it.next(c, shape)) {
+                    const int rows = it.tokens(shape) * c.G;
                     const bool two = PAIR && rows > 128;
                     // entries whose values may be anything: those past the sequence's (or the list's) end
                     int end = it.len;
@@ -234,12 +264,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         const int32_t* list = p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top;
                         end = kept == 0 ? 0 : (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage + 1 : kPage);
                     }
-                    ok = wait(q_full + w0, (uint32_t)(qn[0] & 1), 53, qn[0]) &&
-                         (!two || wait(q_full + 1, (uint32_t)(qn[1] & 1), 53, qn[1])) &&
+                    ok = wait(q_full + w0, (uint32_t)(qn0 & 1), 53, qn0) &&
+                         (!two || wait(q_full + 1, (uint32_t)(qn1 & 1), 53, qn1)) &&
                          wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k);
                     if (!ok) break;
-                    ++qn[0];
-                    if (two) ++qn[1];
+                    ++qn0;
+                    if (two) ++qn1;
                     tc_fence_after();
                     scores(w0, k % ST);
                     if (two) scores(1, k % ST);
@@ -262,29 +292,29 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         }
                         const bool last = u + 1 == it.kv1;
                         const int kst = (k + 1) % ST;
-                        ok = wait(p_full + w0, (uint32_t)(pn[0] & 1), 55, pn[0]);
+                        ok = wait(p_full + w0, (uint32_t)(pn0 & 1), 55, pn0);
                         if (!ok) break;
                         tc_fence_after();
                         values(w0, vst, u == it.kv0);
                         if (!last) {
                             ok = wait(fu + kst, (uint32_t)(((k + 1) / ST) & 1), 54, k + 1) &&
-                                 wait(o_full + w0, (uint32_t)(pn[0] & 1), 56, pn[0]);
+                                 wait(o_full + w0, (uint32_t)(pn0 & 1), 56, pn0);
                             if (!ok) break;
                             scores(w0, kst);
                         }
-                        ++pn[0];
+                        ++pn0;
                         if (two) {
-                            ok = wait(p_full + 1, (uint32_t)(pn[1] & 1), 55, pn[1]);
+                            ok = wait(p_full + 1, (uint32_t)(pn1 & 1), 55, pn1);
                             if (!ok) break;
                             tc_fence_after();
                             values(1, vst, u == it.kv0);
                             free_stage(vst);
                             if (!last) {
-                                ok = wait(o_full + 1, (uint32_t)(pn[1] & 1), 56, pn[1]);
+                                ok = wait(o_full + 1, (uint32_t)(pn1 & 1), 56, pn1);
                                 if (!ok) break;
                                 scores(1, kst);
                             }
-                            ++pn[1];
+                            ++pn1;
                         } else {
                             free_stage(vst);
                         }
@@ -312,11 +342,11 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         const int me = (int)blockIdx.x * NR + (PAIR ? 0 : w);
         const float c2 = p.scale * 1.4426950408889634f;  // exponents of two
         ItemWalk it;
-        it.start(c, shape, pieces[PAIR ? 0 : w], me);
+        it.start(c, shape, pieces[PAIR ? 0 : w]);
         int sn = 0;  // units seen
         bool ok = true;
-        for (; it.more() && ok; it.next()) {
-            const int rows = min(128, it.tokens() * c.G - (PAIR ? w * 128 : 0));
+        for (; it.more() && ok; it.next(c, shape)) {
+            const int rows = min(128, it.tokens(shape) * c.G - (PAIR ? w * 128 : 0));
             if (rows <= 0) continue;
             const int row0 = PAIR ? w * 128 : 0, i0 = it.tile * shape.TP;
             // the queries of this tile; rows past the last one are zero
@@ -392,22 +422,23 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         }
                     }
                     const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    // two columns at a time (paired fp32 instructions), 32 columns per store
+                    const uint64_t c22 = f32x2(c2, c2), neg2 = f32x2(neg, neg);
+                    uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t pk[32];
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t pk[16];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const int e = h * 64 + 2 * i;
-                            const float p0 = ex2(fmaf(__uint_as_float(s[e >> 5][e & 31]), c2, neg));
-                            const float p1 = ex2(fmaf(__uint_as_float(s[e >> 5][(e & 31) + 1]), c2, neg));
-                            sum[(2 * i) & 3] += p0;
-                            sum[(2 * i + 1) & 3] += p1;
+                        for (int i = 0; i < 16; ++i) {
+                            const uint64_t e = fma_f32x2(u32x2(s[h][2 * i], s[h][2 * i + 1]), c22, neg2);
+                            const float p0 = ex2(__uint_as_float((uint32_t)e)), p1 = ex2(__uint_as_float((uint32_t)(e >> 32)));
+                            sum[i & 1] = add_f32x2(sum[i & 1], f32x2(p0, p1));
                             pk[i] = pack_bf16x2(p0, p1);
                         }
-                        tmem_st32(s_col + 32 * h, pk);
+                        tmem_st16(s_col + 16 * h, pk);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    sum[0] = add_f32x2(sum[0], sum[1]);
+                    l += __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 }
                 tc_fence_before();
@@ -462,7 +493,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             }
             if (it.kv0 == 0 && row0 + r == 0)
                 reinterpret_cast<ItemMeta*>(p.scratch + kScratchHead)[(size_t)it.index * c.n_kv + it.g] = {
-                    it.b, it.tile, me, it.whole() ? me : it.last_worker()};
+                    it.b, it.tile, me, it.whole() ? me : it.last_worker(pieces[PAIR ? 0 : w])};
             tc_fence_before();  // the output is read, before the next item's values overwrite it
         }
     }

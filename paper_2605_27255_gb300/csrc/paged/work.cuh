@@ -177,39 +177,30 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
 // the worker that holds unit u
 __device__ __forceinline__ int worker_of(long long u, long long total, int S) { return (int)(((u + 1) * S - 1) / total); }
 
-// One worker's items in turn.  Every thread of a role keeps its own.
+// One worker's items in turn.  Every thread of a role keeps its own; what is only
+// asked of an item that starts here stays in the piece (shared memory).
 struct ItemWalk {
-    const PagedArgs* c;
-    ItemShape s;
-    int S, me;
     int b, tile, g, index, left;
-    long long at, total;
     // the present item
     int n, len, q0;      // new tokens and entries of the sequence, row of its first new token
     int t0, nt;          // first unit, units of the item
     int kv0, kv1;        // this worker's units of it
-    __device__ __forceinline__ void start(const PagedArgs& cc, const ItemShape& ss, const Piece& p, int me_) {
-        c = &cc;
-        s = ss;
-        S = p.workers;
-        me = me_;
+    __device__ __forceinline__ void start(const PagedArgs& c, const ItemShape& s, const Piece& p) {
         b = p.b;
         tile = p.tile;
         g = p.g;
         index = p.index;
         left = p.units;
-        at = p.at;
-        total = p.total;
         kv0 = p.kv;
-        if (left > 0) load();
+        if (left > 0) load(c, s);
     }
-    __device__ __forceinline__ void load() {
-        n = seq_new(*c, b);
-        len = seq_len(*c, b);
-        q0 = q_row(*c, b);
-        shape();
+    __device__ __forceinline__ void load(const PagedArgs& c, const ItemShape& s) {
+        n = seq_new(c, b);
+        len = seq_len(c, b);
+        q0 = q_row(c, b);
+        shape(s);
     }
-    __device__ __forceinline__ void shape() {
+    __device__ __forceinline__ void shape(const ItemShape& s) {
         const RowTile r = row_tile(s, n, len, tile);
         t0 = r.t0;
         nt = r.nt;
@@ -217,29 +208,30 @@ struct ItemWalk {
     }
     __device__ __forceinline__ bool more() const { return left > 0; }
     __device__ __forceinline__ bool whole() const { return kv0 == 0 && kv1 == nt; }
-    __device__ __forceinline__ int tokens() const { return min(s.TP, n - tile * s.TP); }
-    __device__ __forceinline__ void next() {
+    __device__ __forceinline__ int tokens(const ItemShape& s) const { return min(s.TP, n - tile * s.TP); }
+    __device__ __forceinline__ void next(const PagedArgs& c, const ItemShape& s) {
         left -= kv1 - kv0;
-        at += kv1 - kv0;
         kv0 = 0;
         if (left <= 0) return;
-        if (++g < c->n_kv) {
+        if (++g < c.n_kv) {
             kv1 = min(nt, left);
             return;
         }
         g = 0;
         ++index;
         if (++tile * s.TP < n) {
-            shape();
+            shape(s);
             return;
         }
         tile = 0;
         do ++b;
-        while (b + 1 < c->batch && seq_new(*c, b) == 0);
-        load();
+        while (b + 1 < c.batch && seq_new(c, b) == 0);
+        load(c, s);
     }
-    // the last worker that holds a unit of this item (asked by the one with its first unit)
-    __device__ __forceinline__ int last_worker() const { return worker_of(at - kv0 + nt - 1, total, S); }
+    // the last worker that holds a unit of this item, asked by the one with its first unit
+    __device__ __forceinline__ int last_worker(const Piece& p) const {
+        return worker_of(p.at + (p.units - left) + nt - 1, p.total, p.workers);
+    }
 };
 
 // Joins the parts of the shared items.  grid (items, row groups of 4): one warp per row.
