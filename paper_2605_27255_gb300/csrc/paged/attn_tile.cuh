@@ -19,13 +19,17 @@
 // A CTA runs two such pipelines side by side, so that the MMAs of one run under
 // the softmax of the other:
 //   PAIR    the two halves of a 256-row tile: both read each K and V tile
-//           (one copy, two uses).  Chunks of many rows.
+//           (one copy, two uses).  Chunks of many rows.  The pipelines take turns
+//           at the tensor cores, the values of one unit and the scores of the next
+//           at a time: left alone they fall into step, both in the softmax and
+//           then both at the MMAs (530 us for the 2048-token chunk).
 //   single  two workers with items of their own (work.cuh), 128 rows each, and a
 //           ring of copies each.  Few rows per sequence, listed pages.
 //
 // Roles (384 threads): warps 0 and 2 copy K and V tiles (TMA boxes of one page x
-// 64 dims, 128-byte swizzle) and warps 1 and 3 issue the MMAs (PAIR: warps 0
-// and 1 alone), warps 4-7 and 8-11 are the two softmax warpgroups, which also
+// 64 dims, 128-byte swizzle; PAIR: warp 0 alone), warps 1 and 3 issue the MMAs of
+// the two pipelines (a warp for each: a warp that waits for one would hold up the
+// other), warps 4-7 and 8-11 are the two softmax warpgroups, which also
 // load the queries and write the outputs.  Cache slots past a sequence's end may hold
 // anything: their scores are masked, and the MMA warp clears their values in
 // shared memory (0 times NaN would be NaN).
@@ -56,6 +60,12 @@ __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 // pairs of fp32 values, the first one in the low word
@@ -109,7 +119,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
     extern __shared__ __align__(1024) unsigned char at_smem_raw[];
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t full[NR][ST], empty[NR][ST];
-    __shared__ __align__(8) uint64_t q_full[2], s_full[2], p_full[2], o_full[2], drained[2];
+    __shared__ __align__(8) uint64_t q_full[2], s_full[2], p_full[2], o_full[2], turn[2], drained[2];
     __shared__ Piece pieces[NR];
     __shared__ int give_up;
 
@@ -126,13 +136,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         for (int r = 0; r < NR; ++r)
             for (int i = 0; i < ST; ++i) {
                 mbar_init(&full[r][i], 1);
-                mbar_init(&empty[r][i], 1);
+                mbar_init(&empty[r][i], PAIR ? 2 : 1);  // the pipelines that read a stage
             }
         for (int w = 0; w < 2; ++w) {
             mbar_init(q_full + w, 4);  // softmax warps
             mbar_init(s_full + w, 1);
             mbar_init(p_full + w, 4);
             mbar_init(o_full + w, 1);
+            mbar_init(turn + w, 1);
             mbar_init(drained + w, 1);
         }
         give_up = 0;
@@ -159,13 +170,13 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtRegsIo));
-        const int ring = warp >> 1;  // PAIR: warps 2 and 3 have nothing to do
-        if (!(PAIR && ring == 1)) {
+        const int chain = warp >> 1, ring = PAIR ? 0 : chain;  // PAIR: one ring for both pipelines, filled by warp 0
+        if (warp != 2 || !PAIR) {
             ItemWalk it;
-            it.start(c, shape, pieces[PAIR ? 0 : ring]);
-            uint64_t* fu = full[PAIR ? 0 : ring];
-            uint64_t* em = empty[PAIR ? 0 : ring];
-            unsigned char* rs = ring_s + (size_t)(PAIR ? 0 : ring) * ST * kTile;
+            it.start(c, shape, pieces[ring]);
+            uint64_t* fu = full[ring];
+            uint64_t* em = empty[ring];
+            unsigned char* rs = ring_s + (size_t)ring * ST * kTile;
             if ((warp & 1) == 0) {
                 // ---- copies: K then V of every unit
                 int k = 0;  // copies issued
@@ -214,48 +225,51 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 // ---- MMAs.  TMEM: scores / weights of pipeline w at w * 128, its output at 256 + w * 128
                 constexpr uint32_t id_s = umma_idesc_bf16(128, kTileEnt);
                 constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
-                int k = 0;                 // ring position
-                int qn0 = 0, qn1 = 0;      // items begun
-                int pn0 = 0, pn1 = 0;      // units of weights
+                int k = 0;        // ring position
+                int items = 0;    // items begun
+                int units = 0;    // units of weights
+                int turns = 0;    // units of both pipelines
                 bool ok = true;
                 // descriptors count in 16 bytes: a step along a tile is an addition
-                const uint64_t dq = umma_desc_sw128(smem_u32(q_s)), dk = umma_desc_sw128(smem_u32(rs)),
+                const uint64_t dq = umma_desc_sw128(smem_u32(q_s) + chain * kTile), dk = umma_desc_sw128(smem_u32(rs)),
                                dv = umma_desc_mn128(smem_u32(rs));
-                auto scores = [&](int w, int st) {
+                const uint32_t s_at = tmem + (uint32_t)(chain * 128), o_at = s_at + 256u;
+                auto scores = [&](int st) {
                     if (lane == 0) {
-                        uint32_t qb = (uint32_t)dq + (uint32_t)(w * (kTile >> 4)), kb = (uint32_t)dk + (uint32_t)(st * (kTile >> 4));
-                        const uint32_t d = tmem + (uint32_t)(w * 128);
+                        uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)(st * (kTile >> 4));
                         asm volatile("" : "+r"(qb), "+r"(kb));  // eight sums now, not sixteen kept over the loop
 #pragma unroll
                         for (int i = 0; i < DH / 16; ++i) {
                             const uint32_t o = ((i >> 2) * kAtHalf + (i & 3) * 32) >> 4;
-                            umma_bf16(d, u32x2(qb + o, (uint32_t)(dq >> 32)), u32x2(kb + o, (uint32_t)(dk >> 32)), id_s,
+                            umma_bf16(s_at, u32x2(qb + o, (uint32_t)(dq >> 32)), u32x2(kb + o, (uint32_t)(dk >> 32)), id_s,
                                       i > 0 ? 1u : 0u);
                         }
-                        umma_commit(s_full + w);
+                        umma_commit(s_full + chain);
+                        umma_commit(em + st);
                     }
                     __syncwarp();
                 };
-                auto values = [&](int w, int st, bool first) {
+                auto values = [&](int st, bool first) {
                     if (lane == 0) {
-                        uint32_t vb = (uint32_t)dv + (uint32_t)(st * (kTile >> 4)), a = tmem + (uint32_t)(w * 128);
-                        asm volatile("" : "+r"(vb), "+r"(a));
-                        const uint32_t d = a + 256u;
+                        uint32_t vb = (uint32_t)dv + (uint32_t)(st * (kTile >> 4));
+                        asm volatile("" : "+r"(vb));
 #pragma unroll
                         for (int i = 0; i < kTileEnt / 16; ++i)
-                            umma_bf16_ta(d, a + i * 8, u32x2(vb + i * (2048 >> 4), (uint32_t)(dv >> 32)), id_o,
+                            umma_bf16_ta(o_at, s_at + i * 8, u32x2(vb + i * (2048 >> 4), (uint32_t)(dv >> 32)), id_o,
                                          i > 0 || !first ? 1u : 0u);
-                        umma_commit(o_full + w);
+                        umma_commit(o_full + chain);
+                        umma_commit(em + st);
                     }
                     __syncwarp();
                 };
-                auto free_stage = [&](int st) {
-                    if (lane == 0) umma_commit(em + st);
-                };
-                const int w0 = PAIR ? 0 : ring;
                 for (; it.more() && ok; it.next(c, shape)) {
-                    const int rows = it.tokens(shape) * c.G;
-                    const bool two = PAIR && rows > 128;
+                    if (PAIR && chain * 128 >= it.tokens(shape) * c.G) {  // no rows here: hand the stages on
+                        for (int i = 2 * (it.kv1 - it.kv0); i > 0 && ok; --i, ++k) {
+                            ok = wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k);
+                            if (ok && lane == 0) mbar_arrive(em + k % ST);
+                        }
+                        continue;
+                    }
                     // entries whose values may be anything: those past the sequence's (or the list's) end
                     int end = it.len;
                     if (shape.n_top > 0) {
@@ -264,23 +278,21 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         const int32_t* list = p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top;
                         end = kept == 0 ? 0 : (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage + 1 : kPage);
                     }
-                    ok = wait(q_full + w0, (uint32_t)(qn0 & 1), 53, qn0) &&
-                         (!two || wait(q_full + 1, (uint32_t)(qn1 & 1), 53, qn1)) &&
+                    ok = wait(q_full + chain, (uint32_t)(items & 1), 53, items) &&
                          wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k);
                     if (!ok) break;
-                    ++qn0;
-                    if (two) ++qn1;
+                    ++items;
                     tc_fence_after();
-                    scores(w0, k % ST);
-                    if (two) scores(1, k % ST);
-                    free_stage(k % ST);
+                    scores(k % ST);
                     ++k;
+                    const bool two = PAIR && it.tokens(shape) * c.G > 128;
                     for (int u = it.kv0; u < it.kv1; ++u) {
                         const int vst = k % ST;
                         ok = wait(fu + vst, (uint32_t)((k / ST) & 1), 54, k);
                         if (!ok) break;
+                        ++k;
                         const int tail = end - (it.t0 + u) * kTileEnt;
-                        if (tail < kTileEnt) {  // (the generic stores are ordered before the MMAs that read them)
+                        if (tail < kTileEnt) {  // (PAIR: both pipelines clear the same rows before their own MMAs)
                             const int r0 = max(0, tail);
                             for (int i = lane; i < (kTileEnt - r0) * (DH / 8); i += 32) {
                                 const int r = r0 + i / (DH / 8), ch = i % (DH / 8);
@@ -290,45 +302,30 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             fence_proxy_async();
                             __syncwarp();
                         }
-                        const bool last = u + 1 == it.kv1;
-                        const int kst = (k + 1) % ST;
-                        ok = wait(p_full + w0, (uint32_t)(pn0 & 1), 55, pn0);
+                        const bool more = u + 1 < it.kv1;
+                        ok = (!more || wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k)) &&
+                             wait(p_full + chain, (uint32_t)(units & 1), 55, units) &&
+                             (!two || (chain == 0 && turns == 0) || wait(turn + chain, (uint32_t)((turns - 1 + chain) & 1), 60, turns));
                         if (!ok) break;
                         tc_fence_after();
-                        values(w0, vst, u == it.kv0);
-                        if (!last) {
-                            ok = wait(fu + kst, (uint32_t)(((k + 1) / ST) & 1), 54, k + 1) &&
-                                 wait(o_full + w0, (uint32_t)(pn0 & 1), 56, pn0);
+                        values(vst, u == it.kv0);
+                        if (more) {  // the next scores, once the weights they overwrite are read
+                            ok = wait(o_full + chain, (uint32_t)(units & 1), 56, units);
                             if (!ok) break;
-                            scores(w0, kst);
-                        }
-                        ++pn0;
-                        if (two) {
-                            ok = wait(p_full + 1, (uint32_t)(pn1 & 1), 55, pn1);
-                            if (!ok) break;
-                            tc_fence_after();
-                            values(1, vst, u == it.kv0);
-                            free_stage(vst);
-                            if (!last) {
-                                ok = wait(o_full + 1, (uint32_t)(pn1 & 1), 56, pn1);
-                                if (!ok) break;
-                                scores(1, kst);
-                            }
-                            ++pn1;
-                        } else {
-                            free_stage(vst);
-                        }
-                        if (!last) {
-                            free_stage(kst);
+                            scores(k % ST);
                             ++k;
                         }
-                        ++k;
+                        if (two) {
+                            if (lane == 0) mbar_arrive(turn + (chain ^ 1));
+                            ++turns;
+                        }
+                        ++units;
                     }
                 }
                 // commits arrive in order: after one more, none is in flight at the CTA's end
                 if (lane == 0) {
-                    umma_commit(drained + ring);
-                    mbar_wait(drained + ring, 0, 57);
+                    umma_commit(drained + chain);
+                    mbar_wait(drained + chain, 0, 57);
                 }
             }
         }
@@ -393,11 +390,11 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     }
                     float mt[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mt[i] = __uint_as_float(s[i][0]);
+                    for (int i = 0; i < 4; ++i) mt[i] = fmaxf(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]));
 #pragma unroll
-                    for (int j = 1; j < 32; ++j)
+                    for (int j = 2; j < 32; j += 2)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mt[i] = fmaxf(mt[i], __uint_as_float(s[i][j]));
+                        for (int i = 0; i < 4; ++i) mt[i] = max3(mt[i], __uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1]));
                     const float top = fmaxf(fmaxf(mt[0], mt[1]), fmaxf(mt[2], mt[3])) * c2;
                     // the reference moves when the maximum has passed it by the slack (or it is the first one)
                     const bool move = top > m_ref + kAtSlack;
