@@ -2,9 +2,9 @@
 // (tcgen05, sm_103a).
 //
 // out = softmax(scale Q K^T) V for row tiles of 128 rows (tokens times the query
-// heads of one kv head), the rows of the MMAs, over 128 cache entries at a time:
+// heads of one kv head), the rows of the MMAs, over 64 cache entries at a time:
 //   S = Q K^T   fp32 in TMEM, Q and K from shared memory (K-major);
-//   softmax     one thread per row: it reads the row's 128 scores, keeps the
+//   softmax     one thread per row: it reads the row's 64 scores, keeps the
 //               running maximum and sum in fp32, and writes exp2 of the scores back over
 //               them as bf16 (the A operand of the next MMAs, from TMEM).  bf16
 //               weights carry 2^-9 of a weight, about the output's own
@@ -16,23 +16,27 @@
 //               neither O nor the sum is touched; when it moves the row's
 //               thread rescales its row of O in TMEM.
 //
-// A CTA runs two such pipelines side by side, so that the MMAs of one run under
-// the softmax of the other:
+// The scores of 64 entries (a page) have a buffer each, two per pipeline, so that
+// the softmax of one page runs under the MMAs of the next: with one buffer of 128
+// entries every unit waits for its own chain of scores, softmax and values (429 us for a
+// 2048-token chunk over 16 K entries).  The price is that an MMA of 64 columns is bound by
+// shared memory (A and B rows: 48 cycles against 32).
+//
+// A CTA runs two such pipelines side by side:
 //   PAIR    the two halves of a 256-row tile: both read each K and V tile
-//           (one copy, two uses).  Chunks of many rows.  The pipelines take turns
-//           at the tensor cores, the values of one unit and the scores of the next
-//           at a time: left alone they fall into step, both in the softmax and
-//           then both at the MMAs (530 us for the 2048-token chunk).
+//           (one copy, two uses).  Chunks of many rows.
 //   single  two workers with items of their own (work.cuh), 128 rows each, and a
 //           ring of copies each.  Few rows per sequence, listed pages.
 //
-// Roles (384 threads): warps 0 and 2 copy K and V tiles (TMA boxes of one page x
-// 64 dims, 128-byte swizzle; PAIR: warp 0 alone), warps 1 and 3 issue the MMAs of
-// the two pipelines (a warp for each: a warp that waits for one would hold up the
-// other), warps 4-7 and 8-11 are the two softmax warpgroups, which also
-// load the queries and write the outputs.  Cache slots past a sequence's end may hold
-// anything: their scores are masked, and the MMA warp clears their values in
-// shared memory (0 times NaN would be NaN).
+// Roles (512 threads): warps 0 and 2 copy K and V tiles (TMA boxes of one page x
+// 64 dims, 128-byte swizzle; PAIR: warp 0 alone), warps 1 and 3 issue the score
+// MMAs of the two pipelines, warps 13 and 15 their value MMAs, and warps 4-7 and 8-11 are
+// the two softmax warpgroups, which also load the queries and write the
+// outputs.  Scores and values have issuing warps of their own because a warp's next
+// wait is held until its MMAs have left the queue (about 250 cycles each: 440 us
+// for the 2048-token chunk with one warp for both).  Cache slots past a
+// sequence's end may hold anything: their scores are masked, and the value warp
+// clears their values in shared memory (0 times NaN would be NaN).
 //
 // Every wait is bounded; when one gives up the error word is set, every role
 // stops, and the copies and commits in flight are waited for before the CTA ends.
@@ -43,15 +47,18 @@
 
 namespace pipo {
 
-constexpr int kAtThreads = 384;
-constexpr int kAtRegsIo = 56, kAtRegsSoft = 224;
-static_assert(kAtRegsIo + 2 * kAtRegsSoft <= 3 * 168, "register shares must fit the launch's registers");
+constexpr int kAtThreads = 512;
+constexpr int kAtRegsIo = 56, kAtRegsSoft = 200;
+static_assert(2 * kAtRegsIo + 2 * kAtRegsSoft <= 4 * 128, "register shares must fit the launch's registers");
 constexpr int kAtHalf = 128 * 128;  // 64 dims of a tile: 128 rows of 128 bytes
 constexpr float kAtSlack = 8.f;     // exponents above the reference before it moves
 
 __host__ __device__ constexpr int at_tile_bytes(int dh) { return dh / 64 * kAtHalf; }
-// stages of one ring
-__host__ __device__ constexpr int at_stages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 2 : 4); }
+// Stages of one ring: an even number, so that a stage holds K tiles only or V tiles
+// only.  Every warp that waits for a stage then waits for each of its fills in turn; with an odd number
+// the score warps would pass over every second one, and a parity does not tell
+// a fill from the one two before it.
+__host__ __device__ constexpr int at_stages(int dh, bool pair) { return pair ? (dh == 128 ? 4 : 8) : (dh == 128 ? 2 : 4); }
 __host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
     return 1024 + (size_t)at_tile_bytes(dh) * (2 + at_stages(dh, pair) * (pair ? 1 : 2));
 }
@@ -62,10 +69,28 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// one thread of the converged warp, always the same one (the compiler knows that it is alone, which a
+// test of the lane does not tell it: 75 cycles less for every eight MMAs)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+    return e != 0;
+}
+
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+
+__device__ __forceinline__ float max32(const uint32_t (&s)[32]) {
+    float a = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])), b = fmaxf(__uint_as_float(s[2]), __uint_as_float(s[3]));
+#pragma unroll
+    for (int j = 4; j < 32; j += 4) {
+        a = max3(a, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+        b = max3(b, __uint_as_float(s[j + 2]), __uint_as_float(s[j + 3]));
+    }
+    return fmaxf(a, b);
 }
 
 // pairs of fp32 values, the first one in the low word
@@ -80,15 +105,6 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     uint64_t d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
-}
-
-// 16 consecutive 32-bit columns of this thread's TMEM lane
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
 }
 
 // 32 consecutive fp32 columns of this thread's TMEM lane, without the wait
@@ -115,11 +131,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                                                   const __grid_constant__ CUtensorMap tmK,
                                                                   const __grid_constant__ CUtensorMap tmV) {
     constexpr int kTile = at_tile_bytes(DH), ST = at_stages(DH, PAIR), NR = PAIR ? 1 : 2;  // NR: rings
+    static_assert(ST % 2 == 0, "a stage is for K or for V");
     constexpr int kPageHalf = kPage * 128;  // 64 dims of a page
     extern __shared__ __align__(1024) unsigned char at_smem_raw[];
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t full[NR][ST], empty[NR][ST];
-    __shared__ __align__(8) uint64_t q_full[2], s_full[2], p_full[2], o_full[2], turn[2], drained[2];
+    __shared__ __align__(8) uint64_t q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained[4];
     __shared__ Piece pieces[NR];
     __shared__ int give_up;
 
@@ -140,11 +157,13 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             }
         for (int w = 0; w < 2; ++w) {
             mbar_init(q_full + w, 4);  // softmax warps
-            mbar_init(s_full + w, 1);
-            mbar_init(p_full + w, 4);
-            mbar_init(o_full + w, 1);
-            mbar_init(turn + w, 1);
-            mbar_init(drained + w, 1);
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(&s_full[w][i], 1);
+                mbar_init(&p_full[w][i], 4);
+                mbar_init(&o_full[w][i], 1);  // by the page's buffer too: with one barrier a late waiter could miss a phase
+            }
+            mbar_init(drained + 2 * w, 1);
+            mbar_init(drained + 2 * w + 1, 1);
         }
         give_up = 0;
         mbar_init_fence();
@@ -168,10 +187,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         return got;
     };
 
-    if (warp < 4) {
+    if (warp < 4 || warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtRegsIo));
-        const int chain = warp >> 1, ring = PAIR ? 0 : chain;  // PAIR: one ring for both pipelines, filled by warp 0
-        if (warp != 2 || !PAIR) {
+        const int chain = (warp >> 1) & 1, ring = PAIR ? 0 : chain;  // PAIR: one ring for both pipelines, filled by warp 0
+        if ((warp & 1) ? true : warp < 4 && !(PAIR && warp == 2)) {
             ItemWalk it;
             it.start(c, shape, pieces[ring]);
             uint64_t* fu = full[ring];
@@ -184,7 +203,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 for (; it.more() && ok; it.next(c, shape)) {
                     const int32_t* list =
                         shape.n_top > 0 ? p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top : nullptr;
-                    const int seen = (it.len + kPage - 1) / kPage;  // pages with entries
+                    const int seen = 2 * it.t0 + it.np;  // end of the pages to be read
                     int held = -32, mine = -1;                      // lane l holds page held + l
                     for (int u = it.kv0; u < it.kv1 && ok; ++u) {
                         const int pg = (it.t0 + u) * 2;  // index in the cache or the list
@@ -195,7 +214,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                 const int q = i < shape.n_top ? list[i] : -1;
                                 mine = q >= 0 ? page_block(c, it.b, q) : -1;
                             } else {
-                                mine = i < seen ? page_block(c, it.b, i) : -1;
+                                mine = i < seen && i * kPage < it.len ? page_block(c, it.b, i) : -1;
                             }
                         }
                         int blk[2];
@@ -222,110 +241,102 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 // no copy into this CTA's shared memory is in flight at its end
                 if (lane == 0) ring_drain<ST>(k, [&](int st, uint32_t ph, int i) { mbar_wait(fu + st, ph, 52, (unsigned)i); });
             } else {
-                // ---- MMAs.  TMEM: scores / weights of pipeline w at w * 128, its output at 256 + w * 128
-                constexpr uint32_t id_s = umma_idesc_bf16(128, kTileEnt);
-                constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
-                int k = 0;        // ring position
+                // ---- MMAs.  TMEM: scores / weights of pipeline w at w * 128 (two buffers of 64 columns),
+                // its output at 256 + w * 128
+                const bool values = warp >= 12;  // this warp's half of them
+                int k = 0;        // ring position of the unit's K tile
                 int items = 0;    // items begun
-                int units = 0;    // units of weights
-                int turns = 0;    // units of both pipelines
+                int pv = 0;       // pages done
                 bool ok = true;
-                // descriptors count in 16 bytes: a step along a tile is an addition
-                const uint64_t dq = umma_desc_sw128(smem_u32(q_s) + chain * kTile), dk = umma_desc_sw128(smem_u32(rs)),
-                               dv = umma_desc_mn128(smem_u32(rs));
                 const uint32_t s_at = tmem + (uint32_t)(chain * 128), o_at = s_at + 256u;
-                auto scores = [&](int st) {
-                    if (lane == 0) {
-                        uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)(st * (kTile >> 4));
-                        asm volatile("" : "+r"(qb), "+r"(kb));  // eight sums now, not sixteen kept over the loop
-#pragma unroll
-                        for (int i = 0; i < DH / 16; ++i) {
-                            const uint32_t o = ((i >> 2) * kAtHalf + (i & 3) * 32) >> 4;
-                            umma_bf16(s_at, u32x2(qb + o, (uint32_t)(dq >> 32)), u32x2(kb + o, (uint32_t)(dk >> 32)), id_s,
-                                      i > 0 ? 1u : 0u);
-                        }
-                        umma_commit(s_full + chain);
-                        umma_commit(em + st);
-                    }
-                    __syncwarp();
-                };
-                auto values = [&](int st, bool first) {
-                    if (lane == 0) {
-                        uint32_t vb = (uint32_t)dv + (uint32_t)(st * (kTile >> 4));
-                        asm volatile("" : "+r"(vb));
-#pragma unroll
-                        for (int i = 0; i < kTileEnt / 16; ++i)
-                            umma_bf16_ta(o_at, s_at + i * 8, u32x2(vb + i * (2048 >> 4), (uint32_t)(dv >> 32)), id_o,
-                                         i > 0 || !first ? 1u : 0u);
-                        umma_commit(o_full + chain);
-                        umma_commit(em + st);
-                    }
-                    __syncwarp();
-                };
-                for (; it.more() && ok; it.next(c, shape)) {
+                auto filled = [&](int i) { return wait(fu + i % ST, (uint32_t)((i / ST) & 1), 54, i); };
+                for (; it.more() && ok; it.next(c, shape), ++items) {
+                    const int np = it.pages(), nu = it.kv1 - it.kv0;
                     if (PAIR && chain * 128 >= it.tokens(shape) * c.G) {  // no rows here: hand the stages on
-                        for (int i = 2 * (it.kv1 - it.kv0); i > 0 && ok; --i, ++k) {
-                            ok = wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k);
-                            if (ok && lane == 0) mbar_arrive(em + k % ST);
+                        for (int i = values; i < 2 * nu && ok; i += 2) {
+                            ok = filled(k + i);
+                            if (ok && lane == 0) mbar_arrive(em + (k + i) % ST);
                         }
+                        k += 2 * nu;
+                        --items;
                         continue;
                     }
-                    // entries whose values may be anything: those past the sequence's (or the list's) end
-                    int end = it.len;
-                    if (shape.n_top > 0) {
-                        const int pos = it.len - it.n + it.tile;
-                        const int kept = pos < 0 ? 0 : min(shape.n_top, pos / kPage + 1);
-                        const int32_t* list = p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top;
-                        end = kept == 0 ? 0 : (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage + 1 : kPage);
-                    }
-                    ok = wait(q_full + chain, (uint32_t)(items & 1), 53, items) &&
-                         wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k);
-                    if (!ok) break;
-                    ++items;
-                    tc_fence_after();
-                    scores(k % ST);
-                    ++k;
-                    const bool two = PAIR && it.tokens(shape) * c.G > 128;
-                    for (int u = it.kv0; u < it.kv1; ++u) {
-                        const int vst = k % ST;
-                        ok = wait(fu + vst, (uint32_t)((k / ST) & 1), 54, k);
-                        if (!ok) break;
-                        ++k;
-                        const int tail = end - (it.t0 + u) * kTileEnt;
-                        if (tail < kTileEnt) {  // (PAIR: both pipelines clear the same rows before their own MMAs)
-                            const int r0 = max(0, tail);
-                            for (int i = lane; i < (kTileEnt - r0) * (DH / 8); i += 32) {
-                                const int r = r0 + i / (DH / 8), ch = i % (DH / 8);
-                                *reinterpret_cast<uint4*>(rs + (size_t)vst * kTile + (ch >> 3) * kAtHalf + r * 128 +
-                                                          (ch & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    if (!values) {
+                        constexpr uint32_t id_s = umma_idesc_bf16(128, kPage);
+                        // descriptors count in 16 bytes: a step along a tile is an addition
+                        const uint64_t dq = umma_desc_sw128(smem_u32(q_s) + chain * kTile), dk = umma_desc_sw128(smem_u32(rs));
+                        ok = wait(q_full + chain, (uint32_t)(items & 1), 53, items);
+                        for (int j = 0; j < np && ok; ++j, ++pv) {  // page j of the item: half j % 2 of its unit's K tile
+                            const int h = j & 1, st = (k + (j & ~1)) % ST, buf = pv & 1;
+                            // the weights of the page before last lie in the buffer until their values are done
+                            ok = (h == 1 || filled(k + j)) &&
+                                 (j < 2 || wait(&o_full[chain][buf], (uint32_t)(((pv - 2) >> 1) & 1), 56, pv));
+                            if (!ok) break;
+                            tc_fence_after();
+                            if (elect_one()) {
+                                uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)((st * kTile + h * kPageHalf) >> 4);
+                                asm volatile("" : "+r"(qb), "+r"(kb));  // eight sums now, not sixteen kept over the loop
+#pragma unroll
+                                for (int i = 0; i < DH / 16; ++i) {
+                                    const uint32_t o = ((i >> 2) * kAtHalf + (i & 3) * 32) >> 4;
+                                    umma_bf16(s_at + buf * 64, u32x2(qb + o, (uint32_t)(dq >> 32)),
+                                              u32x2(kb + o, (uint32_t)(dk >> 32)), id_s, i > 0 ? 1u : 0u);
+                                }
+                                umma_commit(&s_full[chain][buf]);
+                                if (h == 1 || j + 1 == np) umma_commit(em + st);
                             }
-                            fence_proxy_async();
                             __syncwarp();
                         }
-                        const bool more = u + 1 < it.kv1;
-                        ok = (!more || wait(fu + k % ST, (uint32_t)((k / ST) & 1), 54, k)) &&
-                             wait(p_full + chain, (uint32_t)(units & 1), 55, units) &&
-                             (!two || (chain == 0 && turns == 0) || wait(turn + chain, (uint32_t)((turns - 1 + chain) & 1), 60, turns));
-                        if (!ok) break;
-                        tc_fence_after();
-                        values(vst, u == it.kv0);
-                        if (more) {  // the next scores, once the weights they overwrite are read
-                            ok = wait(o_full + chain, (uint32_t)(units & 1), 56, units);
+                    } else {
+                        constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
+                        const uint64_t dv = umma_desc_mn128(smem_u32(rs));
+                        // entries whose values may be anything: those past the sequence's (or the list's) end
+                        int end = it.len;
+                        if (shape.n_top > 0) {
+                            const int pos = it.len - it.n + it.tile;
+                            const int kept = pos < 0 ? 0 : min(shape.n_top, pos / kPage + 1);
+                            const int32_t* list = p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top;
+                            end = kept == 0 ? 0 : (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage + 1 : kPage);
+                        }
+                        for (int j = 0; j < np; ++j, ++pv) {
+                            const int h = j & 1, st = (k + (j & ~1) + 1) % ST, buf = pv & 1;
+                            if (h == 0) {
+                                ok = filled(k + j + 1);
+                                if (!ok) break;
+                                const int tail = end - (it.t0 + it.kv0 + j / 2) * kTileEnt;
+                                if (tail < kTileEnt) {  // (PAIR: both pipelines clear the same rows before their own MMAs)
+                                    const int r0 = max(0, tail);
+                                    for (int i = lane; i < (kTileEnt - r0) * (DH / 8); i += 32) {
+                                        const int r = r0 + i / (DH / 8), ch = i % (DH / 8);
+                                        *reinterpret_cast<uint4*>(rs + (size_t)st * kTile + (ch >> 3) * kAtHalf + r * 128 +
+                                                                  (ch & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                                    }
+                                    fence_proxy_async();
+                                    __syncwarp();
+                                }
+                            }
+                            ok = wait(&p_full[chain][buf], (uint32_t)((pv >> 1) & 1), 55, pv);
                             if (!ok) break;
-                            scores(k % ST);
-                            ++k;
+                            tc_fence_after();
+                            if (elect_one()) {
+                                uint32_t vb = (uint32_t)dv + (uint32_t)((st * kTile + h * kPageHalf) >> 4);
+                                asm volatile("" : "+r"(vb));
+#pragma unroll
+                                for (int i = 0; i < kPage / 16; ++i)
+                                    umma_bf16_ta(o_at, s_at + buf * 64 + i * 8, u32x2(vb + i * (2048 >> 4), (uint32_t)(dv >> 32)),
+                                                 id_o, i > 0 || j > 0 ? 1u : 0u);
+                                umma_commit(&o_full[chain][buf]);
+                                if (h == 1 || j + 1 == np) umma_commit(em + st);
+                            }
+                            __syncwarp();
                         }
-                        if (two) {
-                            if (lane == 0) mbar_arrive(turn + (chain ^ 1));
-                            ++turns;
-                        }
-                        ++units;
                     }
+                    k += 2 * nu;
                 }
                 // commits arrive in order: after one more, none is in flight at the CTA's end
-                if (lane == 0) {
-                    umma_commit(drained + chain);
-                    mbar_wait(drained + chain, 0, 57);
+                if (elect_one()) {
+                    umma_commit(drained + 2 * chain + values);
+                    mbar_wait(drained + 2 * chain + values, 0, 57);
                 }
             }
         }
@@ -340,7 +351,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         const float c2 = p.scale * 1.4426950408889634f;  // exponents of two
         ItemWalk it;
         it.start(c, shape, pieces[PAIR ? 0 : w]);
-        int sn = 0;  // units seen
+        int sn = 0;  // pages seen
         bool ok = true;
         for (; it.more() && ok; it.next(c, shape)) {
             const int rows = min(128, it.tokens(shape) * c.G - (PAIR ? w * 128 : 0));
@@ -371,39 +382,34 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 if (kept > 0) pos = (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage : kPage - 1);
             }
             float m_ref = -INFINITY, l = 0.f;
-            for (int u = it.kv0; u < it.kv1; ++u, ++sn) {
-                ok = wait(s_full + w, (uint32_t)(sn & 1), 58, sn);
+            const int np = it.pages();
+            for (int j = 0; j < np; ++j, ++sn) {
+                const uint32_t s_buf = s_col + (uint32_t)((sn & 1) * 64);
+                ok = wait(&s_full[w][sn & 1], (uint32_t)((sn >> 1) & 1), 58, sn);
                 if (!ok) break;
                 tc_fence_after();
                 if (live) {
-                    uint32_t s[4][32];
+                    uint32_t s[2][32];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld32_issue(s_col + 32 * i, s[i]);
+                    for (int i = 0; i < 2; ++i) tmem_ld32_issue(s_buf + 32 * i, s[i]);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) pin32(s[i]);
-                    const int e0 = (it.t0 + u) * kTileEnt;
-                    if (e0 + kTileEnt - 1 > pos || e0 < lo) {
+                    for (int i = 0; i < 2; ++i) pin32(s[i]);
+                    const int e0 = (it.t0 + it.kv0) * kTileEnt + j * kPage;
+                    if (e0 + kPage - 1 > pos || e0 < lo) {
 #pragma unroll
-                        for (int i = 0; i < 128; ++i)
+                        for (int i = 0; i < kPage; ++i)
                             if (e0 + i > pos || e0 + i < lo) s[i >> 5][i & 31] = 0xff800000u;
                     }
-                    float mt[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mt[i] = fmaxf(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]));
-#pragma unroll
-                    for (int j = 2; j < 32; j += 2)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mt[i] = max3(mt[i], __uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1]));
-                    const float top = fmaxf(fmaxf(mt[0], mt[1]), fmaxf(mt[2], mt[3])) * c2;
+                    const float top = fmaxf(max32(s[0]), max32(s[1])) * c2;
                     // the reference moves when the maximum has passed it by the slack (or it is the first one)
                     const bool move = top > m_ref + kAtSlack;
                     if (__any_sync(0xffffffffu, move)) {
                         const float f = move ? (m_ref == -INFINITY ? 0.f : ex2(m_ref - top)) : 1.f;
                         if (move) m_ref = top;
                         l *= f;
-                        if (u > it.kv0) {  // the output so far, once the values of the unit before are in it
-                            ok = wait(o_full + w, (uint32_t)((sn - 1) & 1), 59, sn);
+                        if (j > 0) {  // the output so far, once the values of the page before are in it
+                            ok = wait(&o_full[w][(sn - 1) & 1], (uint32_t)(((sn - 1) >> 1) & 1), 59, sn);
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll
@@ -419,31 +425,28 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         }
                     }
                     const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
-                    // two columns at a time (paired fp32 instructions), 32 columns per store
+                    // two columns at a time (paired fp32 instructions)
                     const uint64_t c22 = f32x2(c2, c2), neg2 = f32x2(neg, neg);
                     uint64_t sum[2] = {0ull, 0ull};
+                    uint32_t pk[32];
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const uint64_t e = fma_f32x2(u32x2(s[h][2 * i], s[h][2 * i + 1]), c22, neg2);
-                            const float p0 = ex2(__uint_as_float((uint32_t)e)), p1 = ex2(__uint_as_float((uint32_t)(e >> 32)));
-                            sum[i & 1] = add_f32x2(sum[i & 1], f32x2(p0, p1));
-                            pk[i] = pack_bf16x2(p0, p1);
-                        }
-                        tmem_st16(s_col + 16 * h, pk);
+                    for (int i = 0; i < 32; ++i) {
+                        const uint64_t e = fma_f32x2(u32x2(s[i >> 4][2 * (i & 15)], s[i >> 4][2 * (i & 15) + 1]), c22, neg2);
+                        const float p0 = ex2(__uint_as_float((uint32_t)e)), p1 = ex2(__uint_as_float((uint32_t)(e >> 32)));
+                        sum[i & 1] = add_f32x2(sum[i & 1], f32x2(p0, p1));
+                        pk[i] = pack_bf16x2(p0, p1);
                     }
+                    tmem_st32(s_buf, pk);
                     sum[0] = add_f32x2(sum[0], sum[1]);
                     l += __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + w);
+                if (lane == 0) mbar_arrive(&p_full[w][sn & 1]);
             }
             if (!ok) break;
-            ok = wait(o_full + w, (uint32_t)((sn - 1) & 1), 59, sn);
+            ok = wait(&o_full[w][(sn - 1) & 1], (uint32_t)(((sn - 1) >> 1) & 1), 59, sn);
             if (!ok) break;
             tc_fence_after();
             if (!live) {

@@ -29,17 +29,18 @@ struct ItemShape {
 // Row tile j of a sequence with n new tokens and len entries
 struct RowTile {
     int t0, nt;     // first unit (in kTileEnt entries from the start of the cache or of the list), units
+    int np;         // pages of them: 2 nt, or one less
 };
 __device__ __forceinline__ RowTile row_tile(const ItemShape& s, int n, int len, int j) {
     const int i0 = j * s.TP, i1 = min(n, i0 + s.TP);
     const int first = len - n + i0, last = len - n + i1 - 1;
     if (s.n_top > 0) {
         const int kept = last < 0 ? 0 : min(s.n_top, last / kPage + 1);
-        return {0, max(1, (kept + 1) / 2)};
+        return {0, max(1, (kept + 1) / 2), max(1, kept)};
     }
     const int hi = max(0, last + 1), lo = s.window > 0 ? min(hi, max(0, first - s.window + 1)) : 0;
-    const int t0 = lo / kTileEnt;
-    return {t0, max(1, (hi + kTileEnt - 1) / kTileEnt - t0)};
+    const int t0 = lo / kTileEnt, np = max(1, (hi + kPage - 1) / kPage - 2 * t0);
+    return {t0, (np + 1) / 2, np};
 }
 
 __device__ __forceinline__ int seq_new(const PagedArgs& c, int b) { return max(0, q_row(c, b + 1) - q_row(c, b)); }
@@ -183,7 +184,7 @@ struct ItemWalk {
     int b, tile, g, index, left;
     // the present item
     int n, len, q0;      // new tokens and entries of the sequence, row of its first new token
-    int t0, nt;          // first unit, units of the item
+    int t0, nt, np;      // first unit, units and pages of the item
     int kv0, kv1;        // this worker's units of it
     __device__ __forceinline__ void start(const PagedArgs& c, const ItemShape& s, const Piece& p) {
         b = p.b;
@@ -204,8 +205,10 @@ struct ItemWalk {
         const RowTile r = row_tile(s, n, len, tile);
         t0 = r.t0;
         nt = r.nt;
+        np = r.np;
         kv1 = min(nt, kv0 + left);
     }
+    __device__ __forceinline__ int pages() const { return min(2 * kv1, np) - 2 * kv0; }  // this worker's
     __device__ __forceinline__ bool more() const { return left > 0; }
     __device__ __forceinline__ bool whole() const { return kv0 == 0 && kv1 == nt; }
     __device__ __forceinline__ int tokens(const ItemShape& s) const { return min(s.TP, n - tile * s.TP); }
@@ -238,16 +241,18 @@ struct ItemWalk {
 // out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the workers first .. last in
 // order; the first one's part is its second slot, the others' their first.
 template <int DH, typename T>
-__global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, ItemShape s, int part_rows, size_t part_off) {
+__global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, ItemShape s, int workers, int part_rows,
+                                                      size_t part_off) {
     constexpr int N = DH / 32;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const PagedArgs& c = a.c;
     const int item = blockIdx.x, lane = threadIdx.x & 31;
     if (item / c.n_kv >= *reinterpret_cast<const int*>(a.scratch)) return;
     const ItemMeta m = reinterpret_cast<const ItemMeta*>(a.scratch + kScratchHead)[item];
-    if (m.first == m.last) return;
+    // (after a wait that gave up, the scratch may lack items: nothing outside it is read)
+    if (m.first < 0 || m.first >= m.last || m.last >= workers || m.b < 0 || m.b >= c.batch || m.tile < 0) return;
     const int row = blockIdx.y * 4 + (threadIdx.x >> 5);
-    const int i = m.tile * s.TP + row / c.G;
+    const long long i = (long long)m.tile * s.TP + row / c.G;
     if (row >= s.TP * c.G || i >= seq_new(c, m.b)) return;
     const float* parts = reinterpret_cast<const float*>(a.scratch + part_off);
     auto part = [&](int w) { return parts + ((size_t)w * 2 + (w == m.first ? 1 : 0)) * part_floats(part_rows, DH); };
@@ -278,7 +283,7 @@ __global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, ItemShape
     const float inv = L > 0.f ? 1.0f / L : 0.f;
 #pragma unroll
     for (int e = 0; e < N; ++e) o[e] *= inv;
-    const int g = item % c.n_kv, t = q_row(c, m.b) + i;
+    const int g = item % c.n_kv, t = q_row(c, m.b) + (int)i;
     store_f<T, N>(static_cast<T*>(a.out) + (size_t)t * a.ld_out + (size_t)(g * c.G + row % c.G) * DH + lane * N, o);
 }
 
