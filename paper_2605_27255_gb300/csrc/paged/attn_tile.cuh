@@ -63,6 +63,9 @@ __host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
     return 1024 + (size_t)at_tile_bytes(dh) * (2 + at_stages(dh, pair) * (pair ? 1 : 2));
 }
 
+// x / G for x < 256 and G <= 16, magic = ceil(2^16 / G): off by less than 256 / 2^16 < 1 / G
+__device__ __forceinline__ int div_g(int x, uint32_t magic) { return (int)(((uint32_t)x * magic) >> 16); }
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -351,30 +354,37 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         const float c2 = p.scale * 1.4426950408889634f;  // exponents of two
         ItemWalk it;
         it.start(c, shape, pieces[PAIR ? 0 : w]);
+        const uint32_t g_magic = (65536u + (uint32_t)c.G - 1) / (uint32_t)c.G;
         int sn = 0;  // pages seen
         bool ok = true;
         for (; it.more() && ok; it.next(c, shape)) {
             const int rows = min(128, it.tokens(shape) * c.G - (PAIR ? w * 128 : 0));
             if (rows <= 0) continue;
             const int row0 = PAIR ? w * 128 : 0, i0 = it.tile * shape.TP;
-            // the queries of this tile; rows past the last one are zero
+            // the queries of this tile; rows past the last one are zero.  Every load is in flight before
+            // the first is stored (one after the other they took 19000 cycles)
             {
-                const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)it.g * c.G * DH;
-                for (int i = wt; i < 128 * (DH / 8); i += 128) {
-                    const int v = i / (DH / 8), ch = i % (DH / 8);
-                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                    if (v < rows) {
-                        const int row = row0 + v, tok = it.q0 + i0 + row / c.G;
-                        x = *reinterpret_cast<const uint4*>(q + (size_t)tok * p.ld_q + (size_t)(row % c.G) * DH + ch * 8);
-                    }
-                    *reinterpret_cast<uint4*>(q_s + w * kTile + (ch >> 3) * kAtHalf + v * 128 + (((ch & 7) ^ (v & 7)) << 4)) = x;
+                constexpr int C = DH / 8, RS = 128 / C, NI = 128 / RS;  // 16-byte chunks a row, rows per round, rounds
+                const int ch = wt % C, v0 = wt / C;
+                const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + i0) * p.ld_q + (size_t)it.g * c.G * DH + ch * 8;
+                uint4 x[NI];
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int v = v0 + i * RS, t = div_g(row0 + v, g_magic);
+                    x[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (v < rows) x[i] = *reinterpret_cast<const uint4*>(q + (size_t)t * p.ld_q + (row0 + v - t * c.G) * DH);
+                }
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int v = v0 + i * RS;
+                    *reinterpret_cast<uint4*>(q_s + w * kTile + (ch >> 3) * kAtHalf + v * 128 + (((ch & 7) ^ (v & 7)) << 4)) = x[i];
                 }
                 fence_proxy_async();  // the generic stores above, before the MMAs read them
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full + w);
             }
             const bool live = quad * 32 < rows;  // this warp has rows at all
-            const int tok = i0 + (row0 + min(r, rows - 1)) / c.G;
+            const int row = row0 + min(r, rows - 1), tr = div_g(row, g_magic), tok = i0 + tr;
             int pos = it.len - it.n + tok, lo = p.window > 0 ? pos - p.window + 1 : 0;
             if (shape.n_top > 0) {  // positions in the list's own order
                 const int kept = pos < 0 ? 0 : min(shape.n_top, pos / kPage + 1);
@@ -454,7 +464,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             } else if (it.whole()) {
                 const float inv = l > 0.f ? 1.0f / l : 0.f;
                 bf16_t* o = static_cast<bf16_t*>(p.out) + (size_t)(it.q0 + tok) * p.ld_out +
-                            (size_t)(it.g * c.G + (row0 + min(r, rows - 1)) % c.G) * DH;
+                            (size_t)(it.g * c.G + row - tr * c.G) * DH;
 #pragma unroll
                 for (int h = 0; h < DH / 32; ++h) {
                     uint32_t v[32];
@@ -483,8 +493,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     pin32(v);
                     if (r < rows) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<uint4*>(part + (size_t)(row0 + r) * DH + 32 * h + i) =
+                        for (int i = 0; i < 32; i += 4)  // (four dims of all rows lie side by side)
+                            *reinterpret_cast<uint4*>(part + ((size_t)(8 * h + i / 4) * part_rows + row0 + r) * 4) =
                                 make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                     }
                 }

@@ -20,7 +20,7 @@ cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMa
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 3) / 4));
+    lc.gridDim = dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 31) / 32));
     lc.blockDim = dim3(128);
     lc.stream = s;
     cudaLaunchAttribute at[1];

@@ -59,8 +59,9 @@ __host__ __device__ inline long long tiles_bound(int n_tokens, int batch, int TP
 __host__ __device__ inline size_t meta_bytes(long long items) {
     return (kScratchHead + (size_t)items * sizeof(ItemMeta) + 255) / 256 * 256;
 }
-// floats of one partial: rows of DH outputs, then (maximum, sum) of every row; an even
-// number of rows keeps every partial 16-byte aligned
+// floats of one partial: [DH / 4][rows][4] outputs (a warp whose lanes are rows writes and
+// reads them side by side), then (maximum, sum) of every row; an even number of rows keeps
+// every partial 16-byte aligned
 __host__ __device__ inline size_t part_floats(int rows, int dh) { return (size_t)rows * (dh + 2); }
 
 // A worker's piece: where it starts, and how many units it has.
@@ -72,40 +73,53 @@ struct Piece {
     int workers;         // that have units: S, or as many as there are units
 };
 
+// Ints of shared memory that find_pieces uses
+__host__ __device__ constexpr int find_ints(int batch) { return 3 * batch + 1; }
+
 // All threads of a block (NT of them): the piece of each of its NW workers
-// (w0 .. w0 + NW - 1 of S), written to `out` in shared memory.  seq_tiles:
-// batch + 1 ints of shared memory.  Block 0 also leaves the number of row tiles.
+// (w0 .. w0 + NW - 1 of S), written to `out` in shared memory.  tmp: find_ints(batch)
+// ints of shared memory.  Block 0 also leaves the number of row tiles.
 template <int NT, int NW>
-__device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape& s, int w0, int S, int* seq_tiles,
-                                            Piece* out, int* n_tiles_out) {
-    __shared__ long long warp_units[NT / 32 + 1];
+__device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape& s, int w0, int S, int* tmp, Piece* out,
+                                            int* n_tiles_out) {
+    __shared__ long long warp_units[NT / 32];
     __shared__ int warp_tiles[NT / 32];
-    __shared__ int tiles_before;
+    int* seq_tiles = tmp;            // [batch + 1] row tiles before every sequence
+    int* seq_n = tmp + c.batch + 1;  // [batch] new tokens, entries
+    int* seq_l = seq_n + c.batch;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    // row tiles before every sequence
-    if (tid == 0) tiles_before = 0;
-    __syncthreads();
+    int tiles = 0;
     for (int b0 = 0; b0 < c.batch; b0 += NT) {
         const int b = b0 + tid;
-        const int n = b < c.batch ? (seq_new(c, b) + s.TP - 1) / s.TP : 0;
+        int n = 0;
+        if (b < c.batch) {
+            const int nn = seq_new(c, b);
+            seq_n[b] = nn;
+            seq_l[b] = seq_len(c, b);
+            n = (nn + s.TP - 1) / s.TP;
+        }
         int incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += v;
         }
+        if (b0 > 0) __syncthreads();  // (the sums of the round before are read)
         if (lane == 31) warp_tiles[warp] = incl;
         __syncthreads();
-        int before = tiles_before;
-        for (int w = 0; w < warp; ++w) before += warp_tiles[w];
+        int before = tiles;
+#pragma unroll
+        for (int w = 0; w < NT / 32; ++w) {
+            const int v = warp_tiles[w];
+            if (w < warp) before += v;
+            tiles += v;
+        }
         if (b < c.batch) seq_tiles[b] = before + incl - n;
-        __syncthreads();
-        if (tid == NT - 1) tiles_before = before + incl;
-        __syncthreads();
     }
     // (offsets that decrease could count rows twice: never more tiles than the scratch has room for)
-    const int tiles = (int)min((long long)tiles_before, tiles_bound(c.n_tokens, c.batch, s.TP));
+    tiles = (int)min((long long)tiles, tiles_bound(c.n_tokens, c.batch, s.TP));
     if (tid == 0) seq_tiles[c.batch] = tiles;
+    if (tid < NW) out[tid].units = 0;
     __syncthreads();
     // this thread's run of row tiles and its units
     const int x0 = (int)((long long)tiles * tid / NT), x1 = (int)((long long)tiles * (tid + 1) / NT);
@@ -116,15 +130,10 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
     }
     const int bfirst = lo;
     auto walk = [&](auto&& fn) {  // fn(b, tile, x, shape) -> stop
-        int b = bfirst, n = 0, len = 0, loaded = -1;
+        int b = bfirst;
         for (int x = x0; x < x1; ++x) {
             while (x >= seq_tiles[b + 1]) ++b;
-            if (b != loaded) {
-                n = seq_new(c, b);
-                len = seq_len(c, b);
-                loaded = b;
-            }
-            if (fn(b, x - seq_tiles[b], x, row_tile(s, n, len, x - seq_tiles[b]))) return;
+            if (fn(b, x - seq_tiles[b], x, row_tile(s, seq_n[b], seq_l[b], x - seq_tiles[b]))) return;
         }
     };
     long long mine = 0;
@@ -140,22 +149,17 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
     }
     if (lane == 31) warp_units[warp] = incl;
     __syncthreads();
-    if (tid == 0) {
-        long long sum = 0;
-        for (int w = 0; w < NT / 32; ++w) {
-            const long long v = warp_units[w];
-            warp_units[w] = sum;
-            sum += v;
-        }
-        warp_units[NT / 32] = sum;
-        if (n_tiles_out && blockIdx.x == 0) *n_tiles_out = tiles;
+    long long total = 0, before = incl - mine;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+        const long long v = warp_units[w];
+        if (w < warp) before += v;
+        total += v;
     }
-    if (tid < NW) out[tid].units = 0;
-    __syncthreads();
-    const long long total = warp_units[NT / 32], before = warp_units[warp] + incl - mine;
+    if (tid == 0 && n_tiles_out && blockIdx.x == 0) *n_tiles_out = tiles;
+    const int Sw = (int)min((long long)S, total);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-        const int Sw = (int)min((long long)S, total);
         if (w0 + w >= Sw) break;
         const long long u0 = (long long)(w0 + w) * total / Sw, u1 = (long long)(w0 + w + 1) * total / Sw;
         if (u0 >= before && u0 < before + mine) {
@@ -237,54 +241,60 @@ struct ItemWalk {
     }
 };
 
-// Joins the parts of the shared items.  grid (items, row groups of 4): one warp per row.
+// Joins the parts of the shared items.  grid (items, row groups of 32), 128 threads.
 // out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the workers first .. last in
-// order; the first one's part is its second slot, the others' their first.
+// order; the first one's part is its second slot, the others' their first.  A thread takes one
+// row and every (128 / RP)-th group of four dims, RP rows side by side as they lie in the parts.
 template <int DH, typename T>
 __global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, ItemShape s, int workers, int part_rows,
                                                       size_t part_off) {
-    constexpr int N = DH / 32;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const PagedArgs& c = a.c;
-    const int item = blockIdx.x, lane = threadIdx.x & 31;
+    const int item = blockIdx.x;
     if (item / c.n_kv >= *reinterpret_cast<const int*>(a.scratch)) return;
     const ItemMeta m = reinterpret_cast<const ItemMeta*>(a.scratch + kScratchHead)[item];
     // (after a wait that gave up, the scratch may lack items: nothing outside it is read)
     if (m.first < 0 || m.first >= m.last || m.last >= workers || m.b < 0 || m.b >= c.batch || m.tile < 0) return;
-    const int row = blockIdx.y * 4 + (threadIdx.x >> 5);
-    const long long i = (long long)m.tile * s.TP + row / c.G;
-    if (row >= s.TP * c.G || i >= seq_new(c, m.b)) return;
+    const int rows = (int)min((long long)s.TP * c.G, ((long long)seq_new(c, m.b) - (long long)m.tile * s.TP) * c.G);
+    const int left = rows - (int)blockIdx.y * 32;
+    if (left <= 0) return;
+    const int RP = left >= 32 ? 32 : left > 8 ? 16 : left > 4 ? 8 : 4;
     const float* parts = reinterpret_cast<const float*>(a.scratch + part_off);
-    auto part = [&](int w) { return parts + ((size_t)w * 2 + (w == m.first ? 1 : 0)) * part_floats(part_rows, DH); };
-    float M = -INFINITY;
-    for (int w = m.first + lane; w <= m.last; w += 32) M = fmaxf(M, part(w)[(size_t)part_rows * DH + 2 * row]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    const float ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f, o[N] = {};
-    for (int w0 = m.first; w0 <= m.last; w0 += 32) {
-        float wt = 0.f;
-        if (w0 + lane <= m.last) {
-            const float2 ml = *reinterpret_cast<const float2*>(part(w0 + lane) + (size_t)part_rows * DH + 2 * row);
-            wt = exp2f(ml.x - ref);
-            L += wt * ml.y;
-        }
-        const int k = min(32, m.last - w0 + 1);
+    const size_t step = part_floats(part_rows, DH);
+    const float* p0 = parts + ((size_t)m.first * 2 + 1) * step;  // the first worker's part
+    const float* p1 = parts + (size_t)m.first * 2 * step;        // part of worker first + i: p1 + 2 i step
+    const int n = m.last - m.first;
+    for (int r0 = 0; r0 < min(left, 32); r0 += RP) {
+        const int row = blockIdx.y * 32 + r0 + threadIdx.x % RP;
+        if (row >= rows) continue;
+        const size_t ml = (size_t)part_rows * DH + 2 * row;
+        float M = p0[ml];
 #pragma unroll 8
-        for (int j = 0; j < k; ++j) {
-            const float f = __shfl_sync(0xffffffffu, wt, j);
-            float x[N];
-            load_f<float, N>(part(w0 + j) + (size_t)row * DH + lane * N, x);
+        for (int i = 1; i <= n; ++i) M = fmaxf(M, p1[2 * i * step + ml]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        const int tok = row / c.G, g = item % c.n_kv, t = q_row(c, m.b) + m.tile * s.TP + tok;
+        T* out = static_cast<T*>(a.out) + (size_t)t * a.ld_out + (size_t)(g * c.G + row - tok * c.G) * DH;
+        for (int c4 = threadIdx.x / RP; c4 < DH / 4; c4 += 128 / RP) {
+            const size_t at = ((size_t)c4 * part_rows + row) * 4;
+            float o[4] = {}, L = 0.f;
+#pragma unroll 8
+            for (int i = 0; i <= n; ++i) {
+                const float* p = i ? p1 + 2 * i * step : p0;
+                const float2 e = *reinterpret_cast<const float2*>(p + ml);
+                const float4 x = *reinterpret_cast<const float4*>(p + at);
+                const float f = exp2f(e.x - ref);
+                L = fmaf(f, e.y, L);
+                o[0] = fmaf(f, x.x, o[0]);
+                o[1] = fmaf(f, x.y, o[1]);
+                o[2] = fmaf(f, x.z, o[2]);
+                o[3] = fmaf(f, x.w, o[3]);
+            }
+            const float inv = L > 0.f ? 1.0f / L : 0.f;
 #pragma unroll
-            for (int e = 0; e < N; ++e) o[e] = fmaf(f, x[e], o[e]);
+            for (int e = 0; e < 4; ++e) o[e] *= inv;
+            store_f<T, 4>(out + c4 * 4, o);
         }
     }
-    L = warp_sum(L);
-    const float inv = L > 0.f ? 1.0f / L : 0.f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) o[e] *= inv;
-    const int g = item % c.n_kv, t = q_row(c, m.b) + (int)i;
-    store_f<T, N>(static_cast<T*>(a.out) + (size_t)t * a.ld_out + (size_t)(g * c.G + row % c.G) * DH + lane * N, o);
 }
 
 }  // namespace pipo
