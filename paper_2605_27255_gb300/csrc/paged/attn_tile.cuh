@@ -50,17 +50,32 @@ namespace pipo {
 constexpr int kAtThreads = 512;
 constexpr int kAtRegsIo = 56, kAtRegsSoft = 200;
 static_assert(2 * kAtRegsIo + 2 * kAtRegsSoft <= 4 * 128, "register shares must fit the launch's registers");
-constexpr int kAtHalf = 128 * 128;  // 64 dims of a tile: 128 rows of 128 bytes
-constexpr float kAtSlack = 8.f;     // exponents above the reference before it moves
+constexpr int kAtHalf = 128 * 128;      // 64 dims of a query tile: 128 rows of 128 bytes
+constexpr int kPageHalf = kPage * 128;  // 64 dims of a page
+constexpr float kAtSlack = 8.f;         // exponents above the reference before it moves
 
-__host__ __device__ constexpr int at_tile_bytes(int dh) { return dh / 64 * kAtHalf; }
-// Stages of one ring: an even number, so that a stage holds K tiles only or V tiles
-// only.  Every warp that waits for a stage then waits for each of its fills in turn; with an odd number
-// the score warps would pass over every second one, and a parity does not tell
-// a fill from the one two before it.
-__host__ __device__ constexpr int at_stages(int dh, bool pair) { return pair ? (dh == 128 ? 4 : 8) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr int at_q_bytes(int dh) { return dh / 64 * kAtHalf; }
+__host__ __device__ constexpr int at_page_bytes(int dh) { return dh / 64 * kPageHalf; }
+// Pages in a ring of K and in one of V (single: each pipeline has its own two).  Separate
+// rings: the score warps wait for every K page in turn and the value warps for every V
+// page, so that a parity always tells a fill from the one before it.
+__host__ __device__ constexpr int at_k_pages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 3 : 6); }
+__host__ __device__ constexpr int at_v_pages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 2 : 6); }
 __host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
-    return 1024 + (size_t)at_tile_bytes(dh) * (2 + at_stages(dh, pair) * (pair ? 1 : 2));
+    return 1024 + 2 * (size_t)at_q_bytes(dh) +
+           (size_t)at_page_bytes(dh) * (at_k_pages(dh, pair) + at_v_pages(dh, pair)) * (pair ? 1 : 2);
+}
+
+// B operand [entries][dims] of a page (MN-major, 128-byte swizzle): 64-dim blocks kPageHalf apart,
+// groups of 8 entries 1024 bytes apart
+__device__ __forceinline__ uint64_t umma_desc_mn_page(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+    d |= (uint64_t)(kPageHalf >> 4) << 16;  // leading byte offset: next 64 dims
+    d |= (uint64_t)(1024 >> 4) << 32;       // stride byte offset: next 8 entries
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
 }
 
 // x / G for x < 256 and G <= 16, magic = ceil(2^16 / G): off by less than 256 / 2^16 < 1 / G
@@ -133,19 +148,18 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                                                   int part_rows, size_t part_off,
                                                                   const __grid_constant__ CUtensorMap tmK,
                                                                   const __grid_constant__ CUtensorMap tmV) {
-    constexpr int kTile = at_tile_bytes(DH), ST = at_stages(DH, PAIR), NR = PAIR ? 1 : 2;  // NR: rings
-    static_assert(ST % 2 == 0, "a stage is for K or for V");
-    constexpr int kPageHalf = kPage * 128;  // 64 dims of a page
+    constexpr int kTile = at_q_bytes(DH), kPg = at_page_bytes(DH), NR = PAIR ? 1 : 2;  // NR: pairs of rings
+    constexpr int SK = at_k_pages(DH, PAIR), SV = at_v_pages(DH, PAIR);
     extern __shared__ __align__(1024) unsigned char at_smem_raw[];
     __shared__ uint32_t tmem_base;
-    __shared__ __align__(8) uint64_t full[NR][ST], empty[NR][ST];
+    __shared__ __align__(8) uint64_t k_full[NR][SK], k_empty[NR][SK], v_full[NR][SV], v_empty[NR][SV];
     __shared__ __align__(8) uint64_t q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained[4];
     __shared__ Piece pieces[NR];
     __shared__ int give_up;
 
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* q_s = sm;              // two query tiles
-    unsigned char* ring_s = sm + 2 * kTile;  // NR rings of ST stages
+    unsigned char* ring_s = sm + 2 * kTile;  // NR times SK pages of K, SV pages of V
 
     const PagedArgs& c = p.c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -153,11 +167,16 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
     if (threadIdx.x == 32) {
         prefetch_tmap(&tmK);
         prefetch_tmap(&tmV);
-        for (int r = 0; r < NR; ++r)
-            for (int i = 0; i < ST; ++i) {
-                mbar_init(&full[r][i], 1);
-                mbar_init(&empty[r][i], PAIR ? 2 : 1);  // the pipelines that read a stage
+        for (int r = 0; r < NR; ++r) {  // (an empty barrier counts the pipelines that read a page)
+            for (int i = 0; i < SK; ++i) {
+                mbar_init(&k_full[r][i], 1);
+                mbar_init(&k_empty[r][i], PAIR ? 2 : 1);
             }
+            for (int i = 0; i < SV; ++i) {
+                mbar_init(&v_full[r][i], 1);
+                mbar_init(&v_empty[r][i], PAIR ? 2 : 1);
+            }
+        }
         for (int w = 0; w < 2; ++w) {
             mbar_init(q_full + w, 4);  // softmax warps
             for (int i = 0; i < 2; ++i) {
@@ -196,103 +215,113 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         if ((warp & 1) ? true : warp < 4 && !(PAIR && warp == 2)) {
             ItemWalk it;
             it.start(c, shape, pieces[ring]);
-            uint64_t* fu = full[ring];
-            uint64_t* em = empty[ring];
-            unsigned char* rs = ring_s + (size_t)ring * ST * kTile;
+            unsigned char* k_s = ring_s + (size_t)ring * (SK + SV) * kPg;
+            unsigned char* v_s = k_s + SK * kPg;
             if ((warp & 1) == 0) {
-                // ---- copies: K then V of every unit
-                int k = 0;  // copies issued
+                // ---- copies: the keys one page ahead of the values
+                int kn = 0, vn = 0;  // pages issued
                 bool ok = true;
                 for (; it.more() && ok; it.next(c, shape)) {
                     const int32_t* list =
                         shape.n_top > 0 ? p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top : nullptr;
-                    const int seen = 2 * it.t0 + it.np;  // end of the pages to be read
-                    int held = -32, mine = -1;                      // lane l holds page held + l
-                    for (int u = it.kv0; u < it.kv1 && ok; ++u) {
-                        const int pg = (it.t0 + u) * 2;  // index in the cache or the list
-                        if (pg >= held + 32) {
-                            held = pg;
-                            const int i = pg + lane;
-                            if (list) {
-                                const int q = i < shape.n_top ? list[i] : -1;
-                                mine = q >= 0 ? page_block(c, it.b, q) : -1;
-                            } else {
-                                mine = i < seen && i * kPage < it.len ? page_block(c, it.b, i) : -1;
+                    const int np = it.pages(), pg0 = (it.t0 + it.kv0) * 2;  // first page in the cache or the list
+                    int held = -32, mine = -1;  // lane l holds the block of page held + l
+                    int prev = -1;              // block of the page whose values come next
+                    for (int j = 0; j <= np; ++j) {
+                        int blk = -1;
+                        if (j < np) {
+                            if (j >= held + 32) {
+                                held = j;
+                                const int i = pg0 + j + lane;
+                                if (list) {
+                                    const int q = i < shape.n_top ? list[i] : -1;
+                                    mine = q >= 0 ? page_block(c, it.b, q) : -1;
+                                } else {
+                                    mine = j + lane < np && i * kPage < it.len ? page_block(c, it.b, i) : -1;
+                                }
                             }
+                            blk = __shfl_sync(0xffffffffu, mine, j - held);
                         }
-                        int blk[2];
-                        blk[0] = __shfl_sync(0xffffffffu, mine, pg - held);
-                        blk[1] = __shfl_sync(0xffffffffu, mine, pg - held + 1);
-                        const int np = blk[0] < 0 ? 0 : blk[1] < 0 ? 1 : 2;
 #pragma unroll
-                        for (int v = 0; v < 2 && ok; ++v, ++k) {
-                            const int st = k % ST;
-                            ok = k < ST || wait(em + st, (uint32_t)(((k / ST) & 1) ^ 1), 51, k);
+                        for (int v = 0; v < 2; ++v) {
+                            if (v ? j == 0 : j == np) continue;
+                            const int n = v ? vn : kn, S_ = v ? SV : SK, st = n % S_, from = v ? prev : blk;
+                            uint64_t* fu = v ? &v_full[ring][st] : &k_full[ring][st];
+                            ok = n < S_ || wait(v ? &v_empty[ring][st] : &k_empty[ring][st], (uint32_t)(((n / S_) & 1) ^ 1), 51, n);
                             if (!ok) break;
                             if (lane == 0) {
-                                if (np == 0) mbar_arrive(fu + st);
-                                else mbar_arrive_expect_tx(fu + st, (uint32_t)(np * (DH / 64) * kPageHalf));
-                                for (int i = 0; i < np; ++i)
+                                if (from < 0) {
+                                    mbar_arrive(fu);
+                                } else {
+                                    mbar_arrive_expect_tx(fu, (uint32_t)kPg);
+#pragma unroll
                                     for (int d = 0; d < DH / 64; ++d)
-                                        tma_load_2d(rs + (size_t)st * kTile + d * kAtHalf + i * kPageHalf, v ? &tmV : &tmK,
-                                                    d * 64, (blk[i] * c.n_kv + it.g) * kPage, fu + st);
+                                        tma_load_2d((v ? v_s : k_s) + st * kPg + d * kPageHalf, v ? &tmV : &tmK, d * 64,
+                                                    (from * c.n_kv + it.g) * kPage, fu);
+                                }
                             }
+                            if (v) ++vn; else ++kn;
                         }
                         __syncwarp();
+                        if (!ok) break;
+                        prev = blk;
                     }
                 }
                 // no copy into this CTA's shared memory is in flight at its end
-                if (lane == 0) ring_drain<ST>(k, [&](int st, uint32_t ph, int i) { mbar_wait(fu + st, ph, 52, (unsigned)i); });
+                if (lane == 0) {
+                    ring_drain<SK>(kn, [&](int st, uint32_t ph, int i) { mbar_wait(&k_full[ring][st], ph, 52, (unsigned)i); });
+                    ring_drain<SV>(vn, [&](int st, uint32_t ph, int i) { mbar_wait(&v_full[ring][st], ph, 52, (unsigned)i); });
+                }
             } else {
                 // ---- MMAs.  TMEM: scores / weights of pipeline w at w * 128 (two buffers of 64 columns),
                 // its output at 256 + w * 128
                 const bool values = warp >= 12;  // this warp's half of them
-                int k = 0;        // ring position of the unit's K tile
                 int items = 0;    // items begun
-                int pv = 0;       // pages done
+                int n = 0;        // pages of K or V taken from the ring
+                int pv = 0;       // pages of this pipeline
                 bool ok = true;
                 const uint32_t s_at = tmem + (uint32_t)(chain * 128), o_at = s_at + 256u;
-                auto filled = [&](int i) { return wait(fu + i % ST, (uint32_t)((i / ST) & 1), 54, i); };
-                for (; it.more() && ok; it.next(c, shape), ++items) {
-                    const int np = it.pages(), nu = it.kv1 - it.kv0;
-                    if (PAIR && chain * 128 >= it.tokens(shape) * c.G) {  // no rows here: hand the stages on
-                        for (int i = values; i < 2 * nu && ok; i += 2) {
-                            ok = filled(k + i);
-                            if (ok && lane == 0) mbar_arrive(em + (k + i) % ST);
+                auto filled = [&](int i) {
+                    return values ? wait(&v_full[ring][i % SV], (uint32_t)((i / SV) & 1), 54, i)
+                                  : wait(&k_full[ring][i % SK], (uint32_t)((i / SK) & 1), 54, i);
+                };
+                for (; it.more() && ok; it.next(c, shape)) {
+                    const int np = it.pages();
+                    if (PAIR && chain * 128 >= it.tokens(shape) * c.G) {  // no rows here: hand the pages on
+                        for (int j = 0; j < np && ok; ++j, ++n) {
+                            ok = filled(n);
+                            if (ok && lane == 0) mbar_arrive(values ? &v_empty[ring][n % SV] : &k_empty[ring][n % SK]);
                         }
-                        k += 2 * nu;
-                        --items;
                         continue;
                     }
                     if (!values) {
                         constexpr uint32_t id_s = umma_idesc_bf16(128, kPage);
                         // descriptors count in 16 bytes: a step along a tile is an addition
-                        const uint64_t dq = umma_desc_sw128(smem_u32(q_s) + chain * kTile), dk = umma_desc_sw128(smem_u32(rs));
+                        const uint64_t dq = umma_desc_sw128(smem_u32(q_s) + chain * kTile), dk = umma_desc_sw128(smem_u32(k_s));
                         ok = wait(q_full + chain, (uint32_t)(items & 1), 53, items);
-                        for (int j = 0; j < np && ok; ++j, ++pv) {  // page j of the item: half j % 2 of its unit's K tile
-                            const int h = j & 1, st = (k + (j & ~1)) % ST, buf = pv & 1;
+                        for (int j = 0; j < np && ok; ++j, ++pv, ++n) {
+                            const int st = n % SK, buf = pv & 1;
                             // the weights of the page before last lie in the buffer until their values are done
-                            ok = (h == 1 || filled(k + j)) &&
-                                 (j < 2 || wait(&o_full[chain][buf], (uint32_t)(((pv - 2) >> 1) & 1), 56, pv));
+                            ok = filled(n) && (j < 2 || wait(&o_full[chain][buf], (uint32_t)(((pv - 2) >> 1) & 1), 56, pv));
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
-                                uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)((st * kTile + h * kPageHalf) >> 4);
+                                uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)((st * kPg) >> 4);
                                 asm volatile("" : "+r"(qb), "+r"(kb));  // eight sums now, not sixteen kept over the loop
 #pragma unroll
-                                for (int i = 0; i < DH / 16; ++i) {
-                                    const uint32_t o = ((i >> 2) * kAtHalf + (i & 3) * 32) >> 4;
-                                    umma_bf16(s_at + buf * 64, u32x2(qb + o, (uint32_t)(dq >> 32)),
-                                              u32x2(kb + o, (uint32_t)(dk >> 32)), id_s, i > 0 ? 1u : 0u);
-                                }
+                                for (int i = 0; i < DH / 16; ++i)
+                                    umma_bf16(s_at + buf * 64,
+                                              u32x2(qb + (((i >> 2) * kAtHalf + (i & 3) * 32) >> 4), (uint32_t)(dq >> 32)),
+                                              u32x2(kb + (((i >> 2) * kPageHalf + (i & 3) * 32) >> 4), (uint32_t)(dk >> 32)), id_s,
+                                              i > 0 ? 1u : 0u);
                                 umma_commit(&s_full[chain][buf]);
-                                if (h == 1 || j + 1 == np) umma_commit(em + st);
+                                umma_commit(&k_empty[ring][st]);
                             }
                             __syncwarp();
                         }
                     } else {
                         constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
-                        const uint64_t dv = umma_desc_mn128(smem_u32(rs));
+                        const uint64_t dv = umma_desc_mn_page(smem_u32(v_s));
                         // entries whose values may be anything: those past the sequence's (or the list's) end
                         int end = it.len;
                         if (shape.n_top > 0) {
@@ -301,40 +330,38 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             const int32_t* list = p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top;
                             end = kept == 0 ? 0 : (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage + 1 : kPage);
                         }
-                        for (int j = 0; j < np; ++j, ++pv) {
-                            const int h = j & 1, st = (k + (j & ~1) + 1) % ST, buf = pv & 1;
-                            if (h == 0) {
-                                ok = filled(k + j + 1);
-                                if (!ok) break;
-                                const int tail = end - (it.t0 + it.kv0 + j / 2) * kTileEnt;
-                                if (tail < kTileEnt) {  // (PAIR: both pipelines clear the same rows before their own MMAs)
-                                    const int r0 = max(0, tail);
-                                    for (int i = lane; i < (kTileEnt - r0) * (DH / 8); i += 32) {
-                                        const int r = r0 + i / (DH / 8), ch = i % (DH / 8);
-                                        *reinterpret_cast<uint4*>(rs + (size_t)st * kTile + (ch >> 3) * kAtHalf + r * 128 +
-                                                                  (ch & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                                    }
-                                    fence_proxy_async();
-                                    __syncwarp();
+                        for (int j = 0; j < np; ++j, ++pv, ++n) {
+                            const int st = n % SV, buf = pv & 1;
+                            ok = filled(n);
+                            if (!ok) break;
+                            const int tail = end - (it.t0 + it.kv0) * kTileEnt - j * kPage;
+                            if (tail < kPage) {  // (PAIR: both pipelines clear the same rows before their own MMAs)
+                                const int r0 = max(0, tail);
+                                for (int i = lane; i < (kPage - r0) * (DH / 8); i += 32) {
+                                    const int r = r0 + i / (DH / 8), ch = i % (DH / 8);
+                                    *reinterpret_cast<uint4*>(v_s + st * kPg + (ch >> 3) * kPageHalf + r * 128 + (ch & 7) * 16) =
+                                        make_uint4(0u, 0u, 0u, 0u);
                                 }
+                                fence_proxy_async();
+                                __syncwarp();
                             }
                             ok = wait(&p_full[chain][buf], (uint32_t)((pv >> 1) & 1), 55, pv);
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
-                                uint32_t vb = (uint32_t)dv + (uint32_t)((st * kTile + h * kPageHalf) >> 4);
+                                uint32_t vb = (uint32_t)dv + (uint32_t)((st * kPg) >> 4);
                                 asm volatile("" : "+r"(vb));
 #pragma unroll
                                 for (int i = 0; i < kPage / 16; ++i)
                                     umma_bf16_ta(o_at, s_at + buf * 64 + i * 8, u32x2(vb + i * (2048 >> 4), (uint32_t)(dv >> 32)),
                                                  id_o, i > 0 || j > 0 ? 1u : 0u);
                                 umma_commit(&o_full[chain][buf]);
-                                if (h == 1 || j + 1 == np) umma_commit(em + st);
+                                umma_commit(&v_empty[ring][st]);
                             }
                             __syncwarp();
                         }
                     }
-                    k += 2 * nu;
+                    ++items;
                 }
                 // commits arrive in order: after one more, none is in flight at the CTA's end
                 if (elect_one()) {
@@ -503,7 +530,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             }
             if (it.kv0 == 0 && row0 + r == 0)
                 reinterpret_cast<ItemMeta*>(p.scratch + kScratchHead)[(size_t)it.index * c.n_kv + it.g] = {
-                    it.b, it.tile, me, it.whole() ? me : it.last_worker(pieces[PAIR ? 0 : w])};
+                    it.q0 + i0, it.tokens(shape) * c.G, me, it.whole() ? me : it.last_worker(pieces[PAIR ? 0 : w])};
             tc_fence_before();  // the output is read, before the next item's values overwrite it
         }
     }

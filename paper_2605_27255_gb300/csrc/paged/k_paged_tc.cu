@@ -28,7 +28,7 @@ cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMa
     at[0].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = at;
     lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, &combine_kernel<DH, bf16_t>, a, shape, pl.workers, pl.part_rows, pl.part_off);
+    return cudaLaunchKernelEx(&lc, &combine_kernel<DH, bf16_t>, a, pl.workers, pl.part_rows, pl.part_off);
 }
 
 }  // namespace

@@ -46,8 +46,8 @@ __device__ __forceinline__ RowTile row_tile(const ItemShape& s, int n, int len, 
 __device__ __forceinline__ int seq_new(const PagedArgs& c, int b) { return max(0, q_row(c, b + 1) - q_row(c, b)); }
 
 // scratch header, then one ItemMeta per item, then the partials
-struct ItemMeta {
-    int b, tile;        // sequence and row tile
+struct alignas(16) ItemMeta {
+    int token, rows;    // first token row, rows
     int first, last;    // the workers that share it (first == last: nobody)
 };
 constexpr size_t kScratchHead = 16;  // int: number of row tiles
@@ -244,56 +244,72 @@ struct ItemWalk {
 // Joins the parts of the shared items.  grid (items, row groups of 32), 128 threads.
 // out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the workers first .. last in
 // order; the first one's part is its second slot, the others' their first.  A thread takes one
-// row and every (128 / RP)-th group of four dims, RP rows side by side as they lie in the parts.
+// row and every (128 / RP)-th group of four dims, RP (4 or 32) rows side by side as they lie in
+// the parts, with eight loads in flight.
+template <int DH, typename T, int RP>
+__device__ __forceinline__ void combine_rows(const AttnPagedArgs& a, const ItemMeta& m, int g, int row, const float* p0,
+                                             const float* p1, size_t step, int part_rows) {
+    constexpr int NC = DH * RP >= 512 ? DH * RP / 512 : 1, UI = 8 / NC;  // groups of four dims per thread; parts in flight
+    const int n = m.last - m.first;
+    const size_t ml = (size_t)part_rows * DH + 2 * row;
+    const float* x0 = p0 + ((size_t)(threadIdx.x / RP) * part_rows + row) * 4;
+    const float* x1 = p1 + ((size_t)(threadIdx.x / RP) * part_rows + row) * 4;
+    const size_t cs = (size_t)(128 / RP) * part_rows * 4;  // this thread's next group
+    float M = p0[ml];
+#pragma unroll 8
+    for (int i = 1; i <= n; ++i) M = fmaxf(M, p1[2 * i * step + ml]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float o[NC][4] = {}, L = 0.f;
+#pragma unroll UI
+    for (int i = 0; i <= n; ++i) {
+        const float2 e = *reinterpret_cast<const float2*>((i ? p1 + 2 * i * step : p0) + ml);
+        const float* x = i ? x1 + 2 * i * step : x0;
+        float4 v[NC];
+#pragma unroll
+        for (int k = 0; k < NC; ++k) v[k] = *reinterpret_cast<const float4*>(x + k * cs);
+        const float f = exp2f(e.x - ref);
+        L = fmaf(f, e.y, L);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            o[k][0] = fmaf(f, v[k].x, o[k][0]);
+            o[k][1] = fmaf(f, v[k].y, o[k][1]);
+            o[k][2] = fmaf(f, v[k].z, o[k][2]);
+            o[k][3] = fmaf(f, v[k].w, o[k][3]);
+        }
+    }
+    const float inv = L > 0.f ? 1.0f / L : 0.f;
+    const int G = a.c.G, tok = row / G;
+    T* out = static_cast<T*>(a.out) + (size_t)(m.token + tok) * a.ld_out + (size_t)(g * G + row - tok * G) * DH;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[k][e] *= inv;
+        store_f<T, 4>(out + (threadIdx.x / RP + k * (128 / RP)) * 4, o[k]);
+    }
+}
+
 template <int DH, typename T>
-__global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, ItemShape s, int workers, int part_rows,
-                                                      size_t part_off) {
+__global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, int workers, int part_rows, size_t part_off) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const PagedArgs& c = a.c;
-    const int item = blockIdx.x;
-    if (item / c.n_kv >= *reinterpret_cast<const int*>(a.scratch)) return;
+    const int item = blockIdx.x, n_kv = a.c.n_kv;
+    const int tiles = *reinterpret_cast<const int*>(a.scratch);
     const ItemMeta m = reinterpret_cast<const ItemMeta*>(a.scratch + kScratchHead)[item];
-    // (after a wait that gave up, the scratch may lack items: nothing outside it is read)
-    if (m.first < 0 || m.first >= m.last || m.last >= workers || m.b < 0 || m.b >= c.batch || m.tile < 0) return;
-    const int rows = (int)min((long long)s.TP * c.G, ((long long)seq_new(c, m.b) - (long long)m.tile * s.TP) * c.G);
-    const int left = rows - (int)blockIdx.y * 32;
-    if (left <= 0) return;
-    const int RP = left >= 32 ? 32 : left > 8 ? 16 : left > 4 ? 8 : 4;
+    const int left = m.rows - (int)blockIdx.y * 32;
+    if (item / n_kv >= tiles || m.first == m.last || left <= 0) return;
+    // (after a wait that gave up, the scratch may lack items: nothing outside it is read or written)
+    if (m.first < 0 || m.first > m.last || m.last >= workers || m.rows > part_rows || m.token < 0 ||
+        m.token + (m.rows - 1) / a.c.G >= a.c.n_tokens)
+        return;
     const float* parts = reinterpret_cast<const float*>(a.scratch + part_off);
     const size_t step = part_floats(part_rows, DH);
     const float* p0 = parts + ((size_t)m.first * 2 + 1) * step;  // the first worker's part
     const float* p1 = parts + (size_t)m.first * 2 * step;        // part of worker first + i: p1 + 2 i step
-    const int n = m.last - m.first;
-    for (int r0 = 0; r0 < min(left, 32); r0 += RP) {
-        const int row = blockIdx.y * 32 + r0 + threadIdx.x % RP;
-        if (row >= rows) continue;
-        const size_t ml = (size_t)part_rows * DH + 2 * row;
-        float M = p0[ml];
-#pragma unroll 8
-        for (int i = 1; i <= n; ++i) M = fmaxf(M, p1[2 * i * step + ml]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        const int tok = row / c.G, g = item % c.n_kv, t = q_row(c, m.b) + m.tile * s.TP + tok;
-        T* out = static_cast<T*>(a.out) + (size_t)t * a.ld_out + (size_t)(g * c.G + row - tok * c.G) * DH;
-        for (int c4 = threadIdx.x / RP; c4 < DH / 4; c4 += 128 / RP) {
-            const size_t at = ((size_t)c4 * part_rows + row) * 4;
-            float o[4] = {}, L = 0.f;
-#pragma unroll 8
-            for (int i = 0; i <= n; ++i) {
-                const float* p = i ? p1 + 2 * i * step : p0;
-                const float2 e = *reinterpret_cast<const float2*>(p + ml);
-                const float4 x = *reinterpret_cast<const float4*>(p + at);
-                const float f = exp2f(e.x - ref);
-                L = fmaf(f, e.y, L);
-                o[0] = fmaf(f, x.x, o[0]);
-                o[1] = fmaf(f, x.y, o[1]);
-                o[2] = fmaf(f, x.z, o[2]);
-                o[3] = fmaf(f, x.w, o[3]);
-            }
-            const float inv = L > 0.f ? 1.0f / L : 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] *= inv;
-            store_f<T, 4>(out + c4 * 4, o);
-        }
+    const int row = blockIdx.y * 32, g = item % n_kv;
+    if (left > 4) {
+        if ((int)threadIdx.x % 32 < left)
+            combine_rows<DH, T, 32>(a, m, g, row + threadIdx.x % 32, p0, p1, step, part_rows);
+    } else if ((int)threadIdx.x % 4 < left && (DH == 128 || threadIdx.x < 64)) {
+        combine_rows<DH, T, 4>(a, m, g, row + threadIdx.x % 4, p0, p1, step, part_rows);
     }
 }
 
