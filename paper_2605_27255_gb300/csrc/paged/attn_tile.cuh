@@ -190,6 +190,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         give_up = 0;
         mbar_init_fence();
     }
+    pdl_wait();  // lengths, queries, entries and the scratch come from the kernels before
     // (the sequences' tile counts use the ring's memory before any copy)
     find_pieces<kAtThreads, NR>(c, shape, (int)blockIdx.x * NR, S, reinterpret_cast<int*>(ring_s), pieces,
                                 reinterpret_cast<int*>(p.scratch));

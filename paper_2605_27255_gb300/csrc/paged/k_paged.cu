@@ -13,17 +13,35 @@ unsigned ceil_div(long long a, long long b) { return (unsigned)((a + b - 1) / b)
 template <int DH, typename TI, typename T>
 cudaError_t append_as(const AppendArgs& a, cudaStream_t s) {
     // pages that receive entries: a sequence with n new tokens spans at most n / 64 + 2
-    const long long runs = a.c.n_tokens < a.c.n_tokens / kPage + 2LL * a.c.batch ? a.c.n_tokens
-                                                                              : a.c.n_tokens / kPage + 2LL * a.c.batch;
+    const long long t = a.c.n_tokens, most = t / kPage + 2LL * a.c.batch, runs = t < most ? t : most;
     const int pages = (int)(runs * a.c.n_kv);
-    const unsigned rows = a.q_out ? ceil_div((long long)a.c.n_tokens * a.c.n_q, kAppendWarps * kAppendRows) : 0;
-    kv_append_kernel<DH, TI, T><<<pages + rows, kAppendWarps * 32, 0, s>>>(a, pages);
-    return cudaGetLastError();
+    const unsigned rows = a.q_out ? ceil_div(t, kAppendWarps) : 0;
+    return launch_pdl(&kv_append_kernel<DH, TI, T>, dim3(pages + rows), kAppendWarps * 32, 0, s, a, pages);
 }
 
 template <int DH, typename T>
 cudaError_t append_in(const AppendArgs& a, cudaStream_t s) {
     return a.in_bf16 ? append_as<DH, bf16_t, T>(a, s) : append_as<DH, float, T>(a, s);
+}
+
+template <int DH, typename T>
+cudaError_t scores_as(const ScoreArgs& a, cudaStream_t s) {
+    const unsigned y = ceil_div(a.c.max_pages, kScorePages);
+    // Token by token below two tokens a sequence on average: a chunk's CTA costs about as much as
+    // four single tokens', whose means are then read from L2 anyway.
+    if ((long long)a.c.n_tokens < 2LL * a.c.batch || a.c.n_tokens < 4)
+        return launch_pdl(&page_scores_kernel<DH, T>, dim3((unsigned)(a.c.n_tokens * (long long)a.c.n_kv), y), 128, 0, s, a);
+    static thread_local int ready = -1;  // the shared-memory limit is set per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && ready != dev) {
+        e = cudaFuncSetAttribute(&page_scores_chunk_kernel<DH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)score_smem(DH));
+        if (e == cudaSuccess) ready = dev;
+    }
+    if (e != cudaSuccess) return e;
+    const long long t = a.c.n_tokens, most = t / kScoreTok + a.c.batch, tiles = t < most ? t : most;
+    return launch_pdl(&page_scores_chunk_kernel<DH, T>, dim3((unsigned)(tiles * a.c.n_kv), y), 256, score_smem(DH), s, a);
 }
 
 }  // namespace
@@ -34,20 +52,16 @@ cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s) {
 }
 
 cudaError_t launch_page_scores(const ScoreArgs& a, cudaStream_t s) {
-    const unsigned n = ceil_div((long long)a.c.n_tokens * a.c.n_kv, 4);
-    if (a.c.dh == 64) {
-        if (a.c.dtype) page_scores_kernel<64, bf16_t><<<n, 128, 0, s>>>(a);
-        else page_scores_kernel<64, float><<<n, 128, 0, s>>>(a);
-    } else {
-        if (a.c.dtype) page_scores_kernel<128, bf16_t><<<n, 128, 0, s>>>(a);
-        else page_scores_kernel<128, float><<<n, 128, 0, s>>>(a);
-    }
-    return cudaGetLastError();
+    if (a.c.dh == 64) return a.c.dtype ? scores_as<64, bf16_t>(a, s) : scores_as<64, float>(a, s);
+    return a.c.dtype ? scores_as<128, bf16_t>(a, s) : scores_as<128, float>(a, s);
 }
 
 cudaError_t launch_page_select(const SelectArgs& a, cudaStream_t s) {
-    page_select_kernel<<<ceil_div((long long)a.c.n_tokens * a.c.n_kv, 4), 128, 0, s>>>(a);
-    return cudaGetLastError();
+    const dim3 n(ceil_div((long long)a.c.n_tokens * a.c.n_kv, 4));
+    if (a.c.max_pages <= 128) return launch_pdl(&page_select_kernel<4>, n, 128, 0, s, a);
+    if (a.c.max_pages <= 256) return launch_pdl(&page_select_kernel<8>, n, 128, 0, s, a);
+    if (a.c.max_pages <= 1024) return launch_pdl(&page_select_kernel<32>, n, 128, 0, s, a);
+    return launch_pdl(&page_select_kernel<0>, n, 128, 0, s, a);
 }
 
 cudaError_t launch_attn_plain(const AttnPagedArgs& a, cudaStream_t s) {

@@ -16,19 +16,12 @@ cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMa
         ready_dev = pl.dev;
     }
     const ItemShape shape{pl.TP, a.window, a.pages ? a.n_top : 0};
-    fn<<<pl.ctas, kAtThreads, at_smem(DH, PAIR), s>>>(a, shape, pl.workers, pl.part_rows, pl.part_off, tk, tv);
-    cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kAtThreads, at_smem(DH, PAIR), s, a, shape, pl.workers,
+                                     pl.part_rows, pl.part_off, tk, tv);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 31) / 32));
-    lc.blockDim = dim3(128);
-    lc.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = at;
-    lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, &combine_kernel<DH, bf16_t>, a, pl.workers, pl.part_rows, pl.part_off);
+    return launch_pdl(&combine_kernel<DH, bf16_t>,
+                      dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 31) / 32)), 128, 0, s, a, pl.workers,
+                      pl.part_rows, pl.part_off);
 }
 
 }  // namespace

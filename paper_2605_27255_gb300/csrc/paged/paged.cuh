@@ -70,4 +70,20 @@ __device__ __forceinline__ Tok find_token(const PagedArgs& c, int t) {
     return {lo, max(-1, len - (end - t))};
 }
 
+// a launch whose blocks may start while the kernel before ends (each waits for it before it reads)
+template <typename... P, typename... A>
+inline cudaError_t launch_pdl(void (*fn)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, const A&... args) {
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = grid;
+    lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, fn, args...);
+}
+
 }  // namespace pipo

@@ -290,6 +290,7 @@ __device__ __forceinline__ void combine_rows(const AttnPagedArgs& a, const ItemM
 
 template <int DH, typename T>
 __global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, int workers, int part_rows, size_t part_off) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int item = blockIdx.x, n_kv = a.c.n_kv;
     const int tiles = *reinterpret_cast<const int*>(a.scratch);

@@ -26,6 +26,7 @@ import torch
 from . import capi
 
 PAGE = 64
+_raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's handle, without a Stream object
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -59,29 +60,31 @@ class PagedCache:
             raise ValueError("pools, table and means must be on one CUDA device")
         self.k, self.v, self.table, self.means = k, v, table, means
         self.n_q, self.n_kv, self.d_h, self.dtype, self.device = n_q, k.shape[1], k.shape[3], k.dtype, k.device
+        self.index = k.device.index
         self._c = capi.pipo_paged(_TYPES[k.dtype], n_q, k.shape[1], k.shape[3], PAGE, k.shape[0], table.shape[1],
                                   table.shape[0], k.data_ptr(), v.data_ptr(),
                                   None if means is None else means.data_ptr(), table.data_ptr())
+        self._seqs = table.shape[0]
         self._scratch: Optional[torch.Tensor] = None
         self._scratch_for = -1
 
     # ---- arguments
 
     def _batch(self, q_start: torch.Tensor, kv_len: torch.Tensor) -> None:
-        n = self.table.shape[0]
-        if q_start.dtype != torch.int32 or kv_len.dtype != torch.int32 or q_start.shape != (n + 1,) or \
-                kv_len.shape != (n,) or not q_start.is_contiguous() or not kv_len.is_contiguous() or \
-                q_start.device != self.device or kv_len.device != self.device:
+        n, i32 = self._seqs, torch.int32
+        if q_start.dtype is not i32 or kv_len.dtype is not i32 or q_start.shape != (n + 1,) or kv_len.shape != (n,) or \
+                not (q_start.is_contiguous() and kv_len.is_contiguous()) or q_start.device != self.device or \
+                kv_len.device != self.device:
             raise ValueError(f"q_start [{n + 1}] and kv_len [{n}] must be contiguous int32 on the pools' device")
         self._c.q_start, self._c.kv_len = q_start.data_ptr(), kv_len.data_ptr()
 
-    def _rows(self, x: torch.Tensor, heads: int, name: str, like: Optional[torch.dtype] = None) -> int:
+    def _rows(self, x: torch.Tensor, heads: int, name: str, dtype: torch.dtype) -> int:
         """Token stride of [tokens, heads, d_h] with the heads back to back."""
-        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.d_h or x.device != self.device or \
-                x.dtype != (like or self.dtype) or \
-                (x.shape[0] and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.d_h))):
-            raise ValueError(f"{name} must be [tokens, {heads}, {self.d_h}] {like or self.dtype} with whole rows")
-        return x.stride(0) if x.shape[0] > 1 else heads * self.d_h
+        shape, stride = x.shape, x.stride()
+        if len(shape) != 3 or shape[1] != heads or shape[2] != self.d_h or x.dtype is not dtype or \
+                x.device != self.device or (shape[0] and (stride[2] != 1 or (heads > 1 and stride[1] != self.d_h))):
+            raise ValueError(f"{name} must be [tokens, {heads}, {self.d_h}] {dtype} with whole rows")
+        return stride[0] if shape[0] > 1 else heads * self.d_h
 
     def _work(self, tokens: int) -> torch.Tensor:
         if self._scratch_for != tokens:
@@ -125,7 +128,7 @@ class PagedCache:
         p = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
         capi.pipo_op_kv_append(self._c, tokens, _TYPES[k.dtype], p(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
                                p(q_gain), p(k_gain), eps, p(rope), 0 if rope is None else rope.shape[0], p(out),
-                               torch.cuda.current_stream(self.device).cuda_stream)
+                               _raw_stream(self.index))
         return out
 
     def _out(self, q: torch.Tensor, out: Optional[torch.Tensor]) -> Tuple[torch.Tensor, int]:
@@ -134,7 +137,7 @@ class PagedCache:
             return out, self.n_q * self.d_h
         if out.shape[0] != q.shape[0]:
             raise ValueError("out must have a row for every token")
-        return out, self._rows(out, self.n_q, "out")
+        return out, self._rows(out, self.n_q, "out", self.dtype)
 
     def attend(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -142,12 +145,12 @@ class PagedCache:
         keeps the last ``window`` entries of every token.  scale: 1/sqrt(d_h)
         unless given."""
         self._batch(q_start, kv_len)
-        ld_q = self._rows(q, self.n_q, "q")
+        ld_q = self._rows(q, self.n_q, "q", self.dtype)
         out, ld_out = self._out(q, out)
         w = self._work(q.shape[0])
         capi.pipo_op_attn_paged(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
                                 window, out.data_ptr(), ld_out, w.data_ptr(), w.numel(),
-                                torch.cuda.current_stream(self.device).cuda_stream)
+                                _raw_stream(self.index))
         return out
 
     def page_scores(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
@@ -157,14 +160,14 @@ class PagedCache:
         if self.means is None:
             raise ValueError("page scores need a cache with means")
         self._batch(q_start, kv_len)
-        ld_q = self._rows(q, self.n_q, "q")
+        ld_q = self._rows(q, self.n_q, "q", self.dtype)
         shape = (q.shape[0], self.n_kv, self.table.shape[1])
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=self.device)
         elif out.shape != shape or out.dtype != torch.float32 or not out.is_contiguous() or out.device != self.device:
             raise ValueError("out must be a contiguous float32 [tokens, n_kv, max_pages]")
         capi.pipo_op_page_scores(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
-                                 out.data_ptr(), torch.cuda.current_stream(self.device).cuda_stream)
+                                 out.data_ptr(), _raw_stream(self.index))
         return out
 
     def attend_pages(self, q: torch.Tensor, scores: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
@@ -174,7 +177,7 @@ class PagedCache:
         ``sink``, the last ``local`` and the best scored.  Returns the outputs
         and the pages, int32 [tokens, n_kv, top], ascending, -1 behind the last."""
         self._batch(q_start, kv_len)
-        ld_q = self._rows(q, self.n_q, "q")
+        ld_q = self._rows(q, self.n_q, "q", self.dtype)
         if scores.shape != (q.shape[0], self.n_kv, self.table.shape[1]) or scores.dtype != torch.float32 or \
                 not scores.is_contiguous() or scores.device != self.device:
             raise ValueError("scores must be a contiguous float32 [tokens, n_kv, max_pages]")
@@ -183,5 +186,5 @@ class PagedCache:
         w = self._work(q.shape[0])
         capi.pipo_op_attn_pages(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
                                 scores.data_ptr(), top, sink, local, out.data_ptr(), ld_out, pages.data_ptr(),
-                                w.data_ptr(), w.numel(), torch.cuda.current_stream(self.device).cuda_stream)
+                                w.data_ptr(), w.numel(), _raw_stream(self.index))
         return out, pages
