@@ -1,7 +1,7 @@
 // Paged-cache operators: append, page scores, selection, attention on the CUDA
 // cores (a translation unit of its own).
 #include "append.cuh"
-#include "attn_plain.cuh"
+#include "attn_f32.cuh"
 #include "select.cuh"
 
 namespace pipo {
@@ -44,6 +44,22 @@ cudaError_t scores_as(const ScoreArgs& a, cudaStream_t s) {
     return launch_pdl(&page_scores_chunk_kernel<DH, T>, dim3((unsigned)(tiles * a.c.n_kv), y), 256, score_smem(DH), s, a);
 }
 
+template <int DH, int RT>
+cudaError_t f32_as(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
+    auto* fn = &attn_f32_kernel<DH, RT>;
+    static thread_local int ready = -1;  // the shared-memory limit is set per device
+    if (ready != pl.dev) {
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)af_smem_for(DH, RT, kPagedMaxBatch));
+        if (e != cudaSuccess) return e;
+        ready = pl.dev;
+    }
+    const ItemShape shape{pl.TP, a.window, a.pages ? a.n_top : 0};
+    const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kAfThreads, af_smem_for(DH, RT, a.c.batch), s, a, shape,
+                                     pl.workers, pl.part_rows, pl.part_off);
+    return e == cudaSuccess ? launch_combine<DH, float>(a, pl, s) : e;
+}
+
 }  // namespace
 
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s) {
@@ -64,16 +80,9 @@ cudaError_t launch_page_select(const SelectArgs& a, cudaStream_t s) {
     return launch_pdl(&page_select_kernel<0>, n, 128, 0, s, a);
 }
 
-cudaError_t launch_attn_plain(const AttnPagedArgs& a, cudaStream_t s) {
-    const unsigned n = ceil_div((long long)a.c.n_tokens * a.c.n_q, 4);
-    if (a.c.dh == 64) {
-        if (a.c.dtype) attn_plain_kernel<64, bf16_t><<<n, 128, 0, s>>>(a);
-        else attn_plain_kernel<64, float><<<n, 128, 0, s>>>(a);
-    } else {
-        if (a.c.dtype) attn_plain_kernel<128, bf16_t><<<n, 128, 0, s>>>(a);
-        else attn_plain_kernel<128, float><<<n, 128, 0, s>>>(a);
-    }
-    return cudaGetLastError();
+cudaError_t launch_attn_f32(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
+    if (a.c.dh == 64) return pl.rt == 4 ? f32_as<64, 4>(a, pl, s) : f32_as<64, 1>(a, pl, s);
+    return pl.rt == 4 ? f32_as<128, 4>(a, pl, s) : f32_as<128, 1>(a, pl, s);
 }
 
 }  // namespace pipo

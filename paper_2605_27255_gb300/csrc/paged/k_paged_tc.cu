@@ -1,4 +1,5 @@
 // Paged-cache attention on the tensor cores (a translation unit of its own).
+#include "attn_f32.cuh"
 #include "attn_tile.cuh"
 
 namespace pipo {
@@ -18,28 +19,36 @@ cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMa
     const ItemShape shape{pl.TP, a.window, a.pages ? a.n_top : 0};
     const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kAtThreads, at_smem(DH, PAIR), s, a, shape, pl.workers,
                                      pl.part_rows, pl.part_off, tk, tv);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(&combine_kernel<DH, bf16_t>,
-                      dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 31) / 32)), 128, 0, s, a, pl.workers,
-                      pl.part_rows, pl.part_off);
+    return e == cudaSuccess ? launch_combine<DH, bf16_t>(a, pl, s) : e;
 }
 
 }  // namespace
 
-// The plan of a bf16 launch.  Pairs of row tiles when the sequences of the batch
-// have more than 128 rows on average; scratch: see work.cuh.
-AttnPlan plan_attn_tile(const PagedArgs& c, bool listed, int dev, int sms) {
+// The plan of a launch; scratch: see work.cuh.
+// bf16: pairs of row tiles when the sequences of the batch have more than 128 rows
+// on average.  fp32: tiles of 64 rows when they have more than 16, else of 16.
+AttnPlan plan_attn(const PagedArgs& c, bool listed, int dev, int sms) {
     AttnPlan pl{};
     pl.dev = dev;
-    pl.pair = !listed && (long long)c.n_tokens * c.G > 128LL * c.batch;
-    const int rows = pl.pair ? 256 : 128;
+    const long long mine = (long long)c.n_tokens * c.G;
+    int rows, per;  // rows of a tile, workers of an SM
+    if (c.dtype) {
+        pl.pair = !listed && mine > 128LL * c.batch;
+        rows = pl.pair ? 256 : 128;
+        per = pl.pair ? 1 : 2;
+    } else {
+        pl.rt = !listed && mine > 16LL * c.batch ? 4 : 1;
+        rows = af_rows(pl.rt);
+        per = af_ctas(c.dh, pl.rt);
+    }
     pl.TP = listed ? 1 : rows / c.G;
     pl.tiles = tiles_bound(c.n_tokens, c.batch, pl.TP);
-    const long long most = pl.tiles * c.n_kv * ((c.max_pages + 1) / 2);  // units at most
-    const int per = pl.pair ? 1 : 2;
-    pl.ctas = (int)(most < (long long)sms * per ? (most + per - 1) / per : sms);
-    pl.workers = pl.ctas * per;
-    const long long mine = (long long)c.n_tokens * c.G;
+    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each;  // units of an item, in all, at most
+    pl.workers = (int)(most < (long long)sms * per ? most : (long long)sms * per);
+    const int cta_workers = c.dtype && !pl.pair ? 2 : 1;
+    pl.ctas = (pl.workers + cta_workers - 1) / cta_workers;
+    pl.workers = pl.ctas * cta_workers;
+    pl.join = each > 1;  // items of one unit are nobody's in part
     pl.part_rows = (int)(mine < (long long)pl.TP * c.G ? mine : (long long)pl.TP * c.G);
     pl.part_rows += pl.part_rows & 1;
     pl.part_off = meta_bytes(pl.tiles * c.n_kv);

@@ -61,10 +61,12 @@ struct SelectArgs {
     int32_t* pages;
 };
 
-// How a tensor-core attention launch is laid out (plan_attn_tile)
+// How an attention launch is laid out
 struct AttnPlan {
     int dev;
-    bool pair;          // two 128-row tiles per item share the copies
+    bool pair;          // bf16: two 128-row tiles per item share the copies
+    int rt;             // fp32: rows of a tile / 16
+    bool join;          // items may be shared between workers
     int TP;             // tokens per row tile
     long long tiles;    // row tiles at most
     int ctas, workers;
@@ -73,8 +75,9 @@ struct AttnPlan {
     size_t scratch;     // bytes in all
 };
 
+AttnPlan plan_attn(const PagedArgs& c, bool listed, int dev, int sms);  // k_paged_tc.cu
+
 // k_paged_tc.cu
-AttnPlan plan_attn_tile(const PagedArgs& c, bool listed, int dev, int sms);
 cudaError_t launch_attn_tile(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
                              cudaStream_t s);
 cudaError_t take_error_paged(unsigned* code, unsigned* info);
@@ -83,6 +86,6 @@ cudaError_t take_error_paged(unsigned* code, unsigned* info);
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
 cudaError_t launch_page_scores(const ScoreArgs& a, cudaStream_t s);
 cudaError_t launch_page_select(const SelectArgs& a, cudaStream_t s);
-cudaError_t launch_attn_plain(const AttnPagedArgs& a, cudaStream_t s);
+cudaError_t launch_attn_f32(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s);
 
 }  // namespace pipo

@@ -123,13 +123,13 @@ pipo_status pool_map(const char* who, CUtensorMap* tm, void* pool, const PagedAr
 
 // Scratch and launch of the attention calls
 pipo_status run_attn(const char* who, const AttnPagedArgs& a, size_t scratch_bytes, cudaStream_t s) {
-    if (!a.c.dtype) return cuda_status(who, launch_attn_plain(a, s));
     int dev = 0, sms = 0;
     const cudaError_t e = device_of(&dev, &sms);
     if (e != cudaSuccess) return cuda_status(who, e);
-    const AttnPlan pl = plan_attn_tile(a.c, a.pages != nullptr, dev, sms);
+    const AttnPlan pl = plan_attn(a.c, a.pages != nullptr, dev, sms);
     if (scratch_bytes < pl.scratch)
         return fail(PIPO_EINVAL, "%s: scratch needs %zu bytes, got %zu", who, pl.scratch, scratch_bytes);
+    if (!a.c.dtype) return cuda_status(who, launch_attn_f32(a, pl, s));
     CUtensorMap tk, tv;
     pipo_status st = pool_map(who, &tk, a.c.k, a.c);
     if (st == PIPO_OK) st = pool_map(who, &tv, a.c.v, a.c);
@@ -177,9 +177,9 @@ pipo_status pipo_op_kv_append(const pipo_paged* c, int32_t n_tokens, int32_t in_
 size_t pipo_op_attn_paged_scratch(const pipo_paged* c, int32_t n_tokens) {
     int dev = 0, sms = 0;
     if (!paged_ok(c, n_tokens) || device_of(&dev, &sms) != cudaSuccess) return 0;
-    if (!c->dtype || c->batch == 0 || n_tokens == 0) return 16;
+    if (c->batch == 0 || n_tokens == 0) return 16;
     const PagedArgs a = args_of(c, n_tokens);
-    return std::max(plan_attn_tile(a, false, dev, sms).scratch, plan_attn_tile(a, true, dev, sms).scratch);
+    return std::max(plan_attn(a, false, dev, sms).scratch, plan_attn(a, true, dev, sms).scratch);
 }
 
 pipo_status pipo_op_attn_paged(const pipo_paged* c, int32_t n_tokens, const void* d_q, int64_t ld_q, float scale,

@@ -314,4 +314,11 @@ __global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, int worke
     }
 }
 
+template <int DH, typename T>
+inline cudaError_t launch_combine(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
+    if (!pl.join) return cudaSuccess;
+    return launch_pdl(&combine_kernel<DH, T>, dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 31) / 32)),
+                      128, 0, s, a, pl.workers, pl.part_rows, pl.part_off);
+}
+
 }  // namespace pipo
