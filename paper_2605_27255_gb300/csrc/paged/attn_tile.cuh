@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         for (int j = 0; j < np && ok; ++j, ++pv, ++n) {
                             const int st = n % SK, buf = pv & 1;
                             // the weights of the page before last lie in the buffer until their values are done
-                            ok = filled(n) && (j < 2 || wait(&o_full[chain][buf], (uint32_t)(((pv - 2) >> 1) & 1), 56, pv));
+                            ok = filled(n) && (pv < 2 || wait(&o_full[chain][buf], (uint32_t)(((pv - 2) >> 1) & 1), 56, pv));
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
@@ -383,34 +383,39 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         ItemWalk it;
         it.start(c, shape, pieces[PAIR ? 0 : w]);
         const uint32_t g_magic = (65536u + (uint32_t)c.G - 1) / (uint32_t)c.G;
+        const int row0 = PAIR ? w * 128 : 0;
+        // the next item with rows for this warpgroup, its queries in shared memory (rows past the last one
+        // are zero).  Every load is in flight before the first is stored (one after the other they
+        // took 19000 cycles).
+        auto queries = [&]() {
+            if (PAIR)
+                while (it.more() && it.tokens(shape) * c.G <= row0) it.next(c, shape);
+            if (!it.more()) return;
+            constexpr int C = DH / 8, RS = 128 / C, NI = 128 / RS;  // 16-byte chunks a row, rows per round, rounds
+            const int ch = wt % C, v0 = wt / C, rows = it.tokens(shape) * c.G - row0;
+            const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + it.tile * shape.TP) * p.ld_q +
+                              (size_t)it.g * c.G * DH + ch * 8;
+            uint4 x[NI];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int v = v0 + i * RS, t = div_g(row0 + v, g_magic);
+                x[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (v < rows) x[i] = *reinterpret_cast<const uint4*>(q + (size_t)t * p.ld_q + (row0 + v - t * c.G) * DH);
+            }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int v = v0 + i * RS;
+                *reinterpret_cast<uint4*>(q_s + w * kTile + (ch >> 3) * kAtHalf + v * 128 + (((ch & 7) ^ (v & 7)) << 4)) = x[i];
+            }
+            fence_proxy_async();  // the generic stores above, before the MMAs read them
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full + w);
+        };
         int sn = 0;  // pages seen
         bool ok = true;
-        for (; it.more() && ok; it.next(c, shape)) {
-            const int rows = min(128, it.tokens(shape) * c.G - (PAIR ? w * 128 : 0));
-            if (rows <= 0) continue;
-            const int row0 = PAIR ? w * 128 : 0, i0 = it.tile * shape.TP;
-            // the queries of this tile; rows past the last one are zero.  Every load is in flight before
-            // the first is stored (one after the other they took 19000 cycles)
-            {
-                constexpr int C = DH / 8, RS = 128 / C, NI = 128 / RS;  // 16-byte chunks a row, rows per round, rounds
-                const int ch = wt % C, v0 = wt / C;
-                const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + i0) * p.ld_q + (size_t)it.g * c.G * DH + ch * 8;
-                uint4 x[NI];
-#pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const int v = v0 + i * RS, t = div_g(row0 + v, g_magic);
-                    x[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (v < rows) x[i] = *reinterpret_cast<const uint4*>(q + (size_t)t * p.ld_q + (row0 + v - t * c.G) * DH);
-                }
-#pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const int v = v0 + i * RS;
-                    *reinterpret_cast<uint4*>(q_s + w * kTile + (ch >> 3) * kAtHalf + v * 128 + (((ch & 7) ^ (v & 7)) << 4)) = x[i];
-                }
-                fence_proxy_async();  // the generic stores above, before the MMAs read them
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full + w);
-            }
+        queries();
+        while (it.more() && ok) {
+            const int rows = min(128, it.tokens(shape) * c.G - row0), i0 = it.tile * shape.TP;
             const bool live = quad * 32 < rows;  // this warp has rows at all
             const int row = row0 + min(r, rows - 1), tr = div_g(row, g_magic), tok = i0 + tr;
             int pos = it.len - it.n + tok, lo = p.window > 0 ? pos - p.window + 1 : 0;
@@ -484,54 +489,49 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 if (lane == 0) mbar_arrive(&p_full[w][sn & 1]);
             }
             if (!ok) break;
+            // where this item's rows go
+            const bool whole = it.whole();
+            bf16_t* out = static_cast<bf16_t*>(p.out) + (size_t)(it.q0 + tok) * p.ld_out + (size_t)(it.g * c.G + row - tr * c.G) * DH;
+            float* part = reinterpret_cast<float*>(p.scratch + part_off) +
+                          ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
+            if (it.kv0 == 0 && row0 + r == 0)
+                reinterpret_cast<ItemMeta*>(p.scratch + kScratchHead)[(size_t)it.index * c.n_kv + it.g] = {
+                    it.q0 + i0, it.tokens(shape) * c.G, me, whole ? me : it.last_worker(pieces[PAIR ? 0 : w])};
+            // the scores of this item are all done: the next one's queries, whose first scores then run
+            // under the values and the output below
+            it.next(c, shape);
+            queries();
             ok = wait(&o_full[w][(sn - 1) & 1], (uint32_t)(((sn - 1) >> 1) & 1), 59, sn);
             if (!ok) break;
             tc_fence_after();
-            if (!live) {
-                // (row 0's warp writes the item's meta)
-            } else if (it.whole()) {
+            if (live) {
                 const float inv = l > 0.f ? 1.0f / l : 0.f;
-                bf16_t* o = static_cast<bf16_t*>(p.out) + (size_t)(it.q0 + tok) * p.ld_out +
-                            (size_t)(it.g * c.G + row - tr * c.G) * DH;
 #pragma unroll
                 for (int h = 0; h < DH / 32; ++h) {
                     uint32_t v[32];
                     tmem_ld32_issue(o_col + 32 * h, v);
                     tmem_ld_wait();
                     pin32(v);
-                    if (r < rows) {
+                    if (r < rows && whole) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
                             uint32_t x[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 x[e] = pack_bf16x2(__uint_as_float(v[i + 2 * e]) * inv, __uint_as_float(v[i + 2 * e + 1]) * inv);
-                            *reinterpret_cast<uint4*>(o + 32 * h + i) = make_uint4(x[0], x[1], x[2], x[3]);
+                            *reinterpret_cast<uint4*>(out + 32 * h + i) = make_uint4(x[0], x[1], x[2], x[3]);
                         }
-                    }
-                }
-            } else {
-                float* part = reinterpret_cast<float*>(p.scratch + part_off) +
-                              ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
-#pragma unroll
-                for (int h = 0; h < DH / 32; ++h) {
-                    uint32_t v[32];
-                    tmem_ld32_issue(o_col + 32 * h, v);
-                    tmem_ld_wait();
-                    pin32(v);
-                    if (r < rows) {
+                    } else if (r < rows) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)  // (four dims of all rows lie side by side)
                             *reinterpret_cast<uint4*>(part + ((size_t)(8 * h + i / 4) * part_rows + row0 + r) * 4) =
                                 make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                     }
+                    __syncwarp();
                 }
-                if (r < rows)
+                if (!whole && r < rows)
                     *reinterpret_cast<float2*>(part + (size_t)part_rows * DH + 2 * (row0 + r)) = make_float2(m_ref, l);
             }
-            if (it.kv0 == 0 && row0 + r == 0)
-                reinterpret_cast<ItemMeta*>(p.scratch + kScratchHead)[(size_t)it.index * c.n_kv + it.g] = {
-                    it.q0 + i0, it.tokens(shape) * c.G, me, it.whole() ? me : it.last_worker(pieces[PAIR ? 0 : w])};
             tc_fence_before();  // the output is read, before the next item's values overwrite it
         }
     }
