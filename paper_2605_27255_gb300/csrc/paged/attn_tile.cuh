@@ -48,7 +48,7 @@
 namespace pipo {
 
 constexpr int kAtThreads = 512;
-constexpr int kAtRegsIo = 56, kAtRegsSoft = 200;
+constexpr int kAtRegsIo = 64, kAtRegsSoft = 192;  // (56 and 200: 387 us for the 2048-token chunk against 374)
 static_assert(2 * kAtRegsIo + 2 * kAtRegsSoft <= 4 * 128, "register shares must fit the launch's registers");
 constexpr int kAtHalf = 128 * 128;      // 64 dims of a query tile: 128 rows of 128 bytes
 constexpr int kPageHalf = kPage * 128;  // 64 dims of a page
@@ -143,7 +143,8 @@ __device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
     for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
 }
 
-template <int DH, bool PAIR>
+// SEL: whole tiles over selected pages (AttnPagedArgs::bits), PAIR only
+template <int DH, bool PAIR, bool SEL>
 __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs p, ItemShape shape, int S,
                                                                   int part_rows, size_t part_off,
                                                                   const __grid_constant__ CUtensorMap tmK,
@@ -425,13 +426,29 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 if (kept > 0) pos = (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage : kPage - 1);
             }
             float m_ref = -INFINITY, l = 0.f;
+            // whole tiles over selected pages: this row's bits, 32 pages at a time
+            const uint32_t* bits =
+                SEL ? p.bits + ((size_t)(it.q0 + tok) * c.n_kv + it.g) * bit_words(c.max_pages) : nullptr;
+            uint32_t word = 0;
             const int np = it.pages();
             for (int j = 0; j < np; ++j, ++sn) {
                 const uint32_t s_buf = s_col + (uint32_t)((sn & 1) * 64);
                 ok = wait(&s_full[w][sn & 1], (uint32_t)((sn >> 1) & 1), 58, sn);
                 if (!ok) break;
                 tc_fence_after();
-                if (live) {
+                bool sel = true;
+                if (SEL) {
+                    const int pg = (it.t0 + it.kv0) * 2 + j;
+                    if (j == 0 || (pg & 31) == 0) word = bits[pg >> 5];
+                    sel = word >> (pg & 31) & 1;
+                }
+                if (SEL && live && !__any_sync(0xffffffffu, sel)) {  // nobody's page: no weight on it
+                    uint32_t none[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) none[i] = 0u;
+                    tmem_st32(s_buf, none);
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                } else if (live) {
                     uint32_t s[2][32];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) tmem_ld32_issue(s_buf + 32 * i, s[i]);
@@ -444,7 +461,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         for (int i = 0; i < kPage; ++i)
                             if (e0 + i > pos || e0 + i < lo) s[i >> 5][i & 31] = 0xff800000u;
                     }
-                    const float top = fmaxf(max32(s[0]), max32(s[1])) * c2;
+                    const float top = SEL && !sel ? -INFINITY : fmaxf(max32(s[0]), max32(s[1])) * c2;
                     // the reference moves when the maximum has passed it by the slack (or it is the first one)
                     const bool move = top > m_ref + kAtSlack;
                     if (__any_sync(0xffffffffu, move)) {
@@ -467,7 +484,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             }
                         }
                     }
-                    const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
+                    // (a page that the row has not selected: exponents of -infinity)
+                    const float neg = SEL && !sel ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
                     // two columns at a time (paired fp32 instructions)
                     const uint64_t c22 = f32x2(c2, c2), neg2 = f32x2(neg, neg);
                     uint64_t sum[2] = {0ull, 0ull};

@@ -54,7 +54,7 @@ cudaError_t f32_as(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         ready = pl.dev;
     }
-    const ItemShape shape{pl.TP, a.window, a.pages ? a.n_top : 0};
+    const ItemShape shape{pl.TP, a.window, pl.listed ? a.n_top : 0};
     const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kAfThreads, af_smem_for(DH, RT, a.c.batch), s, a, shape,
                                      pl.workers, pl.part_rows, pl.part_off);
     return e == cudaSuccess ? launch_combine<DH, float>(a, pl, s) : e;

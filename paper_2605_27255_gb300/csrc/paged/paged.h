@@ -43,6 +43,7 @@ struct AttnPagedArgs {
     int window;             // 0: none
     const int32_t* pages;   // [token][n_kv][n_top] kept pages, ascending, -1 behind the last; nullptr: every page
     int n_top;
+    const uint32_t* bits;   // [token][n_kv][bit_words(max_pages)] the same as bits, for whole tiles, in place of the list; or nullptr
     unsigned char* scratch;
 };
 
@@ -59,7 +60,10 @@ struct SelectArgs {
     const float* scores;
     int n_top, n_sink, n_local;
     int32_t* pages;
+    uint32_t* bits;  // or nullptr
 };
+
+inline __host__ __device__ int bit_words(int max_pages) { return (max_pages + 31) / 32; }
 
 // How an attention launch is laid out
 struct AttnPlan {
@@ -67,15 +71,17 @@ struct AttnPlan {
     bool pair;          // bf16: two 128-row tiles per item share the copies
     int rt;             // fp32: rows of a tile / 16
     bool join;          // items may be shared between workers
+    bool listed;        // selected pages: a token's own list; else whole tiles with bits
     int TP;             // tokens per row tile
     long long tiles;    // row tiles at most
     int ctas, workers;
     int part_rows;      // rows of a partial
     size_t part_off;    // partials in the scratch
+    size_t bits_off;    // selected pages as bits
     size_t scratch;     // bytes in all
 };
 
-AttnPlan plan_attn(const PagedArgs& c, bool listed, int dev, int sms);  // k_paged_tc.cu
+AttnPlan plan_attn(const PagedArgs& c, int n_top, int dev, int sms);  // k_paged_tc.cu
 
 // k_paged_tc.cu
 cudaError_t launch_attn_tile(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,

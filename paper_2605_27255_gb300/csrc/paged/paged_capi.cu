@@ -121,14 +121,19 @@ pipo_status pool_map(const char* who, CUtensorMap* tm, void* pool, const PagedAr
     return r == CUDA_SUCCESS ? PIPO_OK : fail(PIPO_ECUDA, "%s: cuTensorMapEncodeTiled: error %d", who, (int)r);
 }
 
-// Scratch and launch of the attention calls
-pipo_status run_attn(const char* who, const AttnPagedArgs& a, size_t scratch_bytes, cudaStream_t s) {
+// Scratch and launches of the attention calls; sel: the selection that comes first, or nullptr
+pipo_status run_attn(const char* who, AttnPagedArgs a, SelectArgs* sel, size_t scratch_bytes, cudaStream_t s) {
     int dev = 0, sms = 0;
-    const cudaError_t e = device_of(&dev, &sms);
+    cudaError_t e = device_of(&dev, &sms);
     if (e != cudaSuccess) return cuda_status(who, e);
-    const AttnPlan pl = plan_attn(a.c, a.pages != nullptr, dev, sms);
+    const AttnPlan pl = plan_attn(a.c, sel ? sel->n_top : 0, dev, sms);
     if (scratch_bytes < pl.scratch)
         return fail(PIPO_EINVAL, "%s: scratch needs %zu bytes, got %zu", who, pl.scratch, scratch_bytes);
+    if (sel) {
+        if (!pl.listed) a.bits = sel->bits = reinterpret_cast<uint32_t*>(a.scratch + pl.bits_off);
+        e = launch_page_select(*sel, s);
+        if (e != cudaSuccess) return cuda_status(who, e);
+    }
     if (!a.c.dtype) return cuda_status(who, launch_attn_f32(a, pl, s));
     CUtensorMap tk, tv;
     pipo_status st = pool_map(who, &tk, a.c.k, a.c);
@@ -179,7 +184,9 @@ size_t pipo_op_attn_paged_scratch(const pipo_paged* c, int32_t n_tokens) {
     if (!paged_ok(c, n_tokens) || device_of(&dev, &sms) != cudaSuccess) return 0;
     if (c->batch == 0 || n_tokens == 0) return 16;
     const PagedArgs a = args_of(c, n_tokens);
-    return std::max(plan_attn(a, false, dev, sms).scratch, plan_attn(a, true, dev, sms).scratch);
+    // every page (with the selection as bits, where tiles take it), or a token's own list
+    const size_t bits = (size_t)n_tokens * c->n_kv_heads * bit_words(c->max_pages) * 4;
+    return std::max(plan_attn(a, 0, dev, sms).scratch + bits, plan_attn(a, -1, dev, sms).scratch);
 }
 
 pipo_status pipo_op_attn_paged(const pipo_paged* c, int32_t n_tokens, const void* d_q, int64_t ld_q, float scale,
@@ -202,7 +209,7 @@ pipo_status pipo_op_attn_paged(const pipo_paged* c, int32_t n_tokens, const void
     a.scale = scale;
     a.window = window;
     a.scratch = static_cast<unsigned char*>(d_scratch);
-    return run_attn("pipo_op_attn_paged", a, scratch_bytes, static_cast<cudaStream_t>(stream));
+    return run_attn("pipo_op_attn_paged", a, nullptr, scratch_bytes, static_cast<cudaStream_t>(stream));
 }
 
 pipo_status pipo_op_page_scores(const pipo_paged* c, int32_t n_tokens, const void* d_q, int64_t ld_q, float scale,
@@ -243,8 +250,6 @@ pipo_status pipo_op_attn_pages(const pipo_paged* c, int32_t n_tokens, const void
     sel.n_sink = n_sink;
     sel.n_local = n_local;
     sel.pages = d_pages;
-    const cudaError_t e = launch_page_select(sel, static_cast<cudaStream_t>(stream));
-    if (e != cudaSuccess) return cuda_status("pipo_op_attn_pages", e);
     AttnPagedArgs a{};
     a.c = sel.c;
     a.q = d_q;
@@ -255,7 +260,7 @@ pipo_status pipo_op_attn_pages(const pipo_paged* c, int32_t n_tokens, const void
     a.pages = d_pages;
     a.n_top = n_top;
     a.scratch = static_cast<unsigned char*>(d_scratch);
-    return run_attn("pipo_op_attn_pages", a, scratch_bytes, static_cast<cudaStream_t>(stream));
+    return run_attn("pipo_op_attn_pages", a, &sel, scratch_bytes, static_cast<cudaStream_t>(stream));
 }
 
 pipo_status pipo_op_paged_check(uint32_t* h_info) {

@@ -179,6 +179,7 @@ __global__ void __launch_bounds__(128) page_select_kernel(SelectArgs a) {
     if (k.b < 0) return;
     int32_t* o = a.pages + (size_t)w * a.n_top;
     const float* sc = a.scores + (size_t)w * c.max_pages;
+    uint32_t* bits = a.bits ? a.bits + (size_t)w * bit_words(c.max_pages) : nullptr;
     const int seen = k.pos < 0 ? 0 : k.pos / kPage + 1;
     const int head = min(a.n_sink, seen), tail = max(head, seen - a.n_local);  // candidates: [head, tail)
     const int want = min(a.n_top, seen) - (seen - tail + head);                 // of them to be kept
@@ -223,6 +224,7 @@ __global__ void __launch_bounds__(128) page_select_kernel(SelectArgs a) {
         if (keep) o[n + __popc(kept & ((1u << l) - 1u))] = p;
         n += __popc(kept);
         ties -= min(ties, (int)__popc(eq));
+        if (bits && l == 0) bits[p / 32] = kept;
     };
     if (KPL > 0) {
 #pragma unroll
@@ -235,6 +237,8 @@ __global__ void __launch_bounds__(128) page_select_kernel(SelectArgs a) {
         }
     }
     for (int i = n + l; i < a.n_top; i += 32) o[i] = -1;
+    if (bits)
+        for (int i = (seen + 31) / 32 + l; i < bit_words(c.max_pages); i += 32) bits[i] = 0u;
 }
 
 }  // namespace pipo

@@ -64,7 +64,7 @@ def ref_attend(x: Batch, scale, window=0, pages=None):
             j = torch.arange(max(0, pos - window + 1) if window else 0, pos + 1)
             if pages is not None:
                 keep = set(pages[t, g].tolist())
-                j = torch.tensor([e for e in j.tolist() if e // PAGE in keep], dtype=torch.long)
+                j = j[torch.isin(j // PAGE, torch.tensor(sorted(keep)))]
             if len(j) == 0:
                 continue
             kk, vv = x.rows(x.k, b, g, j), x.rows(x.v, b, g, j)

@@ -344,3 +344,23 @@ def test_nothing_to_do_is_a_no_op():
     before = c.k.clone()
     c.append(None, k, k, qs, kl)
     assert torch.equal(c.k.nan_to_num(), before.nan_to_num())
+
+
+@pytest.mark.parametrize("top,sink,local", [(4, 1, 1), (6, 0, 0), (20, 2, 3)])
+@pytest.mark.parametrize("heads", [(8, 2, 64), (32, 8, 128), (7, 1, 128), (16, 16, 64)])
+def test_attend_pages_of_chunks(top, sink, local, heads):
+    """Chunks long enough that whole tiles of tokens read each page once and
+    mask by the selection."""
+    lens, new = [1100, 300, 0, 70, 2200], [200, 300, 0, 1, 140]
+    x = Batch(lens, new, *heads, torch.bfloat16, seed=top)
+    c, qs, kl = cache_of(x)
+    g = torch.Generator().manual_seed(top)
+    sc = torch.randn(x.tokens, heads[1], x.width, generator=g)
+    sc[:, :, 2::5] = 0.5
+    sc[3] = float("-inf")
+    sc[7] = float("nan")
+    out, pages = c.attend_pages(x.q.cuda(), sc.cuda(), qs, kl, top=top, sink=sink, local=local)
+    ref = ref_select(x, sc, top, sink, local)
+    assert torch.equal(pages.cpu(), ref)
+    check(out, ref_attend(x, heads[2] ** -0.5, pages=ref), torch.bfloat16)
+    capi.pipo_op_paged_check()
