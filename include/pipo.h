@@ -411,7 +411,7 @@ PIPO_API pipo_status pipo_op_lm_head_argmax_noalloc(int32_t dtype, const void *d
  *
  * Common to the calls: device pointers, no host synchronisation, nothing
  * allocated, everything enqueued on `stream` (NULL = the legacy default
- * stream) and capturable.  EINVAL for bad shapes, pointers that are NULL or not
+ * stream) and capturable.  At most 2^30 tokens times query heads a call.  EINVAL for bad shapes, pointers that are NULL or not
  * 16-byte aligned (the int arrays: 4), strides below a row or not a
  * multiple of 16 bytes, or a short scratch buffer; batch 0 or n_tokens 0 is
  * a no-op. */
@@ -422,7 +422,7 @@ typedef struct {
     int32_t head_dim;    /* d_h: 64 or 128 */
     int32_t page_size;   /* 64 */
     int32_t n_blocks;    /* blocks of the pools */
-    int32_t max_pages;   /* row length of the table; a sequence holds at most 64 * max_pages entries */
+    int32_t max_pages;   /* row length of the table, at most 2^22 - 64; a sequence holds at most 64 * max_pages entries */
     int32_t batch;       /* sequences, at most 4096 */
     void *k;             /* [n_blocks][n_kv][64][d_h] */
     void *v;             /* [n_blocks][n_kv][64][d_h] */
@@ -451,8 +451,8 @@ PIPO_API pipo_status pipo_op_kv_append(const pipo_paged *c, int32_t n_tokens, in
 /* Causal attention of the new tokens over the cache (their own entries
  * appended before): out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over
  * the entries j <= position, and with window > 0 only j > position - window.
- * d_q at ld_q elements per token, d_out at ld_out, both in the pools' type.
- * scale > 0.  d_scratch: pipo_op_attn_paged_scratch(c, n_tokens) bytes, 16-byte
+ * d_q at ld_q elements per token, d_out at ld_out, both in the pools' type;
+ * d_out overlaps none of the inputs.  scale > 0.  d_scratch: pipo_op_attn_paged_scratch(c, n_tokens) bytes, 16-byte
  * aligned, overwritten; not shared with a call that may overlap. */
 PIPO_API pipo_status pipo_op_attn_paged(const pipo_paged *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
                                         float scale, int32_t window, void *d_out, int64_t ld_out, void *d_scratch,

@@ -41,7 +41,7 @@ bool paged_ok(const pipo_paged* c, int32_t n_tokens) {
            c->n_q_heads % c->n_kv_heads == 0 && c->n_q_heads / c->n_kv_heads <= kPagedMaxGroup &&
            c->n_q_heads <= 65536 && (c->head_dim == 64 || c->head_dim == 128) && c->page_size == kPage &&
            c->n_blocks >= 1 && (long long)c->n_blocks * c->n_kv_heads * kPage <= 0x7fffffffLL && c->max_pages >= 1 &&
-           c->max_pages <= 0x7fffffff / kPage && c->batch >= 0 && c->batch <= kPagedMaxBatch && n_tokens >= 0 &&
+           c->max_pages <= 65535 * kPage && c->batch >= 0 && c->batch <= kPagedMaxBatch && n_tokens >= 0 &&
            (long long)n_tokens * c->n_q_heads <= (1 << 30);
 }
 

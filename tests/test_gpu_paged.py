@@ -364,3 +364,88 @@ def test_attend_pages_of_chunks(top, sink, local, heads):
     assert torch.equal(pages.cpu(), ref)
     check(out, ref_attend(x, heads[2] ** -0.5, pages=ref), torch.bfloat16)
     capi.pipo_op_paged_check()
+
+
+def test_example_serves_requests_together_and_alone():
+    """examples/paged_layer.py: the four operators between the projections.  A
+    request's outputs do not depend on what shares its batch beyond the
+    roundings to bf16 (queries, keys, weights and outputs, 2^-9 of a value
+    each, against sums in another order), and all pages selected are dense
+    attention."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_layer.py")
+    spec = importlib.util.spec_from_file_location("paged_layer", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    layer = ex.Layer()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    inputs = [torch.randn(n, layer.hidden, generator=g, device="cuda") for n in (400, 1, 150)]
+    mixed = ex.serve(layer, inputs)
+    for x, y, every in zip(inputs, mixed, ex.serve(layer, inputs, top=64)):
+        alone = ex.serve(layer, [x])[0]
+        assert torch.isfinite(y).all()
+        assert (y - alone).norm() <= 2e-2 * alone.norm()
+        assert (y - every).norm() <= 2e-2 * alone.norm()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_blocks_past_32_bit_offsets(dtype):
+    """Blocks whose elements lie past 2^31 of the pool."""
+    x = Batch([200, 70, 1], [70, 1, 1], 32, 8, 128, dtype, seed=3)
+    high = 36000 - x.blocks  # 36000 blocks of 8 x 64 x 128 elements: 2.36e9
+    assert high * 8 * 64 * 128 > 2 ** 31
+    pools = []
+    for pool in (x.k, x.v):
+        p = torch.empty(36000, 8, 64, 128, dtype=dtype, device="cuda")
+        p[high:] = pool.cuda()
+        pools.append(p)
+    table = torch.where(x.table < x.blocks, x.table + high, x.table)
+    means = torch.zeros(36000, 8, 128, dtype=dtype, device="cuda")
+    c = paged.PagedCache(*pools, table.cuda(), n_q=32, means=means)
+    qs, kl = x.q_start.cuda(), x.kv_len.cuda()
+    ref = ref_attend(x, 128 ** -0.5)
+    check(c.attend(x.q.cuda(), qs, kl), ref, dtype)
+    out, _ = c.attend_pages(x.q.cuda(), torch.zeros(x.tokens, 8, x.width, device="cuda"), qs, kl, top=x.width)
+    check(out, ref, dtype)
+    k = torch.randn(x.tokens, 8, 128, device="cuda")
+    c.append(None, k, k, qs, kl)
+    for t, b, pos in x.each_token():
+        blk = table[b, pos // PAGE].item()
+        assert torch.equal(c.k[blk, :, pos % PAGE], k[t].to(dtype)) and torch.equal(c.v[blk, :, pos % PAGE], k[t].to(dtype))
+    assert (means[table[1, 1].item()] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_scratch_may_hold_anything(dtype):
+    x = Batch([900, 40, 700, 0], [1, 40, 200, 0], 32, 8, 128, dtype, seed=6)
+    c, qs, kl = cache_of(x)
+    a = c.attend(x.q.cuda(), qs, kl).clone()
+    sc = torch.randn(x.tokens, 8, x.width, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    b = c.attend_pages(x.q.cuda(), sc, qs, kl, top=5)[0].clone()
+    for junk in (0, 255, 1, 127):
+        c._scratch.fill_(junk)
+        assert torch.equal(c.attend(x.q.cuda(), qs, kl), a)
+        c._scratch.fill_(junk)
+        assert torch.equal(c.attend_pages(x.q.cuda(), sc, qs, kl, top=5)[0], b)
+
+
+def test_many_sequences():
+    """More sequences than a block has threads, most of them idle or short."""
+    n = 1500
+    lens = [(b * 37) % 150 for b in range(n)]
+    new = [0 if b % 5 else min(1 + b % 3, max(1, lens[b])) for b in range(n)]
+    for dtype in (torch.bfloat16, torch.float32):
+        x = Batch(lens, new, 4, 2, 64, dtype, seed=1)
+        means = torch.randn(x.blocks, 2, 64, generator=torch.Generator().manual_seed(1)).to(dtype)
+        c, qs, kl = cache_of(x, means.cuda())
+        check(c.attend(x.q.cuda(), qs, kl), ref_attend(x, 0.125), dtype)
+        got, ref = c.page_scores(x.q.cuda(), qs, kl).cpu().double(), ref_scores(x, means, 0.125)
+        fin = torch.isfinite(ref)
+        assert torch.equal(fin, torch.isfinite(got)) and (got[fin] - ref[fin]).abs().max() <= 2e-5 * ref[fin].abs().max()
+        k = torch.randn(x.tokens, 2, 64, device="cuda")
+        c.append(None, k, k, qs, kl)
+        for t, b, pos in x.each_token():
+            if pos >= 0:
+                assert torch.equal(c.k[x.table[b, pos // PAGE].item(), :, pos % PAGE], k[t].to(dtype))
