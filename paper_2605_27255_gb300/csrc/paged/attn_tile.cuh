@@ -411,6 +411,16 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             fence_proxy_async();  // the generic stores above, before the MMAs read them
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full + w);
+            // the item after: its queries on their way into L2
+            ItemWalk nx = it;
+            nx.next(c, shape);
+            if (nx.more() && nx.tokens(shape) * c.G > row0 + wt) {
+                const int t = div_g(row0 + wt, g_magic);
+                const bf16_t* r = static_cast<const bf16_t*>(p.q) + (size_t)(nx.q0 + nx.tile * shape.TP + t) * p.ld_q +
+                                  (size_t)(nx.g * c.G + row0 + wt - t * c.G) * DH;
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(r));
+                if (DH == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(r + 64));
+            }
         };
         int sn = 0;  // pages seen
         bool ok = true;

@@ -4,8 +4,9 @@
 // are cut into row tiles of TP tokens; a row tile with one kv head is an item, and
 // an item is nt units, one per tile of kTileEnt cache entries that its rows
 // see.  The units of all items lie on one line (row tiles in order, within a
-// tile head by head), which S workers (or as many as there are units) cut into equal pieces: worker i takes
-// the units [i W / S, (i + 1) W / S).  So every worker reads the same amount
+// tile head by head), each item's behind kItemCost more that stand for its queries and
+// outputs, and S workers (or as many as the line is long) cut the line into equal pieces: worker
+// i takes what lies in [i W / S, (i + 1) W / S).  So every worker has the same to do
 // whatever the lengths are, a long cache with few rows is split over all of
 // them, and with many rows at most one item at each end of a worker's piece
 // is shared.  Of a shared item each worker leaves the running output, maximum
@@ -18,6 +19,10 @@
 namespace pipo {
 
 constexpr int kTileEnt = 128;  // entries per unit (two pages)
+// What an item costs beside its units, in units: about 6300 cycles from the last page of one to
+// the second of the next in the bf16 kernel, against 3300 for a unit.  (Without it the workers of 16
+// mixed sequences took 75000 to 143000 cycles, by their number of items.)
+constexpr int kItemCost = 2;
 
 // What a launch needs of an item's shape
 struct ItemShape {
@@ -68,9 +73,9 @@ __host__ __device__ inline size_t part_floats(int rows, int dh) { return (size_t
 struct Piece {
     int b, tile, g, kv;  // sequence, row tile in it, head, unit within the item
     int index;           // row tile in the whole batch
-    int units;
-    long long at, total;  // unit on the line, units in all
-    int workers;         // that have units: S, or as many as there are units
+    int left;            // of the line, from that unit on (0: nothing to do)
+    long long end, total;  // end of the piece, length of the line
+    int workers;         // S, or as many as the line is long
 };
 
 // Ints of shared memory that find_pieces uses
@@ -119,7 +124,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
     // (offsets that decrease could count rows twice: never more tiles than the scratch has room for)
     tiles = (int)min((long long)tiles, tiles_bound(c.n_tokens, c.batch, s.TP));
     if (tid == 0) seq_tiles[c.batch] = tiles;
-    if (tid < NW) out[tid].units = 0;
+    if (tid < NW) out[tid].left = 0;
     __syncthreads();
     // this thread's run of row tiles and its units
     const int x0 = (int)((long long)tiles * tid / NT), x1 = (int)((long long)tiles * (tid + 1) / NT);
@@ -138,7 +143,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
     };
     long long mine = 0;
     walk([&](int, int, int, const RowTile& r) {
-        mine += (long long)r.nt * c.n_kv;
+        mine += (long long)(r.nt + kItemCost) * c.n_kv;
         return false;
     });
     long long incl = mine;
@@ -165,13 +170,15 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
         if (u0 >= before && u0 < before + mine) {
             long long at = before;
             walk([&](int b, int j, int x, const RowTile& r) {
-                const long long n = (long long)r.nt * c.n_kv;
+                const int len = r.nt + kItemCost;
+                const long long n = (long long)len * c.n_kv;
                 if (u0 >= at + n) {
                     at += n;
                     return false;
                 }
-                const int off = (int)(u0 - at);
-                out[w] = {b, j, off / r.nt, off % r.nt, x, (int)(u1 - u0), u0, total, Sw};
+                const int g = (int)((u0 - at) / len), off = (int)((u0 - at) % len) - kItemCost;
+                // (a piece that starts before the item's first unit)
+                out[w] = {b, j, g, max(0, off), x, max(0, (int)(u1 - u0) + min(0, off)), u1, total, Sw};
                 return true;
             });
         }
@@ -179,7 +186,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
     __syncthreads();
 }
 
-// the worker that holds unit u
+// the worker that holds place u of the line
 __device__ __forceinline__ int worker_of(long long u, long long total, int S) { return (int)(((u + 1) * S - 1) / total); }
 
 // One worker's items in turn.  Every thread of a role keeps its own; what is only
@@ -195,7 +202,7 @@ struct ItemWalk {
         tile = p.tile;
         g = p.g;
         index = p.index;
-        left = p.units;
+        left = p.left;
         kv0 = p.kv;
         if (left > 0) load(c, s);
     }
@@ -217,9 +224,9 @@ struct ItemWalk {
     __device__ __forceinline__ bool whole() const { return kv0 == 0 && kv1 == nt; }
     __device__ __forceinline__ int tokens(const ItemShape& s) const { return min(s.TP, n - tile * s.TP); }
     __device__ __forceinline__ void next(const PagedArgs& c, const ItemShape& s) {
-        left -= kv1 - kv0;
+        left = max(0, left - (kv1 - kv0) - kItemCost);
         kv0 = 0;
-        if (left <= 0) return;
+        if (left == 0) return;
         if (++g < c.n_kv) {
             kv1 = min(nt, left);
             return;
@@ -237,7 +244,7 @@ struct ItemWalk {
     }
     // the last worker that holds a unit of this item, asked by the one with its first unit
     __device__ __forceinline__ int last_worker(const Piece& p) const {
-        return worker_of(p.at + (p.units - left) + nt - 1, p.total, p.workers);
+        return worker_of(p.end - left + nt - 1, p.total, p.workers);
     }
 };
 

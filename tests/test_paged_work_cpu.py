@@ -34,32 +34,39 @@ def test_pieces_cover_every_unit_once(seed):
         length = r.randint(0, 900)
         n = r.choice([0, 1, min(length, r.randint(0, 300)), length + 2])
         items += [t for t in row_tiles(n, length, TP, window, n_top) for _ in range(n_kv)]
-    total = sum(t[1] for t in items)
+    COST = 2  # places of the line before an item's first unit (kItemCost)
+    line = [(i, u - COST) for i, (_, nt, _) in enumerate(items) for u in range(nt + COST)]
+    total = len(line)
     S = min(r.choice([1, 7, 152, 304]), total)
-    owner = [None] * total
+    owner = {}
     for w in range(S):
         a, b = w * total // S, (w + 1) * total // S
-        assert b > a  # a worker that is named has units
-        for u in range(a, b):
-            assert owner[u] is None
-            owner[u] = w
-            assert ((u + 1) * S - 1) // total == w  # worker_of
-    assert None not in owner
-    at = 0
-    for t0, nt, pages in items:
-        mine = owner[at:at + nt]
+        assert b > a
+        # the walk of one worker (find_pieces and ItemWalk): the item at its start, what is left of its piece
+        i, off = line[a]
+        kv0, left = max(0, off), max(0, b - a + min(0, off))
+        while left > 0:
+            nt = items[i][1]
+            kv1 = min(nt, kv0 + left)
+            if kv0 == 0:  # the record of an item that starts here
+                at = b - left
+                assert line[at] == (i, 0)
+                last = ((at + nt - 1 + 1) * S - 1) // total
+                owner[i, "first"], owner[i, "last"] = w, last
+            for u in range(kv0, kv1):
+                assert (i, u) not in owner
+                owner[i, u] = w
+            left = max(0, left - (kv1 - kv0) - COST)
+            i, kv0 = i + 1, 0
+    for i, (_, nt, pages) in enumerate(items):
+        mine = [owner[i, u] for u in range(nt)]  # every unit has a worker
         assert mine == sorted(mine) and set(mine) == set(range(mine[0], mine[-1] + 1))
+        assert (mine[0], mine[-1]) == (owner[i, "first"], owner[i, "last"])
         assert 2 * nt - 1 <= pages <= 2 * nt
-        # a worker begins at most one item that it does not end, and ends at most one that it did not begin
-        at += nt
-    for w in range(S):
-        a, b = w * total // S, (w + 1) * total // S
-        starts, at = 0, 0
-        for _, nt, _ in items:
-            begins, ends = a <= at < b, a < at + nt <= b
-            starts += begins and not ends
-            at += nt
-        assert starts <= 1
+    for w in range(S):  # a worker leaves at most one part of an item that it began, and one of an item that it did not
+        began = [i for i in range(len(items)) if owner[i, 0] == w and owner[i, items[i][1] - 1] != w]
+        joined = [i for i in range(len(items)) if owner[i, 0] != w and w in {owner[i, u] for u in range(items[i][1])}]
+        assert len(began) <= 1 and len(joined) <= 1
 
 
 def test_rows_to_tokens():
