@@ -6,9 +6,11 @@
 //   S = Q K^T   fp32 in TMEM, Q and K from shared memory (K-major);
 //   softmax     one thread per row: it reads the row's 64 scores, keeps the
 //               running maximum and sum in fp32, and writes exp2 of the scores back over
-//               them as bf16 (the A operand of the next MMAs, from TMEM).  bf16
-//               weights carry 2^-9 of a weight, about the output's own
-//               rounding; their sum is taken before the rounding;
+//               them as bf16 (the A operand of the next MMAs, from TMEM); their sum
+//               is taken before the rounding.  PAIR (below): one part, whose 2^-9 of a
+//               weight is about the output's own rounding (together 1.4 times
+//               its error).  Single: bf16 part and bf16 remainder, since the MMAs have time
+//               under the pages' copies; the output's rounding is then all there is;
 //   O += P V    fp32 in TMEM over the whole item; V is the [entry][dim] tile as it
 //               lies in the cache (MN-major).  The reference that the
 //               exponents are taken against moves only when the running maximum
@@ -150,6 +152,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                                                   const __grid_constant__ CUtensorMap tmK,
                                                                   const __grid_constant__ CUtensorMap tmV) {
     constexpr int kTile = at_q_bytes(DH), kPg = at_page_bytes(DH), NR = PAIR ? 1 : 2;  // NR: pairs of rings
+    constexpr int PARTS = PAIR ? 1 : 2;  // bf16 parts of the weights
     constexpr int SK = at_k_pages(DH, PAIR), SV = at_v_pages(DH, PAIR);
     extern __shared__ __align__(1024) unsigned char at_smem_raw[];
     __shared__ uint32_t tmem_base;
@@ -354,9 +357,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                 uint32_t vb = (uint32_t)dv + (uint32_t)((st * kPg) >> 4);
                                 asm volatile("" : "+r"(vb));
 #pragma unroll
-                                for (int i = 0; i < kPage / 16; ++i)
-                                    umma_bf16_ta(o_at, s_at + buf * 64 + i * 8, u32x2(vb + i * (2048 >> 4), (uint32_t)(dv >> 32)),
-                                                 id_o, i > 0 || j > 0 ? 1u : 0u);
+                                for (int i = 0; i < PARTS * kPage / 16; ++i)  // (the second part lies behind the first)
+                                    umma_bf16_ta(o_at, s_at + buf * 64 + i * 8,
+                                                 u32x2(vb + i % (kPage / 16) * (2048 >> 4), (uint32_t)(dv >> 32)), id_o,
+                                                 i > 0 || j > 0 ? 1u : 0u);
                                 umma_commit(&o_full[chain][buf]);
                                 umma_commit(&v_empty[ring][st]);
                             }
@@ -499,15 +503,17 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     // two columns at a time (paired fp32 instructions)
                     const uint64_t c22 = f32x2(c2, c2), neg2 = f32x2(neg, neg);
                     uint64_t sum[2] = {0ull, 0ull};
-                    uint32_t pk[32];
+                    uint32_t pk[32], pl[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const uint64_t e = fma_f32x2(u32x2(s[i >> 4][2 * (i & 15)], s[i >> 4][2 * (i & 15) + 1]), c22, neg2);
                         const float p0 = ex2(__uint_as_float((uint32_t)e)), p1 = ex2(__uint_as_float((uint32_t)(e >> 32)));
                         sum[i & 1] = add_f32x2(sum[i & 1], f32x2(p0, p1));
                         pk[i] = pack_bf16x2(p0, p1);
+                        if (PARTS == 2) pl[i] = pack_bf16x2(p0 - bf_lo(pk[i]), p1 - bf_hi(pk[i]));
                     }
                     tmem_st32(s_buf, pk);
+                    if (PARTS == 2) tmem_st32(s_buf + 32, pl);
                     sum[0] = add_f32x2(sum[0], sum[1]);
                     l += __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
