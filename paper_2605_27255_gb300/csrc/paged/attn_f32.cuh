@@ -60,8 +60,8 @@ __global__ void __launch_bounds__(kAfThreads, af_ctas(DH, RT)) attn_f32_kernel(A
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     pdl_launch();
     pdl_wait();
-    find_pieces<kAfThreads, 1>(c, shape, (int)blockIdx.x, S, reinterpret_cast<int*>(q_s), &piece,
-                               reinterpret_cast<int*>(p.scratch));
+    find_pieces<kAfThreads, 1>(c, shape, (int)blockIdx.x, S, reinterpret_cast<int*>(q_s), &piece);
+    if (tid == 0) reinterpret_cast<SharedItem*>(p.scratch)[blockIdx.x] = {0, 0, 0, -1};
     const float c2 = p.scale * 1.4426950408889634f;  // exponents of two
     ItemWalk it;
     it.start(c, shape, piece);
@@ -203,9 +203,8 @@ __global__ void __launch_bounds__(kAfThreads, af_ctas(DH, RT)) attn_f32_kernel(A
             if (!whole && tx == 0)
                 *reinterpret_cast<float2*>(part + (size_t)part_rows * DH + 2 * row) = make_float2(m[r] * c2, l[r]);
         }
-        if (it.kv0 == 0 && tid == 0)
-            reinterpret_cast<ItemMeta*>(p.scratch + kScratchHead)[(size_t)it.index * c.n_kv + it.g] = {
-                it.q0 + i0, rows, (int)blockIdx.x, whole ? (int)blockIdx.x : it.last_worker(piece)};
+        if (it.begun() && tid == 0)
+            reinterpret_cast<SharedItem*>(p.scratch)[blockIdx.x] = {it.q0 + i0, rows, it.g, it.last_worker(piece)};
     }
 }
 

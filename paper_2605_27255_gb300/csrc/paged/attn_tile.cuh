@@ -196,8 +196,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
     }
     pdl_wait();  // lengths, queries, entries and the scratch come from the kernels before
     // (the sequences' tile counts use the ring's memory before any copy)
-    find_pieces<kAtThreads, NR>(c, shape, (int)blockIdx.x * NR, S, reinterpret_cast<int*>(ring_s), pieces,
-                                reinterpret_cast<int*>(p.scratch));
+    find_pieces<kAtThreads, NR>(c, shape, (int)blockIdx.x * NR, S, reinterpret_cast<int*>(ring_s), pieces);
     fence_proxy_async();  // those generic accesses, before the copies into the ring
     tc_fence_before();
     __syncthreads();
@@ -426,6 +425,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 if (DH == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(r + 64));
             }
         };
+        if (wt == 0 && row0 == 0) reinterpret_cast<SharedItem*>(p.scratch)[me] = {0, 0, 0, -1};
         int sn = 0;  // pages seen
         bool ok = true;
         queries();
@@ -528,9 +528,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             bf16_t* out = static_cast<bf16_t*>(p.out) + (size_t)(it.q0 + tok) * p.ld_out + (size_t)(it.g * c.G + row - tr * c.G) * DH;
             float* part = reinterpret_cast<float*>(p.scratch + part_off) +
                           ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
-            if (it.kv0 == 0 && row0 + r == 0)
-                reinterpret_cast<ItemMeta*>(p.scratch + kScratchHead)[(size_t)it.index * c.n_kv + it.g] = {
-                    it.q0 + i0, it.tokens(shape) * c.G, me, whole ? me : it.last_worker(pieces[PAIR ? 0 : w])};
+            if (it.begun() && row0 + r == 0)
+                reinterpret_cast<SharedItem*>(p.scratch)[me] = {it.q0 + i0, it.tokens(shape) * c.G, it.g,
+                                                                it.last_worker(pieces[PAIR ? 0 : w])};
             // the scores of this item are all done: the next one's queries, whose first scores then run
             // under the values and the output below
             it.next(c, shape);

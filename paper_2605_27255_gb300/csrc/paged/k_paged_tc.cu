@@ -63,7 +63,7 @@ AttnPlan plan_attn(const PagedArgs& c, int n_top, int dev, int sms) {
     pl.join = each > 1;  // items of one unit are nobody's in part
     pl.part_rows = (int)(mine < (long long)pl.TP * c.G ? mine : (long long)pl.TP * c.G);
     pl.part_rows += pl.part_rows & 1;
-    pl.part_off = meta_bytes(pl.tiles * c.n_kv);
+    pl.part_off = record_bytes(pl.workers);
     pl.bits_off = pl.part_off + (size_t)pl.workers * 2 * part_floats(pl.part_rows, c.dh) * sizeof(float);
     pl.scratch = pl.bits_off;
     if (n_top > 0 && !listed) pl.scratch += (size_t)c.n_tokens * c.n_kv * bit_words(c.max_pages) * 4;

@@ -50,20 +50,18 @@ __device__ __forceinline__ RowTile row_tile(const ItemShape& s, int n, int len, 
 
 __device__ __forceinline__ int seq_new(const PagedArgs& c, int b) { return max(0, q_row(c, b + 1) - q_row(c, b)); }
 
-// scratch header, then one ItemMeta per item, then the partials
-struct alignas(16) ItemMeta {
-    int token, rows;    // first token row, rows
-    int first, last;    // the workers that share it (first == last: nobody)
+// The scratch: one record per worker, then the parts.  A worker leaves at most one
+// item that it has begun for others to go on with, its last one.
+struct alignas(16) SharedItem {
+    int token, rows;   // first token row, rows
+    int g, last;       // kv head; the last worker that shares it (-1: there is no such item)
 };
-constexpr size_t kScratchHead = 16;  // int: number of row tiles
 
 __host__ __device__ inline long long tiles_bound(int n_tokens, int batch, int TP) {
     const long long a = n_tokens, b = n_tokens / TP + (long long)batch;
     return a < b ? a : b;
 }
-__host__ __device__ inline size_t meta_bytes(long long items) {
-    return (kScratchHead + (size_t)items * sizeof(ItemMeta) + 255) / 256 * 256;
-}
+__host__ __device__ inline size_t record_bytes(int workers) { return ((size_t)workers * sizeof(SharedItem) + 255) / 256 * 256; }
 // floats of one partial: [DH / 4][rows][4] outputs (a warp whose lanes are rows writes and
 // reads them side by side), then (maximum, sum) of every row; an even number of rows keeps
 // every partial 16-byte aligned
@@ -72,7 +70,6 @@ __host__ __device__ inline size_t part_floats(int rows, int dh) { return (size_t
 // A worker's piece: where it starts, and how many units it has.
 struct Piece {
     int b, tile, g, kv;  // sequence, row tile in it, head, unit within the item
-    int index;           // row tile in the whole batch
     int left;            // of the line, from that unit on (0: nothing to do)
     long long end, total;  // end of the piece, length of the line
     int workers;         // S, or as many as the line is long
@@ -83,10 +80,9 @@ __host__ __device__ constexpr int find_ints(int batch) { return 3 * batch + 1; }
 
 // All threads of a block (NT of them): the piece of each of its NW workers
 // (w0 .. w0 + NW - 1 of S), written to `out` in shared memory.  tmp: find_ints(batch)
-// ints of shared memory.  Block 0 also leaves the number of row tiles.
+// ints of shared memory.
 template <int NT, int NW>
-__device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape& s, int w0, int S, int* tmp, Piece* out,
-                                            int* n_tiles_out) {
+__device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape& s, int w0, int S, int* tmp, Piece* out) {
     __shared__ long long warp_units[NT / 32];
     __shared__ int warp_tiles[NT / 32];
     int* seq_tiles = tmp;            // [batch + 1] row tiles before every sequence
@@ -134,15 +130,15 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
         if (seq_tiles[m] <= x0) lo = m; else hi = m - 1;
     }
     const int bfirst = lo;
-    auto walk = [&](auto&& fn) {  // fn(b, tile, x, shape) -> stop
+    auto walk = [&](auto&& fn) {  // fn(b, tile, shape) -> stop
         int b = bfirst;
         for (int x = x0; x < x1; ++x) {
             while (x >= seq_tiles[b + 1]) ++b;
-            if (fn(b, x - seq_tiles[b], x, row_tile(s, seq_n[b], seq_l[b], x - seq_tiles[b]))) return;
+            if (fn(b, x - seq_tiles[b], row_tile(s, seq_n[b], seq_l[b], x - seq_tiles[b]))) return;
         }
     };
     long long mine = 0;
-    walk([&](int, int, int, const RowTile& r) {
+    walk([&](int, int, const RowTile& r) {
         mine += (long long)(r.nt + kItemCost) * c.n_kv;
         return false;
     });
@@ -161,7 +157,6 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
         if (w < warp) before += v;
         total += v;
     }
-    if (tid == 0 && n_tiles_out && blockIdx.x == 0) *n_tiles_out = tiles;
     const int Sw = (int)min((long long)S, total);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -169,7 +164,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
         const long long u0 = (long long)(w0 + w) * total / Sw, u1 = (long long)(w0 + w + 1) * total / Sw;
         if (u0 >= before && u0 < before + mine) {
             long long at = before;
-            walk([&](int b, int j, int x, const RowTile& r) {
+            walk([&](int b, int j, const RowTile& r) {
                 const int len = r.nt + kItemCost;
                 const long long n = (long long)len * c.n_kv;
                 if (u0 >= at + n) {
@@ -178,7 +173,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
                 }
                 const int g = (int)((u0 - at) / len), off = (int)((u0 - at) % len) - kItemCost;
                 // (a piece that starts before the item's first unit)
-                out[w] = {b, j, g, max(0, off), x, max(0, (int)(u1 - u0) + min(0, off)), u1, total, Sw};
+                out[w] = {b, j, g, max(0, off), max(0, (int)(u1 - u0) + min(0, off)), u1, total, Sw};
                 return true;
             });
         }
@@ -192,7 +187,7 @@ __device__ __forceinline__ int worker_of(long long u, long long total, int S) { 
 // One worker's items in turn.  Every thread of a role keeps its own; what is only
 // asked of an item that starts here stays in the piece (shared memory).
 struct ItemWalk {
-    int b, tile, g, index, left;
+    int b, tile, g, left;
     // the present item
     int n, len, q0;      // new tokens and entries of the sequence, row of its first new token
     int t0, nt, np;      // first unit, units and pages of the item
@@ -201,7 +196,6 @@ struct ItemWalk {
         b = p.b;
         tile = p.tile;
         g = p.g;
-        index = p.index;
         left = p.left;
         kv0 = p.kv;
         if (left > 0) load(c, s);
@@ -222,6 +216,7 @@ struct ItemWalk {
     __device__ __forceinline__ int pages() const { return min(2 * kv1, np) - 2 * kv0; }  // this worker's
     __device__ __forceinline__ bool more() const { return left > 0; }
     __device__ __forceinline__ bool whole() const { return kv0 == 0 && kv1 == nt; }
+    __device__ __forceinline__ bool begun() const { return kv0 == 0 && kv1 < nt; }  // here, and not finished
     __device__ __forceinline__ int tokens(const ItemShape& s) const { return min(s.TP, n - tile * s.TP); }
     __device__ __forceinline__ void next(const PagedArgs& c, const ItemShape& s) {
         left = max(0, left - (kv1 - kv0) - kItemCost);
@@ -232,7 +227,6 @@ struct ItemWalk {
             return;
         }
         g = 0;
-        ++index;
         if (++tile * s.TP < n) {
             shape(s);
             return;
@@ -248,84 +242,93 @@ struct ItemWalk {
     }
 };
 
-// Joins the parts of the shared items.  grid (items, row groups of 32), 128 threads.
-// out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the workers first .. last in
-// order; the first one's part is its second slot, the others' their first.  A thread takes one
-// row and every (128 / RP)-th group of four dims, RP (4 or 32) rows side by side as they lie in
-// the parts, with eight loads in flight.
+// Joins the parts of the shared items: out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.
+// grid (workers, groups of 32 rows, DH / 16), 128 threads: the item that worker x began and did
+// not finish; its own part is its second slot, those of the workers after it their first.
+// A block takes 16 dims of 32 rows in 4 slices of the parts (a thread: one row, 4 x 4 dims), or
+// of up to 4 rows in 8 slices (4 dims), so that a few parts' loads are all in flight at once; the
+// slices are added up in order.  (One thread for all parts of a row: 12 us of the 59 of
+// four decoding sequences of 15.5 K entries.)
 template <int DH, typename T, int RP>
-__device__ __forceinline__ void combine_rows(const AttnPagedArgs& a, const ItemMeta& m, int g, int row, const float* p0,
-                                             const float* p1, size_t step, int part_rows) {
-    constexpr int NC = DH * RP >= 512 ? DH * RP / 512 : 1, UI = 8 / NC;  // groups of four dims per thread; parts in flight
-    const int n = m.last - m.first;
-    const size_t ml = (size_t)part_rows * DH + 2 * row;
-    const float* x0 = p0 + ((size_t)(threadIdx.x / RP) * part_rows + row) * 4;
-    const float* x1 = p1 + ((size_t)(threadIdx.x / RP) * part_rows + row) * 4;
-    const size_t cs = (size_t)(128 / RP) * part_rows * 4;  // this thread's next group
-    float M = p0[ml];
-#pragma unroll 8
-    for (int i = 1; i <= n; ++i) M = fmaxf(M, p1[2 * i * step + ml]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float o[NC][4] = {}, L = 0.f;
-#pragma unroll UI
-    for (int i = 0; i <= n; ++i) {
-        const float2 e = *reinterpret_cast<const float2*>((i ? p1 + 2 * i * step : p0) + ml);
-        const float* x = i ? x1 + 2 * i * step : x0;
-        float4 v[NC];
+__device__ __forceinline__ void join_rows(const AttnPagedArgs& a, const SharedItem& m, const float* parts, int part_rows,
+                                          float* tmp) {
+    constexpr int PS = RP == 32 ? 4 : 8, NC = RP == 32 ? 4 : 1, V = NC * 4 + 2;  // slices; 4-dim groups; values passed on
+    const int t = threadIdx.x, rl = t % RP, row = blockIdx.y * 32 + rl, cg = RP == 32 ? 0 : t / 4 % 4, ps = t * PS / 128;
+    const int first = blockIdx.x, n = m.last - first + 1, c0 = blockIdx.z * 4 + cg;
+    const size_t step = part_floats(part_rows, DH);
+    float M = -INFINITY, L = 0.f, o[NC][4] = {};
+    if (row < m.rows) {
+#pragma unroll 2
+        for (int i = ps; i < n; i += PS) {
+            const float* p = parts + ((size_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * step;
+            const float2 e = *reinterpret_cast<const float2*>(p + (size_t)part_rows * DH + 2 * row);
+            float4 v[NC];
 #pragma unroll
-        for (int k = 0; k < NC; ++k) v[k] = *reinterpret_cast<const float4*>(x + k * cs);
-        const float f = exp2f(e.x - ref);
-        L = fmaf(f, e.y, L);
+            for (int k = 0; k < NC; ++k) v[k] = *reinterpret_cast<const float4*>(p + ((size_t)(c0 + k) * part_rows + row) * 4);
+            const float top = fmaxf(M, e.x), ref = top == -INFINITY ? 0.f : top, f = exp2f(M - ref), w = exp2f(e.x - ref);
+            M = top;
+            L = L * f + w * e.y;
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            o[k][0] = fmaf(f, v[k].x, o[k][0]);
-            o[k][1] = fmaf(f, v[k].y, o[k][1]);
-            o[k][2] = fmaf(f, v[k].z, o[k][2]);
-            o[k][3] = fmaf(f, v[k].w, o[k][3]);
+            for (int k = 0; k < NC; ++k) {
+                o[k][0] = fmaf(w, v[k].x, o[k][0] * f);
+                o[k][1] = fmaf(w, v[k].y, o[k][1] * f);
+                o[k][2] = fmaf(w, v[k].z, o[k][2] * f);
+                o[k][3] = fmaf(w, v[k].w, o[k][3] * f);
+            }
         }
+    }
+    constexpr int U = 128 / PS;  // threads of a slice
+    if (ps > 0) {
+        float* x = tmp + (size_t)(ps - 1) * U * V + t % U;
+        x[0] = M;
+        x[U] = L;
+#pragma unroll
+        for (int k = 0; k < NC * 4; ++k) x[(2 + k) * U] = o[k / 4][k % 4];
+    }
+    __syncthreads();
+    if (ps > 0 || row >= m.rows) return;
+#pragma unroll
+    for (int q = 0; q < PS - 1; ++q) {
+        const float* x = tmp + (size_t)q * U * V + t;
+        const float mx = x[0], top = fmaxf(M, mx), ref = top == -INFINITY ? 0.f : top, f = exp2f(M - ref), w = exp2f(mx - ref);
+        M = top;
+        L = L * f + w * x[U];
+#pragma unroll
+        for (int k = 0; k < NC * 4; ++k) o[k / 4][k % 4] = fmaf(w, x[(2 + k) * U], o[k / 4][k % 4] * f);
     }
     const float inv = L > 0.f ? 1.0f / L : 0.f;
     const int G = a.c.G, tok = row / G;
-    T* out = static_cast<T*>(a.out) + (size_t)(m.token + tok) * a.ld_out + (size_t)(g * G + row - tok * G) * DH;
+    T* out = static_cast<T*>(a.out) + (size_t)(m.token + tok) * a.ld_out + (size_t)(m.g * G + row - tok * G) * DH + c0 * 4;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[k][e] *= inv;
-        store_f<T, 4>(out + (threadIdx.x / RP + k * (128 / RP)) * 4, o[k]);
+        store_f<T, 4>(out + 4 * k, o[k]);
     }
 }
 
 template <int DH, typename T>
 __global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, int workers, int part_rows, size_t part_off) {
+    __shared__ float tmp[7 * 32 * 18 / 2];  // the larger of 3 x 32 x 18 and 7 x 16 x 6
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int item = blockIdx.x, n_kv = a.c.n_kv;
-    const int tiles = *reinterpret_cast<const int*>(a.scratch);
-    const ItemMeta m = reinterpret_cast<const ItemMeta*>(a.scratch + kScratchHead)[item];
+    const SharedItem m = reinterpret_cast<const SharedItem*>(a.scratch)[blockIdx.x];
     const int left = m.rows - (int)blockIdx.y * 32;
-    if (item / n_kv >= tiles || m.first == m.last || left <= 0) return;
-    // (after a wait that gave up, the scratch may lack items: nothing outside it is read or written)
-    if (m.first < 0 || m.first > m.last || m.last >= workers || m.rows > part_rows || m.token < 0 ||
+    if (m.last <= (int)blockIdx.x || left <= 0) return;
+    // (after a wait that gave up, the scratch may lack records: nothing outside it is read or written)
+    if (m.last >= workers || m.rows > part_rows || m.g < 0 || m.g >= a.c.n_kv || m.token < 0 ||
         m.token + (m.rows - 1) / a.c.G >= a.c.n_tokens)
         return;
     const float* parts = reinterpret_cast<const float*>(a.scratch + part_off);
-    const size_t step = part_floats(part_rows, DH);
-    const float* p0 = parts + ((size_t)m.first * 2 + 1) * step;  // the first worker's part
-    const float* p1 = parts + (size_t)m.first * 2 * step;        // part of worker first + i: p1 + 2 i step
-    const int row = blockIdx.y * 32, g = item % n_kv;
-    if (left > 4) {
-        if ((int)threadIdx.x % 32 < left)
-            combine_rows<DH, T, 32>(a, m, g, row + threadIdx.x % 32, p0, p1, step, part_rows);
-    } else if ((int)threadIdx.x % 4 < left && (DH == 128 || threadIdx.x < 64)) {
-        combine_rows<DH, T, 4>(a, m, g, row + threadIdx.x % 4, p0, p1, step, part_rows);
-    }
+    if (left > 4) join_rows<DH, T, 32>(a, m, parts, part_rows, tmp);
+    else join_rows<DH, T, 4>(a, m, parts, part_rows, tmp);
 }
 
 template <int DH, typename T>
 inline cudaError_t launch_combine(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
     if (!pl.join) return cudaSuccess;
-    return launch_pdl(&combine_kernel<DH, T>, dim3((unsigned)(pl.tiles * a.c.n_kv), (unsigned)((pl.part_rows + 31) / 32)),
-                      128, 0, s, a, pl.workers, pl.part_rows, pl.part_off);
+    return launch_pdl(&combine_kernel<DH, T>, dim3((unsigned)pl.workers, (unsigned)((pl.part_rows + 31) / 32), DH / 16), 128,
+                      0, s, a, pl.workers, pl.part_rows, pl.part_off);
 }
 
 }  // namespace pipo
