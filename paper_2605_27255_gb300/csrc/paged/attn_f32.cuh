@@ -28,7 +28,8 @@ __host__ __device__ constexpr size_t af_smem(int dh, int rt) {
 __host__ __device__ constexpr size_t af_smem_for(int dh, int rt, int batch) {
     return af_smem(dh, rt) > (size_t)find_ints(batch) * 4 ? af_smem(dh, rt) : ((size_t)find_ints(batch) * 4 + 15) / 16 * 16;
 }
-// CTAs of an SM, by shared memory
+// CTAs of an SM, by shared memory (dh 64, rt 4: three with 80 registers and a few spilled, 36.6 us for
+// the windowed fp32 chunks; two without, 41.5)
 __host__ __device__ constexpr int af_ctas(int dh, int rt) {
     return 227 * 1024 / (int)(af_smem(dh, rt) + 2048) < 4 ? 227 * 1024 / (int)(af_smem(dh, rt) + 2048) : 4;
 }

@@ -243,18 +243,20 @@ struct ItemWalk {
 };
 
 // Joins the parts of the shared items: out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.
-// grid (workers, groups of 32 rows, DH / 16), 128 threads: the item that worker x began and did
-// not finish; its own part is its second slot, those of the workers after it their first.
-// A block takes 16 dims of 32 rows in 4 slices of the parts (a thread: one row, 4 x 4 dims), or
-// of up to 4 rows in 8 slices (4 dims), so that a few parts' loads are all in flight at once; the
-// slices are added up in order.  (One thread for all parts of a row: 12 us of the 59 of
-// four decoding sequences of 15.5 K entries.)
+// grid (workers, groups of 32 rows, DH / dims of a block), 128 threads: the item that worker x
+// began and did not finish; its own part is its second slot, those of the workers after it their first.
+// A block takes 32 dims of 32 rows in 2 slices of the parts (a thread: one row, 16 dims; most
+// items of chunks are shared by two), or, where no tile has more than 4 rows, 16 dims in 8
+// slices (a thread: 4 dims), so that a few parts' loads are all in flight at once; the slices are
+// added up in order.  (One thread for all parts of a row: 12 us of the 59 of four decoding
+// sequences of 15.5 K entries.)
 template <int DH, typename T, int RP>
 __device__ __forceinline__ void join_rows(const AttnPagedArgs& a, const SharedItem& m, const float* parts, int part_rows,
                                           float* tmp) {
-    constexpr int PS = RP == 32 ? 4 : 8, NC = RP == 32 ? 4 : 1, V = NC * 4 + 2;  // slices; 4-dim groups; values passed on
-    const int t = threadIdx.x, rl = t % RP, row = blockIdx.y * 32 + rl, cg = RP == 32 ? 0 : t / 4 % 4, ps = t * PS / 128;
-    const int first = blockIdx.x, n = m.last - first + 1, c0 = blockIdx.z * 4 + cg;
+    constexpr int PS = RP == 32 ? 2 : 8, NC = RP == 32 ? 4 : 1, V = NC * 4 + 2;  // slices; 4-dim groups; values passed on
+    constexpr int CG = 128 / (RP * PS);                                          // threads of a row and slice
+    const int t = threadIdx.x, rl = t % RP, row = blockIdx.y * 32 + rl, ps = t * PS / 128;
+    const int first = blockIdx.x, n = m.last - first + 1, c0 = (blockIdx.z * CG + t / RP % CG) * NC;
     const size_t step = part_floats(part_rows, DH);
     float M = -INFINITY, L = 0.f, o[NC][4] = {};
     if (row < m.rows) {
@@ -307,9 +309,9 @@ __device__ __forceinline__ void join_rows(const AttnPagedArgs& a, const SharedIt
     }
 }
 
-template <int DH, typename T>
+template <int DH, typename T, int RP>
 __global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, int workers, int part_rows, size_t part_off) {
-    __shared__ float tmp[7 * 32 * 18 / 2];  // the larger of 3 x 32 x 18 and 7 x 16 x 6
+    __shared__ float tmp[RP == 32 ? 64 * 18 : 7 * 16 * 6];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const SharedItem m = reinterpret_cast<const SharedItem*>(a.scratch)[blockIdx.x];
@@ -320,15 +322,17 @@ __global__ void __launch_bounds__(128) combine_kernel(AttnPagedArgs a, int worke
         m.token + (m.rows - 1) / a.c.G >= a.c.n_tokens)
         return;
     const float* parts = reinterpret_cast<const float*>(a.scratch + part_off);
-    if (left > 4) join_rows<DH, T, 32>(a, m, parts, part_rows, tmp);
-    else join_rows<DH, T, 4>(a, m, parts, part_rows, tmp);
+    join_rows<DH, T, RP>(a, m, parts, part_rows, tmp);
 }
 
 template <int DH, typename T>
 inline cudaError_t launch_combine(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
     if (!pl.join) return cudaSuccess;
-    return launch_pdl(&combine_kernel<DH, T>, dim3((unsigned)pl.workers, (unsigned)((pl.part_rows + 31) / 32), DH / 16), 128,
-                      0, s, a, pl.workers, pl.part_rows, pl.part_off);
+    if (pl.part_rows <= 4)
+        return launch_pdl(&combine_kernel<DH, T, 4>, dim3((unsigned)pl.workers, 1, DH / 16), 128, 0, s, a, pl.workers,
+                          pl.part_rows, pl.part_off);
+    return launch_pdl(&combine_kernel<DH, T, 32>, dim3((unsigned)pl.workers, (unsigned)((pl.part_rows + 31) / 32), DH / 32),
+                      128, 0, s, a, pl.workers, pl.part_rows, pl.part_off);
 }
 
 }  // namespace pipo
