@@ -50,7 +50,7 @@
 namespace pipo {
 
 constexpr int kAtThreads = 512;
-constexpr int kAtRegsIo = 64, kAtRegsSoft = 192;  // (56 and 200: 387 us for the 2048-token chunk against 374)
+constexpr int kAtRegsIo = 72, kAtRegsSoft = 184;  // (56 and 200: 396 us for the 2048-token chunk, these 389)
 static_assert(2 * kAtRegsIo + 2 * kAtRegsSoft <= 4 * 128, "register shares must fit the launch's registers");
 constexpr int kAtHalf = 128 * 128;      // 64 dims of a query tile: 128 rows of 128 bytes
 constexpr int kPageHalf = kPage * 128;  // 64 dims of a page
