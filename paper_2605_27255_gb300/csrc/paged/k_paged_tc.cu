@@ -31,7 +31,7 @@ cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMa
 // tile of tokens reads each page once for all of them and masks by bits, every page of
 // the cache in the worst case.  Whole tiles, where they never read more: when the tokens of a
 // sequence (on average, a tile's at most) times n_top reach max_pages.  (bf16, 512 tokens with 16 of
-// 249 pages each: 279 us by lists, see the table for tiles.)
+// 249 pages each: 279 us by lists, 143 by tiles at that time.)
 AttnPlan plan_attn(const PagedArgs& c, int n_top, int dev, int sms) {
     AttnPlan pl{};
     pl.dev = dev;

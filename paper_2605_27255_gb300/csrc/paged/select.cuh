@@ -7,7 +7,8 @@ namespace pipo {
 
 // scores[t][g][p] = scale * sum_h q[t, h] . mean[p], all in fp32: the queries of a kv head are
 // added up first, then one product per page.  Bound by the means read and the scores written;
-// the products are far below the CUDA cores' rate.
+// the products are far below the CUDA cores' rate.  Measured (8 kv heads of 128): four tokens over 243
+// pages 8 us, 512 tokens over 256 pages 16 us, both by latency.
 constexpr int kScorePages = 64;  // pages per CTA
 
 // One token per CTA row (decoding): DH / 16 lanes hold 16 dims each of a page, a warp 512 / DH pages.
