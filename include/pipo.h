@@ -407,7 +407,8 @@ PIPO_API pipo_status pipo_op_lm_head_argmax_noalloc(int32_t dtype, const void *d
  * table entries of pages below kv_len are read; a block outside [0, n_blocks)
  * is not followed (an append skips it, a read takes block 0 or n_blocks - 1).
  * Cache slots at and past kv_len may hold anything, also NaN; those below it
- * must be finite.
+ * must be finite, but for attention with a window those that it has passed for
+ * every new token of the sequence (their pages and table entries may be gone).
  *
  * Common to the calls: device pointers, no host synchronisation, nothing
  * allocated, everything enqueued on `stream` (NULL = the legacy default

@@ -274,15 +274,18 @@ __global__ void __launch_bounds__(kAfThreads, af_ctas(DH, RT)) attn_f32_kernel(A
             const int pos = it.len - it.n + it.tile, kept = pos < 0 ? 0 : min(shape.n_top, pos / kPage + 1);
             end = kept == 0 ? 0 : (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage + 1 : kPage);
         }
-        // page j of this piece into shared memory; what lies past the end becomes zero
+        const int first = first_seen(shape, it.n, it.len, it.tile);
+        // page j of this piece into shared memory; what no row sees before the window or past the end becomes zero
         auto copy = [&](float* dst, int ld, const void* pool, int j) {
-            const int pg = pg0 + j, live = min(kPage, end - pg * kPage);
-            const int q = live > 0 ? (list ? list[pg] : pg) : 0;
-            const float* src = static_cast<const float*>(pool) + (live > 0 ? block_off(c, page_block(c, it.b, q), it.g) : 0);
+            const int pg = pg0 + j, dead = first - pg * kPage, live = min(kPage, end - pg * kPage);  // rows [dead, live)
+            const bool any = live > max(0, dead);
+            const int q = any && list ? list[pg] : pg;
+            const float* src = static_cast<const float*>(pool) + (any ? block_off(c, page_block(c, it.b, q), it.g) : 0);
 #pragma unroll
             for (int i = 0; i < kPage * DH / 4 / kAfThreads; ++i) {
                 const int x = tid + i * kAfThreads, r = x / (DH / 4), d = x % (DH / 4) * 4;
-                cp_async16(dst + r * ld + d, src + (r < live ? r * DH + d : 0), r < live);
+                const bool take = r < live && r >= dead;
+                cp_async16(dst + r * ld + d, src + (take ? r * DH + d : 0), take);
             }
             cp_async_commit();
         };

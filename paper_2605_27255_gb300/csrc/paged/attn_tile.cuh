@@ -234,6 +234,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     const int32_t* list =
                         shape.n_top > 0 ? p.pages + ((size_t)(it.q0 + it.tile) * c.n_kv + it.g) * shape.n_top : nullptr;
                     const int np = it.pages(), pg0 = (it.t0 + it.kv0) * 2;  // first page in the cache or the list
+                    const int gone = first_seen(shape, it.n, it.len, it.tile) / kPage;  // pages that no row sees
                     int held = -32, mine = -1;  // lane l holds the block of page held + l
                     int prev = -1;              // block of the page whose values come next
                     for (int j = 0; j <= np; ++j) {
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                     const int q = i < shape.n_top ? list[i] : -1;
                                     mine = q >= 0 ? page_block(c, it.b, q) : -1;
                                 } else {
-                                    mine = j + lane < np && i * kPage < it.len ? page_block(c, it.b, i) : -1;
+                                    mine = j + lane < np && i * kPage < it.len && i >= gone ? page_block(c, it.b, i) : -1;
                                 }
                             }
                             blk = __shfl_sync(0xffffffffu, mine, j - held);
@@ -331,7 +332,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     } else {
                         constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
                         const uint64_t dv = umma_desc_mn_page(smem_u32(v_s));
-                        // entries whose values may be anything: those past the sequence's (or the list's) end
+                        // entries whose values may be anything: those before the window and past the
+                        // sequence's (or the list's) end
+                        const int first = first_seen(shape, it.n, it.len, it.tile);
                         int end = it.len;
                         if (shape.n_top > 0) {
                             const int pos = it.len - it.n + it.tile;
@@ -343,11 +346,13 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             const int st = n % SV, buf = pv & 1;
                             ok = filled(n);
                             if (!ok) break;
-                            const int tail = end - (it.t0 + it.kv0) * kTileEnt - j * kPage;
-                            if (tail < kPage) {  // (PAIR: both pipelines clear the same rows before their own MMAs)
-                                const int r0 = max(0, tail);
-                                for (int i = lane; i < (kPage - r0) * (DH / 8); i += 32) {
-                                    const int r = r0 + i / (DH / 8), ch = i % (DH / 8);
+                            const int at = (it.t0 + it.kv0) * kTileEnt + j * kPage, head = min(kPage, first - at), tail = end - at;
+                            if (head > 0 || tail < kPage) {  // (PAIR: both pipelines clear the same rows before their own MMAs)
+                                const int a = max(0, head), z = min(kPage - a, kPage - max(0, tail));  // rows before, rows past
+                                for (int i = lane; i < (a + max(0, z)) * (DH / 8); i += 32) {
+                                    int r = i / (DH / 8);
+                                    const int ch = i % (DH / 8);
+                                    r = r < a ? r : kPage - 1 - (r - a);
                                     *reinterpret_cast<uint4*>(v_s + st * kPg + (ch >> 3) * kPageHalf + r * 128 + (ch & 7) * 16) =
                                         make_uint4(0u, 0u, 0u, 0u);
                                 }

@@ -36,14 +36,19 @@ struct RowTile {
     int t0, nt;     // first unit (in kTileEnt entries from the start of the cache or of the list), units
     int np;         // pages of them: 2 nt, or one less
 };
+// The first entry that any row of it sees.  Those before may hold anything (pages that the window
+// has passed may be gone): they are not read, or their values are cleared.
+__device__ __forceinline__ int first_seen(const ItemShape& s, int n, int len, int j) {
+    return s.window > 0 ? max(0, len - n + j * s.TP - s.window + 1) : 0;
+}
 __device__ __forceinline__ RowTile row_tile(const ItemShape& s, int n, int len, int j) {
     const int i0 = j * s.TP, i1 = min(n, i0 + s.TP);
-    const int first = len - n + i0, last = len - n + i1 - 1;
+    const int last = len - n + i1 - 1;
     if (s.n_top > 0) {
         const int kept = last < 0 ? 0 : min(s.n_top, last / kPage + 1);
         return {0, max(1, (kept + 1) / 2), max(1, kept)};
     }
-    const int hi = max(0, last + 1), lo = s.window > 0 ? min(hi, max(0, first - s.window + 1)) : 0;
+    const int hi = max(0, last + 1), lo = min(hi, first_seen(s, n, len, j));
     const int t0 = lo / kTileEnt, np = max(1, (hi + kPage - 1) / kPage - 2 * t0);
     return {t0, (np + 1) / 2, np};
 }

@@ -142,8 +142,9 @@ class PagedCache:
     def attend(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of the new tokens over the cache; ``window`` > 0
-        keeps the last ``window`` entries of every token.  scale: 1/sqrt(d_h)
-        unless given."""
+        keeps the last ``window`` entries of every token, and pages that it has
+        passed for all new tokens of a sequence are not needed (their blocks
+        and table entries may hold anything).  scale: 1/sqrt(d_h) unless given."""
         self._batch(q_start, kv_len)
         ld_q = self._rows(q, self.n_q, "q", self.dtype)
         out, ld_out = self._out(q, out)

@@ -122,6 +122,27 @@ def test_attend_strided_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d_h", [64, 128])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [7, 1, 130, 40], [200, 300, 5, 333]])
+@pytest.mark.parametrize("window", [1, 50, 64, 200])
+def test_attend_window_over_pages_that_are_gone(dtype, d_h, new, window):
+    """What the window has passed for all of a sequence's new tokens may be NaN,
+    and the table may hold anything for its pages."""
+    x = Batch([700, 333, 192, 1025], new, 8, 2, d_h, dtype, seed=13)
+    ref = ref_attend(x, d_h ** -0.5, window)
+    for b in range(4):
+        first = x.lens[b] - new[b] - window + 1
+        for p in range(-(-x.lens[b] // PAGE)):
+            gone = min(PAGE, max(0, first - p * PAGE))
+            x.k[x.table[b, p].item(), :, :gone] = float("nan")
+            x.v[x.table[b, p].item(), :, :gone] = float("nan")
+            if gone == PAGE:
+                x.table[b, p] = -5 if p & 1 else 1 << 30
+    c, qs, kl = cache_of(x)
+    check(c.attend(x.q.cuda(), qs, kl, window=window), ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_attend_sharp_and_flat_scores(dtype):
     """Scores of a hundred and more (one entry takes all the weight) and all equal."""
     x = Batch([500], [3], 4, 2, 64, dtype, seed=1)
