@@ -37,7 +37,7 @@
 // outputs.  Scores and values have issuing warps of their own because a warp's next
 // wait is held until its MMAs have left the queue (about 250 cycles each: 440 us
 // for the 2048-token chunk with one warp for both).  Cache slots past a
-// sequence's end may hold anything: their scores are masked, and the value warp
+// sequence's end or before its window may hold anything: their scores are masked, and the value warp
 // clears their values in shared memory (0 times NaN would be NaN).
 //
 // Bound and measured (32 query and 8 kv heads of 128): 2048 tokens behind 14336 entries, 388 us,
