@@ -19,7 +19,7 @@ everything else by the library (``capi.PipoError``).
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple
+from typing import Dict, Optional, Tuple
 
 import torch
 
@@ -42,9 +42,10 @@ class PagedCache:
     """Pools ``k``, ``v`` [n_blocks, n_kv, 64, d_h] (bf16 or fp32), the block
     table [batch, max_pages] (int32) and, for the page scores, the mean keys
     ``means`` [n_blocks, n_kv, d_h] that ``append`` maintains.  The tensors stay
-    the caller's; nothing is copied.  ``attend`` and ``attend_pages`` keep one
-    scratch buffer per object, so calls of one object that may overlap on the
-    device (other streams) need objects of their own."""
+    the caller's; nothing is copied.  ``attend`` and ``attend_pages`` keep a
+    scratch buffer per stream; a call that ``torch.cuda.graph`` captures takes
+    one from the graph's own pool instead, which lasts as long as the graph, so that
+    later calls, whatever their size, leave its replays alone."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_q: int,
                  means: Optional[torch.Tensor] = None):
@@ -65,8 +66,8 @@ class PagedCache:
                                   table.shape[0], k.data_ptr(), v.data_ptr(),
                                   None if means is None else means.data_ptr(), table.data_ptr())
         self._seqs = table.shape[0]
-        self._scratch: Optional[torch.Tensor] = None
-        self._scratch_for = -1
+        self._buffers: Dict[int, torch.Tensor] = {}  # scratch by stream
+        self._need, self._need_for = 0, -1           # scratch bytes of the last token count
 
     # ---- arguments
 
@@ -86,13 +87,25 @@ class PagedCache:
             raise ValueError(f"{name} must be [tokens, {heads}, {self.d_h}] {dtype} with whole rows")
         return stride[0] if shape[0] > 1 else heads * self.d_h
 
-    def _work(self, tokens: int) -> torch.Tensor:
-        if self._scratch_for != tokens:
-            need = capi.pipo_op_attn_paged_scratch(self._c, tokens)
-            if self._scratch is None or self._scratch.numel() < need:
-                self._scratch = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
-            self._scratch_for = tokens
-        return self._scratch
+    def _work(self, tokens: int, stream: int) -> torch.Tensor:
+        """Scratch of a call on the current stream (``stream``).  A buffer is allocated on
+        the stream that uses it: an outgrown one goes back behind that stream's work.  Under a
+        capture it is new: the graph's pool keeps it for the replays, and calls of
+        one capture take the same memory in turn."""
+        if self._need_for != tokens:
+            self._need = max(capi.pipo_op_attn_paged_scratch(self._c, tokens), 16)
+            self._need_for = tokens
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(self._need, dtype=torch.uint8, device=self.device)
+        buf = self._buffers.get(stream)
+        if buf is None or buf.numel() < self._need:
+            buf = self._buffers[stream] = torch.empty(self._need, dtype=torch.uint8, device=self.device)
+        return buf
+
+    @property
+    def _scratch(self) -> Optional[torch.Tensor]:
+        """The current stream's buffer, if it has one."""
+        return self._buffers.get(_raw_stream(self.index))
 
     # ---- the calls
 
@@ -148,10 +161,10 @@ class PagedCache:
         self._batch(q_start, kv_len)
         ld_q = self._rows(q, self.n_q, "q", self.dtype)
         out, ld_out = self._out(q, out)
-        w = self._work(q.shape[0])
+        stream = _raw_stream(self.index)
+        w = self._work(q.shape[0], stream)
         capi.pipo_op_attn_paged(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
-                                window, out.data_ptr(), ld_out, w.data_ptr(), w.numel(),
-                                _raw_stream(self.index))
+                                window, out.data_ptr(), ld_out, w.data_ptr(), w.numel(), stream)
         return out
 
     def page_scores(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
@@ -184,8 +197,9 @@ class PagedCache:
             raise ValueError("scores must be a contiguous float32 [tokens, n_kv, max_pages]")
         out, ld_out = self._out(q, out)
         pages = torch.empty((q.shape[0], self.n_kv, top), dtype=torch.int32, device=self.device)
-        w = self._work(q.shape[0])
+        stream = _raw_stream(self.index)
+        w = self._work(q.shape[0], stream)
         capi.pipo_op_attn_pages(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
                                 scores.data_ptr(), top, sink, local, out.data_ptr(), ld_out, pages.data_ptr(),
-                                w.data_ptr(), w.numel(), _raw_stream(self.index))
+                                w.data_ptr(), w.numel(), stream)
         return out, pages

@@ -470,3 +470,28 @@ def test_many_sequences():
         for t, b, pos in x.each_token():
             if pos >= 0:
                 assert torch.equal(c.k[x.table[b, pos // PAGE].item(), :, pos % PAGE], k[t].to(dtype))
+
+
+def test_a_graph_keeps_its_scratch_beside_larger_calls():
+    """A captured decode step is replayed after a long chunk has gone through the same object:
+    its replays write nothing that other tensors own by then, and their outputs stay right."""
+    x = Batch([5000, 130], [1, 1], 32, 8, 128, torch.bfloat16, seed=4)
+    c, qs, kl = cache_of(x)
+    q, ref = x.q.cuda(), ref_attend(x, 128 ** -0.5)
+    sc = torch.zeros(2, 8, x.width, device="cuda")
+    c.attend(q, qs, kl)
+    g, out = torch.cuda.CUDAGraph(), torch.zeros_like(q)
+    with torch.cuda.graph(g):
+        c.attend(q, qs, kl, out=out)
+        some = c.attend_pages(q, sc, qs, kl, top=x.width)[0]
+    chunk = Batch([5000, 130], [2000, 100], 32, 8, 128, torch.bfloat16, seed=4)
+    c.attend(chunk.q.cuda(), chunk.q_start.cuda(), kl)
+    other = [torch.full((n << 20,), 7, dtype=torch.uint8, device="cuda") for n in (1, 2, 4, 8, 16, 32, 64)]
+    for _ in range(3):
+        out.zero_()
+        g.replay()
+        c.attend(chunk.q.cuda(), chunk.q_start.cuda(), kl)
+        torch.cuda.synchronize()
+        check(out, ref, torch.bfloat16)
+        check(some, ref, torch.bfloat16)
+    assert all((t == 7).all() for t in other)
