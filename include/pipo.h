@@ -412,7 +412,9 @@ PIPO_API pipo_status pipo_op_lm_head_argmax_noalloc(int32_t dtype, const void *d
  *
  * Common to the calls: device pointers, no host synchronisation, nothing
  * allocated, everything enqueued on `stream` (NULL = the legacy default
- * stream) and capturable.  At most 2^30 tokens times query heads a call.  EINVAL for bad shapes, pointers that are NULL or not
+ * stream) and capturable.  They run on the calling thread's current device, to
+ * which the pointers and the stream have to belong.  At most 2^30 tokens times
+ * query heads a call.  EINVAL for bad shapes, pointers that are NULL or not
  * 16-byte aligned (the int arrays: 4), strides below a row or not a
  * multiple of 16 bytes, or a short scratch buffer; batch 0 or n_tokens 0 is
  * a no-op. */

@@ -1,7 +1,7 @@
 """The paged-cache operators of ``include/pipo.h`` on torch tensors.
 
 ``PagedCache`` describes pools and a block table that the caller owns and
-makes the four calls of an attention layer on the current CUDA stream:
+makes the four calls of an attention layer on its device's current CUDA stream:
 
     cache = PagedCache(k_pool, v_pool, table, n_q=32, means=means)
     q = cache.append(q, k, v, q_start, kv_len, q_gain=..., k_gain=..., rope=...)
@@ -19,6 +19,7 @@ everything else by the library (``capi.PipoError``).
 """
 from __future__ import annotations
 
+import functools
 from typing import Dict, Optional, Tuple
 
 import torch
@@ -27,6 +28,7 @@ from . import capi
 
 PAGE = 64
 _raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's handle, without a Stream object
+_current_device = torch._C._cuda_getDevice
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -36,6 +38,17 @@ def rope_table(n: int, d_h: int, theta: float, device="cuda") -> torch.Tensor:
     i = torch.arange(0, d_h, 2, device=device, dtype=torch.float64)
     a = torch.arange(n, device=device, dtype=torch.float64)[:, None] * theta ** (-i / d_h)
     return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+
+
+def _on_pools_device(method):
+    """The library plans and launches on the thread's current device: make that the pools'."""
+    @functools.wraps(method)
+    def call(self, *args, **kw):
+        if _current_device() == self.index:
+            return method(self, *args, **kw)
+        with torch.cuda.device(self.index):
+            return method(self, *args, **kw)
+    return call
 
 
 class PagedCache:
@@ -109,6 +122,7 @@ class PagedCache:
 
     # ---- the calls
 
+    @_on_pools_device
     def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor,
                kv_len: torch.Tensor, *, q_gain: Optional[torch.Tensor] = None,
                k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, rope: Optional[torch.Tensor] = None,
@@ -152,6 +166,7 @@ class PagedCache:
             raise ValueError("out must have a row for every token")
         return out, self._rows(out, self.n_q, "out", self.dtype)
 
+    @_on_pools_device
     def attend(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of the new tokens over the cache; ``window`` > 0
@@ -167,6 +182,7 @@ class PagedCache:
                                 window, out.data_ptr(), ld_out, w.data_ptr(), w.numel(), stream)
         return out
 
+    @_on_pools_device
     def page_scores(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """fp32 [tokens, n_kv, max_pages]: the score of every page a token sees,
@@ -184,6 +200,7 @@ class PagedCache:
                                  out.data_ptr(), _raw_stream(self.index))
         return out
 
+    @_on_pools_device
     def attend_pages(self, q: torch.Tensor, scores: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                      top: int, sink: int = 1, local: int = 1, scale: Optional[float] = None,
                      out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -14,6 +14,8 @@ class Host:
 
     def __init__(self):
         self.stream, self.capturing = 0, False
+        self.device = None   # the thread's current device (that of CPU tensors)
+        self.calls = []      # (library call, current device)
         self.scratch = []    # (address, bytes) of every attention call
         self.allocated = {}  # address of a new tensor -> (stream, capturing) at its allocation
         self.kept = []       # those tensors: an address stays one tensor's
@@ -25,7 +27,31 @@ def host(monkeypatch):
     monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True), raising=False)
     monkeypatch.setattr(paged, "_raw_stream", lambda index: h.stream)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: h.capturing)
-    monkeypatch.setattr(capi, "pipo_op_attn_paged_scratch", lambda c, tokens: 1000 * tokens)
+    monkeypatch.setattr(paged, "_current_device", lambda: h.device, raising=False)
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.outer, h.device = h.device, self.index
+
+        def __exit__(self, *a):
+            h.device = self.outer
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+
+    def stands_in(name, fn):
+        def call(*a):
+            h.calls.append((name, h.device))
+            return fn(*a)
+        monkeypatch.setattr(capi, name, call)
+
+    stands_in("pipo_op_attn_paged_scratch", lambda c, tokens: 1000 * tokens)
+    stands_in("pipo_op_attn_paged", lambda *a: h.scratch.append(a[8:10]))
+    stands_in("pipo_op_attn_pages", lambda *a: h.scratch.append(a[12:14]))
+    stands_in("pipo_op_kv_append", lambda *a: None)
+    stands_in("pipo_op_page_scores", lambda *a: None)
 
     def empty(*args, **kw):
         t = torch.zeros(*args, **kw)
@@ -36,18 +62,42 @@ def host(monkeypatch):
     stand_in = types.SimpleNamespace(**{k: getattr(torch, k) for k in dir(torch) if not k.startswith("__")})
     stand_in.empty = empty
     monkeypatch.setattr(paged, "torch", stand_in)
-    monkeypatch.setattr(capi, "pipo_op_attn_paged", lambda *a: h.scratch.append(a[8:10]))
     return h
 
 
 def cache(batch=2, pages=3, n_q=4, n_kv=2, d_h=64):
     pool = lambda: torch.zeros(batch * pages, n_kv, paged.PAGE, d_h)  # noqa: E731
-    return paged.PagedCache(pool(), pool(), torch.zeros(batch, pages, dtype=torch.int32), n_q=n_q)
+    return paged.PagedCache(pool(), pool(), torch.zeros(batch, pages, dtype=torch.int32), n_q=n_q,
+                            means=torch.zeros(batch * pages, n_kv, d_h))
+
+
+def batch_of(c, tokens):
+    """Queries, q_start and kv_len."""
+    n = c.table.shape[0]
+    return (torch.zeros(tokens, c.n_q, c.d_h), torch.tensor([0] + [tokens] * n, dtype=torch.int32),
+            torch.zeros(n, dtype=torch.int32))
 
 
 def attend(c, tokens, **kw):
-    q_start = torch.tensor([0] + [tokens] * c.table.shape[0], dtype=torch.int32)
-    return c.attend(torch.zeros(tokens, c.n_q, c.d_h), q_start, torch.zeros(c.table.shape[0], dtype=torch.int32), **kw)
+    return c.attend(*batch_of(c, tokens), **kw)
+
+
+def append(c, tokens, **kw):
+    q, qs, kl = batch_of(c, tokens)
+    k = torch.zeros(tokens, c.n_kv, c.d_h)
+    return c.append(q, k, k, qs, kl, **kw)
+
+
+def page_scores(c, tokens, **kw):
+    return c.page_scores(*batch_of(c, tokens), **kw)
+
+
+def attend_pages(c, tokens, top=2, **kw):
+    q, qs, kl = batch_of(c, tokens)
+    return c.attend_pages(q, torch.zeros(tokens, c.n_kv, c.table.shape[1]), qs, kl, top=top, **kw)
+
+
+CALLS = [append, attend, page_scores, attend_pages]
 
 
 def test_a_captured_call_has_scratch_of_the_capture(host):
@@ -78,3 +128,19 @@ def test_scratch_belongs_to_the_stream_that_uses_it(host):
         assert size >= 1000 * tokens and host.allocated[address] == (stream, False)
     # the calls of a stream share a buffer while it is large enough
     assert host.scratch[0] == host.scratch[2] and host.scratch[4] == host.scratch[5]
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_calls_run_on_the_pools_device(host, call):
+    """The library launches on the thread's current device, whichever that is; pools on
+    another one make it theirs for the call."""
+    c = cache()
+    c.index = 1
+    host.device = 0
+    call(c, 3)
+    assert host.device == 0
+    assert host.calls and all(device == 1 for _, device in host.calls), host.calls
+    host.calls.clear()
+    host.device = 1
+    call(c, 5)
+    assert host.calls and all(device == 1 for _, device in host.calls)
