@@ -20,6 +20,7 @@ everything else by the library (``capi.PipoError``).
 from __future__ import annotations
 
 import functools
+import threading
 from typing import Dict, Optional, Tuple
 
 import torch
@@ -40,14 +41,17 @@ def rope_table(n: int, d_h: int, theta: float, device="cuda") -> torch.Tensor:
     return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
 
 
-def _on_pools_device(method):
-    """The library plans and launches on the thread's current device: make that the pools'."""
+def _library_call(method):
+    """The library plans and launches on the thread's current device: make that the pools'.  And
+    it reads the object's description of the batch without the interpreter lock: one call of
+    an object at a time."""
     @functools.wraps(method)
     def call(self, *args, **kw):
-        if _current_device() == self.index:
-            return method(self, *args, **kw)
-        with torch.cuda.device(self.index):
-            return method(self, *args, **kw)
+        with self._lock:
+            if _current_device() == self.index:
+                return method(self, *args, **kw)
+            with torch.cuda.device(self.index):
+                return method(self, *args, **kw)
     return call
 
 
@@ -58,7 +62,8 @@ class PagedCache:
     the caller's; nothing is copied.  ``attend`` and ``attend_pages`` keep a
     scratch buffer per stream; a call that ``torch.cuda.graph`` captures takes
     one from the graph's own pool instead, which lasts as long as the graph, so that
-    later calls, whatever their size, leave its replays alone."""
+    later calls, whatever their size, leave its replays alone.  Threads may
+    share an object."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_q: int,
                  means: Optional[torch.Tensor] = None):
@@ -79,6 +84,7 @@ class PagedCache:
                                   table.shape[0], k.data_ptr(), v.data_ptr(),
                                   None if means is None else means.data_ptr(), table.data_ptr())
         self._seqs = table.shape[0]
+        self._lock = threading.Lock()
         self._buffers: Dict[int, torch.Tensor] = {}  # scratch by stream
         self._need, self._need_for = 0, -1           # scratch bytes of the last token count
 
@@ -122,7 +128,7 @@ class PagedCache:
 
     # ---- the calls
 
-    @_on_pools_device
+    @_library_call
     def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor,
                kv_len: torch.Tensor, *, q_gain: Optional[torch.Tensor] = None,
                k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, rope: Optional[torch.Tensor] = None,
@@ -166,7 +172,7 @@ class PagedCache:
             raise ValueError("out must have a row for every token")
         return out, self._rows(out, self.n_q, "out", self.dtype)
 
-    @_on_pools_device
+    @_library_call
     def attend(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of the new tokens over the cache; ``window`` > 0
@@ -182,7 +188,7 @@ class PagedCache:
                                 window, out.data_ptr(), ld_out, w.data_ptr(), w.numel(), stream)
         return out
 
-    @_on_pools_device
+    @_library_call
     def page_scores(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """fp32 [tokens, n_kv, max_pages]: the score of every page a token sees,
@@ -200,7 +206,7 @@ class PagedCache:
                                  out.data_ptr(), _raw_stream(self.index))
         return out
 
-    @_on_pools_device
+    @_library_call
     def attend_pages(self, q: torch.Tensor, scores: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                      top: int, sink: int = 1, local: int = 1, scale: Optional[float] = None,
                      out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -1,6 +1,7 @@
 """What ``paged.PagedCache`` does on the host, with the library's calls, the
 stream and the capture state replaced by stand-ins and CPU tensors in place of
 device tensors: nothing is launched."""
+import threading
 import types
 
 import pytest
@@ -144,3 +145,34 @@ def test_calls_run_on_the_pools_device(host, call):
     host.device = 1
     call(c, 5)
     assert host.calls and all(device == 1 for _, device in host.calls)
+
+
+def test_threads_do_not_see_each_others_batch(host, monkeypatch):
+    """The library reads the batch's pointers after the interpreter lock is let go: a call of
+    another thread in between must not change them."""
+    c = cache()
+    inside, go_on, seen = threading.Event(), threading.Event(), {}
+
+    def kv_append(desc, tokens, *rest):
+        if tokens == 3:
+            inside.set()
+            go_on.wait(5)
+        seen[tokens] = (desc.q_start, desc.kv_len)
+
+    monkeypatch.setattr(capi, "pipo_op_kv_append", kv_append)
+    batches = {n: batch_of(c, n) for n in (3, 8)}
+
+    def run(n):
+        q, qs, kl = batches[n]
+        k = torch.zeros(n, c.n_kv, c.d_h)
+        c.append(None, k, k, qs, kl)
+
+    first, second = (threading.Thread(target=run, args=(n,)) for n in (3, 8))
+    first.start()
+    assert inside.wait(5)
+    second.start()
+    second.join(0.3)  # (it either ends here or waits for the first)
+    go_on.set()
+    first.join(5)
+    second.join(5)
+    assert seen == {n: (b[1].data_ptr(), b[2].data_ptr()) for n, b in batches.items()}
