@@ -156,7 +156,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append_kernel(AppendA
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int h = h0 + u * HL::H + hl;
-                norm_turn<DH>(a[u], b[u], p.q_gain != nullptr, gain, p.eps, an);
+                // (a token without an entry stays zero: with eps = 0 the norm of nothing is NaN)
+                norm_turn<DH>(a[u], b[u], p.q_gain != nullptr && k.pos >= 0, gain, p.eps, an);
                 if (h < c.n_q) {
                     store_f<T, 4>(dst + (size_t)h * DH, a[u]);
                     store_f<T, 4>(dst + (size_t)h * DH + DH / 2, b[u]);

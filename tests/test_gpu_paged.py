@@ -495,3 +495,19 @@ def test_a_graph_keeps_its_scratch_beside_larger_calls():
         check(out, ref, torch.bfloat16)
         check(some, ref, torch.bfloat16)
     assert all((t == 7).all() for t in other)
+
+
+@pytest.mark.parametrize("tin", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d_h", [64, 128])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_queries_without_an_entry_are_zero_with_norms(tin, dtype, d_h, eps):
+    """A token with a negative position has zero queries, whatever the norm makes of nothing."""
+    x = Batch([3, 0, 130], [5, 2, 1], 8, 2, d_h, dtype, seed=3)
+    c, qs, kl = cache_of(x)
+    g = torch.Generator().manual_seed(3)
+    q, k = (torch.randn(x.tokens, n, d_h, generator=g).to(tin).cuda() for n in (8, 2))
+    gain = torch.ones(d_h, dtype=dtype, device="cuda")
+    y = c.append(q, k, k, qs, kl, q_gain=gain, k_gain=gain, eps=eps, rope=paged.rope_table(x.width * PAGE, d_h, 1e4))
+    assert (y[:2] == 0).all() and (y[5:7] == 0).all()
+    assert torch.isfinite(y).all() and (y[2:5] != 0).any() and (y[7] != 0).any()
