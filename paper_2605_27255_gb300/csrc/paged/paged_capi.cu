@@ -207,7 +207,8 @@ pipo_status pipo_op_attn_paged(const pipo_paged* c, int32_t n_tokens, const void
     a.out = d_out;
     a.ld_out = ld_out;
     a.scale = scale;
-    a.window = window;
+    // a window as long as any sequence is none; below that, positions minus the window fit in 32 bits
+    a.window = (long long)window < (long long)kPage * c->max_pages ? window : 0;
     a.scratch = static_cast<unsigned char*>(d_scratch);
     return run_attn("pipo_op_attn_paged", a, nullptr, scratch_bytes, static_cast<cudaStream_t>(stream));
 }

@@ -511,3 +511,13 @@ def test_queries_without_an_entry_are_zero_with_norms(tin, dtype, d_h, eps):
     y = c.append(q, k, k, qs, kl, q_gain=gain, k_gain=gain, eps=eps, rope=paged.rope_table(x.width * PAGE, d_h, 1e4))
     assert (y[:2] == 0).all() and (y[5:7] == 0).all()
     assert torch.isfinite(y).all() and (y[2:5] != 0).any() and (y[7] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 70, 2 ** 30, 449, 448, 447])
+def test_attend_windows_of_every_entry(dtype, window):
+    """A window longer than any sequence hides nothing, also where more tokens than entries put
+    positions below zero; so do windows of and just below the longest sequence's 448 entries."""
+    x = Batch([5, 70, 0, 448, 130], [10, 150, 2, 448, 1], 8, 2, 64, dtype, seed=3)
+    c, qs, kl = cache_of(x)
+    check(c.attend(x.q.cuda(), qs, kl, window=window), ref_attend(x, 0.125, window), dtype)
