@@ -33,6 +33,11 @@ _current_device = torch._C._cuda_getDevice
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
+def _int32(n: int) -> int:
+    """The nearest integer that the library's int32 arguments hold (ctypes would drop the upper bits)."""
+    return max(-1 << 31, min(n, (1 << 31) - 1))
+
+
 def rope_table(n: int, d_h: int, theta: float, device="cuda") -> torch.Tensor:
     """(cos, sin) of every position and pair, angle ``position * theta^(-2i/d_h)``,
     computed in fp64 and rounded once: fp32 [n, d_h/2, 2]."""
@@ -80,8 +85,8 @@ class PagedCache:
         self.k, self.v, self.table, self.means = k, v, table, means
         self.n_q, self.n_kv, self.d_h, self.dtype, self.device = n_q, k.shape[1], k.shape[3], k.dtype, k.device
         self.index = k.device.index
-        self._c = capi.pipo_paged(_TYPES[k.dtype], n_q, k.shape[1], k.shape[3], PAGE, k.shape[0], table.shape[1],
-                                  table.shape[0], k.data_ptr(), v.data_ptr(),
+        self._c = capi.pipo_paged(_TYPES[k.dtype], _int32(n_q), k.shape[1], k.shape[3], PAGE, k.shape[0],
+                                  table.shape[1], table.shape[0], k.data_ptr(), v.data_ptr(),
                                   None if means is None else means.data_ptr(), table.data_ptr())
         self._seqs = table.shape[0]
         self._lock = threading.Lock()
@@ -185,7 +190,7 @@ class PagedCache:
         stream = _raw_stream(self.index)
         w = self._work(q.shape[0], stream)
         capi.pipo_op_attn_paged(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
-                                window, out.data_ptr(), ld_out, w.data_ptr(), w.numel(), stream)
+                                _int32(window), out.data_ptr(), ld_out, w.data_ptr(), w.numel(), stream)
         return out
 
     @_library_call
@@ -223,6 +228,6 @@ class PagedCache:
         stream = _raw_stream(self.index)
         w = self._work(q.shape[0], stream)
         capi.pipo_op_attn_pages(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
-                                scores.data_ptr(), top, sink, local, out.data_ptr(), ld_out, pages.data_ptr(),
-                                w.data_ptr(), w.numel(), stream)
+                                scores.data_ptr(), _int32(top), _int32(sink), _int32(local), out.data_ptr(), ld_out,
+                                pages.data_ptr(), w.data_ptr(), w.numel(), stream)
         return out, pages

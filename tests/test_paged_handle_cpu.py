@@ -1,6 +1,7 @@
 """What ``paged.PagedCache`` does on the host, with the library's calls, the
 stream and the capture state replaced by stand-ins and CPU tensors in place of
 device tensors: nothing is launched."""
+import ctypes
 import threading
 import types
 
@@ -176,3 +177,33 @@ def test_threads_do_not_see_each_others_batch(host, monkeypatch):
     first.join(5)
     second.join(5)
     assert seen == {n: (b[1].data_ptr(), b[2].data_ptr()) for n, b in batches.items()}
+
+
+def test_integers_past_32_bits_are_not_wrapped(host, monkeypatch):
+    """ctypes keeps the low 32 bits of an integer: what the library is given has to be in
+    range already, a larger window as the largest there is, other values as ones it refuses."""
+    given = []
+    monkeypatch.setattr(capi, "pipo_op_attn_paged", lambda *a: given.append([a[5]]))
+    monkeypatch.setattr(capi, "pipo_op_attn_pages", lambda *a: given.append(list(a[6:9])))
+    c = cache()
+
+    def passed(call, **kw):
+        call(c, 2, **kw)
+        values = given.pop()
+        assert [ctypes.c_int32(v).value for v in values] == values, values
+        return values
+
+    for w in (0, 1, 100, 2 ** 31 - 1):
+        assert passed(attend, window=w) == [w]
+    for w in (2 ** 31, 2 ** 32, 2 ** 32 + 5, 1 << 60):
+        assert passed(attend, window=w) == [2 ** 31 - 1]
+    for w in (-1, -2 ** 32, -2 ** 32 + 5):
+        assert passed(attend, window=w)[0] < 0
+    assert passed(attend_pages, top=5, sink=2, local=3) == [5, 2, 3]
+    for n in (2 ** 31, 2 ** 32, 2 ** 32 + 1):
+        assert passed(attend_pages, sink=n)[1] > 4096 and passed(attend_pages, local=n)[2] > 4096
+    for n in (-1, -2 ** 32, -2 ** 32 + 1):
+        assert passed(attend_pages, sink=n)[1] < 0 and passed(attend_pages, local=n)[2] < 0
+    pool = torch.zeros(2, 2, paged.PAGE, 64)
+    wide = paged.PagedCache(pool, pool, torch.zeros(1, 1, dtype=torch.int32), n_q=2 ** 32 + 4)
+    assert wide._c.n_q_heads > 65536  # (refused by every call)
