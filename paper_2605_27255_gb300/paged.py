@@ -14,8 +14,10 @@ token tensors ``[tokens, heads, d_h]`` (any token stride; the heads of a token
 back to back), and ``kv_len[b]`` counts its cached entries, the new ones
 included.  ``q_start`` and ``kv_len`` are int32 tensors on the device and are
 read there: the calls neither synchronise nor depend on host copies, and a
-captured graph follows their values.  Shapes and types are checked here,
-everything else by the library (``capi.PipoError``).
+captured graph follows their values.  There is no backward pass: inputs that
+require gradients are refused unless gradients are off (``torch.no_grad``).
+Shapes and types are checked here, everything else by the library
+(``capi.PipoError``).
 """
 from __future__ import annotations
 
@@ -44,6 +46,11 @@ def rope_table(n: int, d_h: int, theta: float, device="cuda") -> torch.Tensor:
     i = torch.arange(0, d_h, 2, device=device, dtype=torch.float64)
     a = torch.arange(n, device=device, dtype=torch.float64)[:, None] * theta ** (-i / d_h)
     return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+
+
+def _no_backward(name: str, x: torch.Tensor) -> None:
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and the paged-cache operators have none")
 
 
 def _library_call(method):
@@ -109,6 +116,7 @@ class PagedCache:
         if len(shape) != 3 or shape[1] != heads or shape[2] != self.d_h or x.dtype is not dtype or \
                 x.device != self.device or (shape[0] and (stride[2] != 1 or (heads > 1 and stride[1] != self.d_h))):
             raise ValueError(f"{name} must be [tokens, {heads}, {self.d_h}] {dtype} with whole rows")
+        _no_backward(name, x)
         return stride[0] if shape[0] > 1 else heads * self.d_h
 
     def _work(self, tokens: int, stream: int) -> torch.Tensor:
@@ -150,12 +158,17 @@ class PagedCache:
         if v.shape[0] != tokens or (q is not None and q.shape[0] != tokens):
             raise ValueError("q, k and v must have the same number of tokens")
         for gain in (q_gain, k_gain):
-            if gain is not None and (gain.dtype != self.dtype or gain.shape != (self.d_h,) or
-                                     not gain.is_contiguous() or gain.device != self.device):
+            if gain is None:
+                continue
+            if gain.dtype != self.dtype or gain.shape != (self.d_h,) or not gain.is_contiguous() or \
+                    gain.device != self.device:
                 raise ValueError("gains must be [d_h] of the pools' type")
-        if rope is not None and (rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1] != self.d_h // 2 or
-                                 rope.shape[2] != 2 or not rope.is_contiguous() or rope.device != self.device):
-            raise ValueError("rope must be a contiguous float32 [positions, d_h / 2, 2]")
+            _no_backward("a gain", gain)
+        if rope is not None:
+            if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1] != self.d_h // 2 or \
+                    rope.shape[2] != 2 or not rope.is_contiguous() or rope.device != self.device:
+                raise ValueError("rope must be a contiguous float32 [positions, d_h / 2, 2]")
+            _no_backward("rope", rope)
         if q is None:
             out = None
         elif out is None:
@@ -223,6 +236,7 @@ class PagedCache:
         if scores.shape != (q.shape[0], self.n_kv, self.table.shape[1]) or scores.dtype != torch.float32 or \
                 not scores.is_contiguous() or scores.device != self.device:
             raise ValueError("scores must be a contiguous float32 [tokens, n_kv, max_pages]")
+        _no_backward("scores", scores)
         out, ld_out = self._out(q, out)
         pages = torch.empty((q.shape[0], self.n_kv, top), dtype=torch.int32, device=self.device)
         stream = _raw_stream(self.index)

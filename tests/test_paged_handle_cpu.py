@@ -207,3 +207,37 @@ def test_integers_past_32_bits_are_not_wrapped(host, monkeypatch):
     pool = torch.zeros(2, 2, paged.PAGE, 64)
     wide = paged.PagedCache(pool, pool, torch.zeros(1, 1, dtype=torch.int32), n_q=2 ** 32 + 4)
     assert wide._c.n_q_heads > 65536  # (refused by every call)
+
+
+def test_inputs_that_require_grad_are_refused(host):
+    """The operators have no backward pass: with gradients enabled an output would silently
+    carry none."""
+    c = cache()
+
+    def inputs():
+        q, qs, kl = batch_of(c, 2)
+        k, gain = torch.zeros(2, c.n_kv, c.d_h), torch.ones(c.d_h)
+        scores = torch.zeros(2, c.n_kv, c.table.shape[1])
+        rope = paged.rope_table(c.table.shape[1] * paged.PAGE, c.d_h, 1e4, "cpu")
+        return dict(q=q, k=k, v=k.clone(), q_gain=gain, k_gain=gain.clone(), scores=scores, rope=rope), qs, kl
+
+    calls = {
+        "q": [lambda x, *b: c.append(x["q"], x["k"], x["v"], *b), lambda x, *b: c.attend(x["q"], *b),
+              lambda x, *b: c.page_scores(x["q"], *b), lambda x, *b: c.attend_pages(x["q"], x["scores"], *b, top=1)],
+        "k": [lambda x, *b: c.append(None, x["k"], x["v"], *b)],
+        "v": [lambda x, *b: c.append(None, x["k"], x["v"], *b)],
+        "q_gain": [lambda x, *b: c.append(x["q"], x["k"], x["v"], *b, q_gain=x["q_gain"])],
+        "k_gain": [lambda x, *b: c.append(x["q"], x["k"], x["v"], *b, k_gain=x["k_gain"])],
+        "rope": [lambda x, *b: c.append(None, x["k"], x["v"], *b, rope=x["rope"])],
+        "scores": [lambda x, *b: c.attend_pages(x["q"], x["scores"], *b, top=1)],
+    }
+    for name, fns in calls.items():
+        for fn in fns:
+            x, qs, kl = inputs()
+            fn(x, qs, kl)
+            x[name].requires_grad_()
+            with pytest.raises(ValueError, match="gradient"):
+                fn(x, qs, kl)
+            with torch.no_grad():
+                fn(x, qs, kl)
+            fn({n: t.detach() for n, t in x.items()}, qs, kl)
