@@ -21,7 +21,6 @@ Shapes and types are checked here, everything else by the library
 """
 from __future__ import annotations
 
-import functools
 import threading
 from typing import Dict, Optional, Tuple
 
@@ -37,7 +36,7 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 def _int32(n: int) -> int:
     """The nearest integer that the library's int32 arguments hold (ctypes would drop the upper bits)."""
-    return max(-1 << 31, min(n, (1 << 31) - 1))
+    return n if -0x80000000 <= n <= 0x7fffffff else 0x7fffffff if n > 0 else -0x80000000
 
 
 def rope_table(n: int, d_h: int, theta: float, device="cuda") -> torch.Tensor:
@@ -51,20 +50,6 @@ def rope_table(n: int, d_h: int, theta: float, device="cuda") -> torch.Tensor:
 def _no_backward(name: str, x: torch.Tensor) -> None:
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, and the paged-cache operators have none")
-
-
-def _library_call(method):
-    """The library plans and launches on the thread's current device: make that the pools'.  And
-    it reads the object's description of the batch without the interpreter lock: one call of
-    an object at a time."""
-    @functools.wraps(method)
-    def call(self, *args, **kw):
-        with self._lock:
-            if _current_device() == self.index:
-                return method(self, *args, **kw)
-            with torch.cuda.device(self.index):
-                return method(self, *args, **kw)
-    return call
 
 
 class PagedCache:
@@ -139,9 +124,10 @@ class PagedCache:
         """The current stream's buffer, if it has one."""
         return self._buffers.get(_raw_stream(self.index))
 
-    # ---- the calls
+    # ---- the calls.  The library plans and launches on the thread's current device, so that each
+    # makes that the pools' first; and it reads the object's description of the batch without
+    # the interpreter lock, so that the calls of an object take turns from there on.
 
-    @_library_call
     def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor,
                kv_len: torch.Tensor, *, q_gain: Optional[torch.Tensor] = None,
                k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, rope: Optional[torch.Tensor] = None,
@@ -149,7 +135,9 @@ class PagedCache:
         """Normalise (where a gain is given) and rotate (where a table is) the
         new queries and keys, append keys and values, update the page means.
         Returns the queries [tokens, n_q, d_h] in the pools' type (None without q)."""
-        self._batch(q_start, kv_len)
+        if _current_device() != self.index:
+            with torch.cuda.device(self.index):
+                return self.append(q, k, v, q_start, kv_len, q_gain=q_gain, k_gain=k_gain, eps=eps, rope=rope, out=out)
         if k.dtype not in _TYPES:
             raise ValueError("keys must be float32 or bfloat16")
         tokens = k.shape[0]
@@ -177,9 +165,11 @@ class PagedCache:
                 out.device != self.device:
             raise ValueError("out must be a contiguous [tokens, n_q, d_h] of the pools' type")
         p = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
-        capi.pipo_op_kv_append(self._c, tokens, _TYPES[k.dtype], p(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
-                               p(q_gain), p(k_gain), eps, p(rope), 0 if rope is None else rope.shape[0], p(out),
-                               _raw_stream(self.index))
+        with self._lock:
+            self._batch(q_start, kv_len)
+            capi.pipo_op_kv_append(self._c, tokens, _TYPES[k.dtype], p(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(),
+                                   ld_v, p(q_gain), p(k_gain), eps, p(rope), 0 if rope is None else rope.shape[0],
+                                   p(out), _raw_stream(self.index))
         return out
 
     def _out(self, q: torch.Tensor, out: Optional[torch.Tensor]) -> Tuple[torch.Tensor, int]:
@@ -190,48 +180,58 @@ class PagedCache:
             raise ValueError("out must have a row for every token")
         return out, self._rows(out, self.n_q, "out", self.dtype)
 
-    @_library_call
     def attend(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of the new tokens over the cache; ``window`` > 0
         keeps the last ``window`` entries of every token, and pages that it has
         passed for all new tokens of a sequence are not needed (their blocks
         and table entries may hold anything).  scale: 1/sqrt(d_h) unless given."""
-        self._batch(q_start, kv_len)
+        if _current_device() != self.index:
+            with torch.cuda.device(self.index):
+                return self.attend(q, q_start, kv_len, scale=scale, window=window, out=out)
         ld_q = self._rows(q, self.n_q, "q", self.dtype)
         out, ld_out = self._out(q, out)
         stream = _raw_stream(self.index)
-        w = self._work(q.shape[0], stream)
-        capi.pipo_op_attn_paged(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
-                                _int32(window), out.data_ptr(), ld_out, w.data_ptr(), w.numel(), stream)
+        with self._lock:
+            self._batch(q_start, kv_len)
+            w = self._work(q.shape[0], stream)
+            capi.pipo_op_attn_paged(self._c, q.shape[0], q.data_ptr(), ld_q,
+                                    self.d_h ** -0.5 if scale is None else scale, _int32(window), out.data_ptr(),
+                                    ld_out, w.data_ptr(), w.numel(), stream)
         return out
 
-    @_library_call
     def page_scores(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """fp32 [tokens, n_kv, max_pages]: the score of every page a token sees,
         -inf for the others."""
         if self.means is None:
             raise ValueError("page scores need a cache with means")
-        self._batch(q_start, kv_len)
+        if _current_device() != self.index:
+            with torch.cuda.device(self.index):
+                return self.page_scores(q, q_start, kv_len, scale=scale, out=out)
         ld_q = self._rows(q, self.n_q, "q", self.dtype)
         shape = (q.shape[0], self.n_kv, self.table.shape[1])
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=self.device)
         elif out.shape != shape or out.dtype != torch.float32 or not out.is_contiguous() or out.device != self.device:
             raise ValueError("out must be a contiguous float32 [tokens, n_kv, max_pages]")
-        capi.pipo_op_page_scores(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
-                                 out.data_ptr(), _raw_stream(self.index))
+        with self._lock:
+            self._batch(q_start, kv_len)
+            capi.pipo_op_page_scores(self._c, q.shape[0], q.data_ptr(), ld_q,
+                                     self.d_h ** -0.5 if scale is None else scale, out.data_ptr(),
+                                     _raw_stream(self.index))
         return out
 
-    @_library_call
     def attend_pages(self, q: torch.Tensor, scores: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                      top: int, sink: int = 1, local: int = 1, scale: Optional[float] = None,
                      out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Causal attention over ``top`` pages per token and kv head: the first
         ``sink``, the last ``local`` and the best scored.  Returns the outputs
         and the pages, int32 [tokens, n_kv, top], ascending, -1 behind the last."""
-        self._batch(q_start, kv_len)
+        if _current_device() != self.index:
+            with torch.cuda.device(self.index):
+                return self.attend_pages(q, scores, q_start, kv_len, top=top, sink=sink, local=local, scale=scale,
+                                         out=out)
         ld_q = self._rows(q, self.n_q, "q", self.dtype)
         if scores.shape != (q.shape[0], self.n_kv, self.table.shape[1]) or scores.dtype != torch.float32 or \
                 not scores.is_contiguous() or scores.device != self.device:
@@ -240,8 +240,11 @@ class PagedCache:
         out, ld_out = self._out(q, out)
         pages = torch.empty((q.shape[0], self.n_kv, top), dtype=torch.int32, device=self.device)
         stream = _raw_stream(self.index)
-        w = self._work(q.shape[0], stream)
-        capi.pipo_op_attn_pages(self._c, q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale,
-                                scores.data_ptr(), _int32(top), _int32(sink), _int32(local), out.data_ptr(), ld_out,
-                                pages.data_ptr(), w.data_ptr(), w.numel(), stream)
+        with self._lock:
+            self._batch(q_start, kv_len)
+            w = self._work(q.shape[0], stream)
+            capi.pipo_op_attn_pages(self._c, q.shape[0], q.data_ptr(), ld_q,
+                                    self.d_h ** -0.5 if scale is None else scale, scores.data_ptr(), _int32(top),
+                                    _int32(sink), _int32(local), out.data_ptr(), ld_out, pages.data_ptr(),
+                                    w.data_ptr(), w.numel(), stream)
         return out, pages
