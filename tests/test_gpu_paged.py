@@ -521,3 +521,48 @@ def test_attend_windows_of_every_entry(dtype, window):
     x = Batch([5, 70, 0, 448, 130], [10, 150, 2, 448, 1], 8, 2, 64, dtype, seed=3)
     c, qs, kl = cache_of(x)
     check(c.attend(x.q.cuda(), qs, kl, window=window), ref_attend(x, 0.125, window), dtype)
+
+
+# ---- long tables: more than one block of pages per score row, every width of the selection ------
+# (tolerances as above: scores are within a few 2^-24 of their size, which moves a weight by 1e-6 at
+# most, whatever the number of entries)
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("new", [[1, 1], [1, 45], [0, 3]])
+@pytest.mark.parametrize("lens,width", [([4160, 8200], 0), ([4096, 4097], 0), ([130, 9000], 300)])
+def test_page_scores_of_many_pages(dtype, new, lens, width):
+    x = Batch(lens, new, 6, 2, 64, dtype, seed=3, width=width or None)
+    means = torch.randn(x.blocks, 2, 64, generator=torch.Generator().manual_seed(2)).to(dtype)
+    c, qs, kl = cache_of(x, means.cuda())
+    got, ref = c.page_scores(x.q.cuda(), qs, kl, scale=0.25).cpu().double(), ref_scores(x, means, 0.25)
+    assert torch.equal(torch.isinf(got), torch.isinf(ref)) and not torch.isnan(got).any()
+    fin = torch.isfinite(ref)
+    assert (got[fin] - ref[fin]).abs().max() <= 2e-5 * max(1.0, ref[fin].abs().max().item())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("new", [[1, 2, 1], [1, 40, 0]])  # (40 tokens of 16 heads: whole tiles in bf16, if `top` is large)
+@pytest.mark.parametrize("last,width", [(8129, 0), (9000, 256), (16385, 0), (40000, 0), (9000, 1024), (70400, 0),
+                                        (300, 1500)])
+@pytest.mark.parametrize("top", [5, 100])
+def test_attend_pages_of_long_tables(dtype, new, last, width, top):
+    x = Batch([130, last, 64], new, 16, 1, 64, dtype, seed=top, width=width or None)
+    c, qs, kl = cache_of(x)
+    sc = torch.randn(x.tokens, 1, x.width, generator=torch.Generator().manual_seed(top))
+    sc[:, :, 2::5] = 0.5
+    sc[1, :, 3::2] = float("nan")
+    sc[2, :, :] = float("-inf")
+    out, pages = c.attend_pages(x.q.cuda(), sc.cuda(), qs, kl, top=top, sink=1, local=2)
+    ref = ref_select(x, sc, top, 1, 2)
+    assert torch.equal(pages.cpu(), ref)
+    check(out, ref_attend(x, 0.125, pages=ref), dtype)
+    capi.pipo_op_paged_check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("new", [[1, 1], [20, 1]])
+def test_attend_long(dtype, new):
+    x = Batch([70001, 8200], new, 16, 1, 64, dtype, seed=3, width=1200)
+    c, qs, kl = cache_of(x)
+    check(c.attend(x.q.cuda(), qs, kl), ref_attend(x, 0.125), dtype)
+    check(c.attend(x.q.cuda(), qs, kl, window=3000), ref_attend(x, 0.125, 3000), dtype)
