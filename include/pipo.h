@@ -455,8 +455,15 @@ PIPO_API pipo_status pipo_op_kv_append(const pipo_paged *c, int32_t n_tokens, in
  * appended before): out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over
  * the entries j <= position, and with window > 0 only j > position - window.
  * d_q at ld_q elements per token, d_out at ld_out, both in the pools' type;
- * d_out overlaps none of the inputs.  scale > 0.  d_scratch: pipo_op_attn_paged_scratch(c, n_tokens) bytes, 16-byte
- * aligned, overwritten; not shared with a call that may overlap. */
+ * d_out overlaps none of the inputs.  scale > 0.  Scores, softmax and sums are
+ * fp32.  With bf16 pools the softmax weights meet the values as two bf16 parts
+ * where the batch has at most 128 rows (new tokens times query heads of a kv
+ * head) per sequence on average, else as one part (an error of about 1.4 times
+ * that of the output's own rounding): the low bits of a sequence's outputs
+ * depend on what shares its batch, the same call gives the same bits.
+ * d_scratch: pipo_op_attn_paged_scratch(c, n_tokens) bytes, 16-byte aligned,
+ * overwritten; not shared with a call that may overlap, and for a captured call
+ * kept for the graph's replays. */
 PIPO_API pipo_status pipo_op_attn_paged(const pipo_paged *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
                                         float scale, int32_t window, void *d_out, int64_t ld_out, void *d_scratch,
                                         size_t scratch_bytes, void *stream);
@@ -468,7 +475,9 @@ PIPO_API size_t pipo_op_attn_paged_scratch(const pipo_paged *c, int32_t n_tokens
 /* The cheap score of every page a token sees: d_scores[t][g][p] = scale *
  * sum over the query heads h of kv head g of q[t, h] . means[table[b][p]][g],
  * fp32 [n_tokens][n_kv][max_pages]; -infinity for pages past the token's
- * position.  Needs c->means (k and v may be NULL). */
+ * position.  Needs c->means (k and v may be NULL).  A mean is of all entries
+ * its page holds: that of the page a token stands in counts later tokens of
+ * the same call too. */
 PIPO_API pipo_status pipo_op_page_scores(const pipo_paged *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
                                          float scale, float *d_scores, void *stream);
 
@@ -477,7 +486,9 @@ PIPO_API pipo_status pipo_op_page_scores(const pipo_paged *c, int32_t n_tokens, 
  * those with the largest d_scores[t][g][p] (ties go to the lower page, NaN
  * comes last) until it has n_top, or all of them; d_pages[t][g][n_top] (int32)
  * receives them in ascending order, -1 behind the last.  n_sink, n_local >= 0,
- * n_sink + n_local <= n_top, 1 <= n_top <= 4096.  d_scores is
+ * n_sink + n_local <= n_top, 1 <= n_top <= 4096.  n_local >= 1 keeps the page
+ * a token stands in whatever its score (with n_local 0 and scores from page
+ * means, the selection depends on how a prompt was cut into calls).  d_scores is
  * [n_tokens][n_kv][max_pages] as pipo_op_page_scores writes it (what it holds
  * past a token's pages is not read); any values will do, e.g. those of a
  * learned indexer.  Otherwise as pipo_op_attn_paged. */

@@ -53,8 +53,9 @@ __device__ __forceinline__ void cp_async_wait() {
 
 // 64 rows: threads as 16 x 16, thread (ty, tx) has the scores of rows ty + 16 r and entries
 // tx + 16 i, and rows ty + 16 r and dims 4 tx + 64 c of the output: 64 multiply-adds per 8 shared
-// loads, bound by the fp32 rate.  (As in AfRows, with 8 rows per warp: four chunks of 500 tokens up to
-// entry 1000, 16 query and 4 kv heads of 64, 348 us, so 310.)
+// loads.  Four chunks of 500 tokens up to entry 1000, 16 query and 4 kv heads of 64, 310 us: 20
+// TFLOP/s, a quarter of the fp32 rate, with three barriers a page and one buffer each for keys and
+// values.  (As in AfRows, with 8 rows per warp: 348 us.)
 template <int DH>
 struct AfGrid {
     static constexpr int RT = 4, LD = DH + 4, LP = kPage + 4, NC = DH / 64;

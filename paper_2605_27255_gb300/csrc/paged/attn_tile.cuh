@@ -17,6 +17,8 @@
 //               has passed it by 2^8: until then the weights are at most 256 and
 //               neither O nor the sum is touched; when it moves the row's
 //               thread rescales its row of O in TMEM.
+// (Such a reference, and warps of their own for issuing, softmax and copies, are published
+// methods for attention on this architecture.)
 //
 // The scores of 64 entries (a page) have a buffer each, two per pipeline, so that
 // the softmax of one page runs under the MMAs of the next: with one buffer of 128

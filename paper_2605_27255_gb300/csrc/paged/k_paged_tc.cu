@@ -27,11 +27,15 @@ cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMa
 // The plan of a launch; scratch: see work.cuh.
 // bf16: pairs of row tiles when the sequences of the batch have more than 128 rows
 // on average.  fp32: tiles of 64 rows when they have more than 16, else of 16.
-// n_top > 0: attention over selected pages (< 0: by lists, whatever the sizes).  A token and kv head alone read n_top pages; a
-// tile of tokens reads each page once for all of them and masks by bits, every page of
-// the cache in the worst case.  Whole tiles, where they never read more: when the tokens of a
-// sequence (on average, a tile's at most) times n_top reach max_pages.  (bf16, 512 tokens with 16 of
-// 249 pages each: 279 us by lists, 143 by tiles at that time.)
+// n_top > 0: attention over selected pages (< 0: by lists, whatever the sizes).  By lists a token and
+// kv head read n_top pages; a tile of tokens reads every page up to its last position once
+// for all of them and masks by bits.  Whole tiles, when the tokens of a sequence (on average, a
+// tile's at most) times n_top reach max_pages: such a tile reads no more than its tokens' lists
+// name.  (bf16, 512 tokens with 16 of 249 pages each: 279 us by lists, 143 by tiles at that time.)
+// The lengths are on the device, so the rule goes by the batch's average and the table's width:
+// decoding sequences beside a long chunk read all their pages with it, and a chunk under a table much
+// wider than its cache, or beside many idle sequences, goes by lists.  Either way the same
+// pages have weight.
 AttnPlan plan_attn(const PagedArgs& c, int n_top, int dev, int sms) {
     AttnPlan pl{};
     pl.dev = dev;

@@ -21,7 +21,8 @@ namespace pipo {
 constexpr int kTileEnt = 128;  // entries per unit (two pages)
 // What an item costs beside its units, in units: about 6300 cycles from the last page of one to
 // the second of the next in the bf16 kernel, against 3300 for a unit.  (Without it the workers of 16
-// mixed sequences took 75000 to 143000 cycles, by their number of items.)
+// mixed sequences took 75000 to 143000 cycles, by their number of items.)  The fp32 kernel cuts
+// its pieces by the same number; it was not measured there.
 constexpr int kItemCost = 2;
 
 // What a launch needs of an item's shape

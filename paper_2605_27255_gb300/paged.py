@@ -226,8 +226,9 @@ class PagedCache:
                      top: int, sink: int = 1, local: int = 1, scale: Optional[float] = None,
                      out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Causal attention over ``top`` pages per token and kv head: the first
-        ``sink``, the last ``local`` and the best scored.  Returns the outputs
-        and the pages, int32 [tokens, n_kv, top], ascending, -1 behind the last."""
+        ``sink``, the last ``local`` and the best scored.  ``local`` >= 1 keeps the
+        page a token stands in, whose mean counts later tokens of the same call.  Returns
+        the outputs and the pages, int32 [tokens, n_kv, top], ascending, -1 behind the last."""
         if _current_device() != self.index:
             with torch.cuda.device(self.index):
                 return self.attend_pages(q, scores, q_start, kv_len, top=top, sink=sink, local=local, scale=scale,
