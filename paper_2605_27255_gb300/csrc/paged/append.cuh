@@ -140,6 +140,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append_kernel(AppendA
         const Angles an = load_angles<DH>(k.pos >= 0 ? p.rope : nullptr, k.pos);
         const TI* src = static_cast<const TI*>(p.q) + (size_t)t * p.ld_q + d;
         T* dst = static_cast<T*>(p.q_out) + (size_t)t * c.n_q * DH + d;
+        const float eps = k.pos >= 0 ? p.eps : 1.f;  // (a token without an entry: zeros, also where eps is 0)
         constexpr int U = 4;  // heads in flight per lane
         for (int h0 = 0; h0 < c.n_q; h0 += U * HL::H) {
             float a[U][4], b[U][4];
@@ -156,8 +157,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append_kernel(AppendA
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int h = h0 + u * HL::H + hl;
-                // (a token without an entry stays zero: with eps = 0 the norm of nothing is NaN)
-                norm_turn<DH>(a[u], b[u], p.q_gain != nullptr && k.pos >= 0, gain, p.eps, an);
+                norm_turn<DH>(a[u], b[u], p.q_gain != nullptr, gain, eps, an);
                 if (h < c.n_q) {
                     store_f<T, 4>(dst + (size_t)h * DH, a[u]);
                     store_f<T, 4>(dst + (size_t)h * DH + DH / 2, b[u]);
