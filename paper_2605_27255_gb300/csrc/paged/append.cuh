@@ -118,7 +118,7 @@ __device__ __forceinline__ bool find_run(const PagedArgs& c, int r, int& b, int&
     return false;
 }
 
-// Four CTAs an SM (64 registers) keep enough loads in flight: 73 us for two 8191-token prompts,
+// Four CTAs an SM (64 registers) keep enough loads in flight: 74 us for two 8191-token prompts,
 // 5.6 TB/s; with two entries per lane at a time 80, with the registers that take (three CTAs) 89, with 16
 // dims per lane 90.
 // grid: page_ctas = runs * n_kv CTAs of (page, kv head), then kAppendWarps tokens' queries each
