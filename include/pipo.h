@@ -497,6 +497,112 @@ PIPO_API pipo_status pipo_op_attn_pages(const pipo_paged *c, int32_t n_tokens, c
                                         int32_t n_local, void *d_out, int64_t ld_out, int32_t *d_pages,
                                         void *d_scratch, size_t scratch_bytes, void *stream);
 
+/* ---- the same cache in 8 bits --------------------------------------------
+ * Half the bytes of a bf16 cache: keys and values as e4m3 codes with one scale for every
+ * block and kv head.  An entry stands for code * scale.  Scales are powers of two
+ * between 2^-100 and 2^7 (fp32; magnitudes above 448 * 2^7 = 57344 saturate); the append
+ * chooses them, and pools that something else has filled need such scales too.  Queries, gains
+ * and outputs are bf16.  Everything else (layout, ragged batches, positions, what may
+ * hold anything, what is refused) as for pipo_paged. */
+typedef struct {
+    int32_t n_q_heads;
+    int32_t n_kv_heads;  /* n_q_heads / n_kv_heads a whole number of at most 16 */
+    int32_t head_dim;    /* d_h: 64 or 128 */
+    int32_t page_size;   /* 64 */
+    int32_t n_blocks;
+    int32_t max_pages;
+    int32_t batch;
+    void *k;             /* [n_blocks][n_kv][64][d_h] e4m3 */
+    void *v;             /* [n_blocks][n_kv][64][d_h] e4m3 */
+    float *k_scale;      /* [n_blocks][n_kv] */
+    float *v_scale;      /* [n_blocks][n_kv] */
+    const int32_t *table;    /* [batch][max_pages] */
+    const int32_t *q_start;  /* [batch + 1] */
+    const int32_t *kv_len;   /* [batch] */
+} pipo_paged8;
+
+/* Norm, rotation and append, as pipo_op_kv_append, to an 8-bit cache; the queries come
+ * out in bf16.  A call that writes slot 0 of a block chooses the block's scales:
+ * the power of two that leaves the largest finite magnitude of its new entries in [32, 64).
+ * Later entries keep a scale while they fit 448 times it; else it is chosen from
+ * them in the same way, and the codes held before move by the ratio (exactly, but for those
+ * that become subnormal).  So a block's codes depend on how its entries were cut
+ * into calls by at most a power of two and the subnormals' rounding.  Infinities saturate,
+ * NaN is stored as NaN.  Blocks that two sequences share must not receive entries. */
+PIPO_API pipo_status pipo_op_kv_append8(const pipo_paged8 *c, int32_t n_tokens, int32_t in_dtype, const void *d_q,
+                                        int64_t ld_q, const void *d_k, int64_t ld_k, const void *d_v, int64_t ld_v,
+                                        const void *d_q_gain, const void *d_k_gain, float eps, const float *d_rope,
+                                        int32_t n_rope, void *d_q_out, void *stream);
+
+/* Causal attention over an 8-bit cache, as pipo_op_attn_paged, with scratch of
+ * pipo_op_attn_paged8_scratch(c, n_tokens) bytes.  Scores, softmax and sums are fp32. */
+PIPO_API pipo_status pipo_op_attn_paged8(const pipo_paged8 *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
+                                         float scale, int32_t window, void *d_out, int64_t ld_out, void *d_scratch,
+                                         size_t scratch_bytes, void *stream);
+
+/* Scratch bytes of pipo_op_attn_paged8 on the current device (0 for arguments it
+ * rejects or when no device is usable). */
+PIPO_API size_t pipo_op_attn_paged8_scratch(const pipo_paged8 *c, int32_t n_tokens);
+
+/* ---- block tables ----------------------------------------------------------
+ * Which blocks the sequences of a paged cache (either kind) hold, kept on the
+ * device.  `free_blocks` is a stack: its first *n_free entries are the blocks that nobody
+ * holds.  Sequence b holds the blocks table[b][0 .. held[b]-1]. */
+typedef struct {
+    int32_t n_blocks;    /* blocks of the pools, at most 2^25 - 1 */
+    int32_t max_pages;   /* row length of the table */
+    int32_t batch;       /* sequences, at most 4096 */
+    int32_t *table;        /* [batch][max_pages] */
+    int32_t *held;         /* [batch] pages */
+    int32_t *free_blocks;  /* [n_blocks] */
+    int32_t *n_free;       /* [1] */
+} pipo_page_tables;
+
+/* The tables of a step in one call.  Sequence b keeps its first d_kept[b] entries (fewer than
+ * it holds after rejected drafts, 0 when it has ended) and gets d_added[b] new
+ * tokens (negative counts as 0).  Blocks past the kept entries go back onto the stack, in the order of the
+ * sequences and pages; then b is served if its row has room, and the stack has the blocks
+ * and n_tokens the room that all sequences up to b (but those without room in their row) ask for;
+ * a sequence that needs no new block waits for tokens only.  The blocks handed out are
+ * the last ones on the stack, in order, so that the same call on its own result changes nothing.
+ * Pages given back and not handed out again are -1 in the table.
+ *   d_kv_len[b]      entries of b with its new ones (d_kept[b] alone if it was not served);
+ *   d_q_start[b]     rows of the tokens before b's, [batch + 1]: the difference is
+ *                    d_added[b], or 0 for a sequence that was not served;
+ *   d_slots[t]       block * 64 + slot of token row t, [n_tokens], -1 behind the last;
+ *   d_positions[t]   its position, likewise.
+ * These are the q_start and kv_len of the other calls.  d_kv_len may be d_kept.  Nothing is shared
+ * between sequences: a block has one holder.  EINVAL for bad sizes or pointers; batch 0 is
+ * a no-op.  Enqueued on `stream`, capturable, nothing allocated. */
+PIPO_API pipo_status pipo_op_page_tables(const pipo_page_tables *p, const int32_t *d_kept, const int32_t *d_added,
+                                         int32_t n_tokens, int32_t *d_q_start, int32_t *d_kv_len, int32_t *d_slots,
+                                         int32_t *d_positions, void *stream);
+
+/* ---- verification of drafted tokens -----------------------------------------
+ * Drafts of sequence b are d_drafted[d_start[b] .. d_start[b+1]-1] (none is allowed; more than
+ * width - 1 are cut off), with a random number in [0, 1) each, d_u, the draft's
+ * probabilities d_draft (row i: of draft i; NULL: the drafts were taken greedily, probability
+ * one) and the target's d_target: rows d_start[b] + b + i for draft i, and one more for the
+ * token behind the last draft, n_drafted + batch in all.  Both fp32 (dtype 0) or bf16 (1),
+ * rows ld elements apart, vocab (at most 2^19) values each.
+ * Draft i is kept if all before it are and d_u[i] q(token) < p(token) (products in
+ * 64 bits; a token outside the vocabulary is not kept).  One token more is drawn with
+ * d_r[b] in [0, 1): from max(p - q, 0) (greedy: p without the drafted token) at the first draft
+ * that is not kept, or from the target's last row: the first token whose running weight exceeds
+ * floor(r W), W the weight of all.  A weight is the probability (a fp32 difference) rounded to
+ * a multiple of 2^-44, below 0 or NaN as 0, above 1 as 1; rows need not add up to one.  If
+ * nothing is left of p - q, p itself is drawn from; if that has no weight, the last id is taken.
+ * d_tokens[batch][width] gets the kept drafts, the drawn token, and -1 behind;
+ * d_count[b] how many there are (kept + 1).  The same inputs give the same tokens.
+ * d_start must not decrease (it is clamped to [0, n_drafted]).  At most 65536 sequences.
+ * EINVAL for bad sizes, strides or pointers; batch 0 is a no-op.  Enqueued on `stream`, capturable,
+ * nothing allocated, no host synchronisation. */
+PIPO_API pipo_status pipo_op_verify_drafts(int32_t dtype, int32_t vocab, int32_t batch, int32_t n_drafted,
+                                           const void *d_target, int64_t ld_target, const void *d_draft,
+                                           int64_t ld_draft, const int32_t *d_drafted, const int32_t *d_start,
+                                           const float *d_u, const float *d_r, int32_t width, int32_t *d_tokens,
+                                           int32_t *d_count, void *stream);
+
 /* Whether a device-side wait of the calls above has given up since the last
  * check (their outputs are then incomplete): synchronises the current device, reads and clears
  * the error word.  PIPO_ECUDA with the wait site in the message, else PIPO_OK.

@@ -16,9 +16,10 @@ INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libpipo.so")
 # the host code first (the longest units start first)
-SOURCES = ["k_gemv_bf16.cu", "k_gemv_f32.cu", "k_attn.cu", "pipo_capi.cu", "k_tc.cu"]
+SOURCES = ["k_gemv_bf16.cu", "k_gemv_f32.cu", "k_attn.cu", "pipo_capi.cu", "k_tc.cu",
+           "k_verify.cu"]
 # the operators on caller-owned paged caches
-PAGED_SOURCES = ["paged/k_paged.cu", "paged/k_paged_tc.cu", "paged/paged_capi.cu"]
+PAGED_SOURCES = ["paged/k_paged.cu", "paged/k_paged8.cu", "paged/k_paged_tc.cu", "paged/paged_capi.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

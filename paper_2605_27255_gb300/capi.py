@@ -75,7 +75,21 @@ class pipo_paged(C.Structure):
                [(n, C.c_void_p) for n in ("k", "v", "means", "table", "q_start", "kv_len")]
 
 
+class pipo_paged8(C.Structure):
+    """The same in 8 bits, with a scale for every block and kv head."""
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_blocks", "max_pages",
+                                         "batch")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "q_start", "kv_len")]
+
+
+class pipo_page_tables(C.Structure):
+    """Block tables and the stack of free blocks (include/pipo.h); pointers are device addresses."""
+    _fields_ = [(n, C.c_int32) for n in ("n_blocks", "max_pages", "batch")] + \
+               [(n, C.c_void_p) for n in ("table", "held", "free_blocks", "n_free")]
+
+
 _PG = C.POINTER(pipo_paged)
+_PG8 = C.POINTER(pipo_paged8)
 
 # name -> (restype, argtypes): every entry point declared in include/pipo.h
 SIGNATURES = {
@@ -123,6 +137,17 @@ SIGNATURES = {
     "pipo_op_attn_pages": (C.c_int, [_PG, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int32,
                                      C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t,
                                      C.c_void_p]),
+    "pipo_op_kv_append8": (C.c_int, [_PG8, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                     C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int32,
+                                     C.c_void_p, C.c_void_p]),
+    "pipo_op_attn_paged8": (C.c_int, [_PG8, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_int32, C.c_void_p,
+                                      C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "pipo_op_attn_paged8_scratch": (C.c_size_t, [_PG8, C.c_int32]),
+    "pipo_op_page_tables": (C.c_int, [C.POINTER(pipo_page_tables), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "pipo_op_verify_drafts": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
+                                        C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                        C.c_void_p, C.c_void_p, C.c_void_p]),
     "pipo_op_paged_check": (C.c_int, [C.POINTER(C.c_uint32)]),
     "pipo_describe_step": (C.c_int, [C.c_void_p, C.c_char_p, C.c_size_t]),
     "pipo_replay_family": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_double), _IP]),
@@ -386,6 +411,43 @@ def pipo_op_attn_pages(c: pipo_paged, n_tokens: int, q: int, ld_q: int, scale: f
     _check(load().pipo_op_attn_pages(c, n_tokens, q or None, ld_q, scale, scores or None, n_top, n_sink, n_local,
                                      out or None, ld_out, pages or None, scratch or None, scratch_bytes,
                                      stream or None), None)
+
+
+def pipo_op_kv_append8(c: pipo_paged8, n_tokens: int, in_dtype: int, q: int, ld_q: int, k: int, ld_k: int, v: int,
+                       ld_v: int, q_gain: int, k_gain: int, eps: float, rope: int, n_rope: int, q_out: int,
+                       stream: int = 0) -> None:
+    """Norm, rotation and append of new tokens to an 8-bit cache; see include/pipo.h."""
+    _check(load().pipo_op_kv_append8(c, n_tokens, in_dtype, q or None, ld_q, k or None, ld_k, v or None, ld_v,
+                                     q_gain or None, k_gain or None, eps, rope or None, n_rope, q_out or None,
+                                     stream or None), None)
+
+
+def pipo_op_attn_paged8_scratch(c: pipo_paged8, n_tokens: int) -> int:
+    """Scratch bytes of pipo_op_attn_paged8 (0: rejected arguments)."""
+    return load().pipo_op_attn_paged8_scratch(c, n_tokens)
+
+
+def pipo_op_attn_paged8(c: pipo_paged8, n_tokens: int, q: int, ld_q: int, scale: float, window: int, out: int,
+                        ld_out: int, scratch: int, scratch_bytes: int, stream: int = 0) -> None:
+    """Causal attention of new tokens over an 8-bit cache; see include/pipo.h."""
+    _check(load().pipo_op_attn_paged8(c, n_tokens, q or None, ld_q, scale, window, out or None, ld_out,
+                                      scratch or None, scratch_bytes, stream or None), None)
+
+
+def pipo_op_page_tables(p: pipo_page_tables, kept: int, added: int, n_tokens: int, q_start: int, kv_len: int,
+                        slots: int, positions: int, stream: int = 0) -> None:
+    """Block tables, lengths and slots of a step; see include/pipo.h."""
+    _check(load().pipo_op_page_tables(p, kept or None, added or None, n_tokens, q_start or None, kv_len or None,
+                                      slots or None, positions or None, stream or None), None)
+
+
+def pipo_op_verify_drafts(dtype: int, vocab: int, batch: int, n_drafted: int, target: int, ld_target: int, draft: int,
+                          ld_draft: int, drafted: int, start: int, u: int, r: int, width: int, tokens: int, count: int,
+                          stream: int = 0) -> None:
+    """Drafted tokens against the target's probabilities; see include/pipo.h."""
+    _check(load().pipo_op_verify_drafts(dtype, vocab, batch, n_drafted, target or None, ld_target, draft or None,
+                                        ld_draft, drafted or None, start or None, u or None, r or None, width,
+                                        tokens or None, count or None, stream or None), None)
 
 
 def pipo_op_paged_check():

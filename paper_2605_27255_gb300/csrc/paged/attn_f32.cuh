@@ -38,19 +38,6 @@ __host__ __device__ constexpr int af_ctas(int dh, int rt) {
     return 227 * 1024 / (int)(af_smem(dh, rt) + 2048) < 4 ? 227 * 1024 / (int)(af_smem(dh, rt) + 2048) : 4;
 }
 
-// 16 bytes from global to shared memory, or zeros
-__device__ __forceinline__ void cp_async16(float* dst, const float* src, bool take) {
-    const uint32_t n = take ? 16u : 0u;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
-                 "r"(n)
-                 : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // 64 rows: threads as 16 x 16, thread (ty, tx) has the scores of rows ty + 16 r and entries
 // tx + 16 i, and rows ty + 16 r and dims 4 tx + 64 c of the output: 64 multiply-adds per 8 shared
 // loads.  Four chunks of 500 tokens up to entry 1000, 16 query and 4 kv heads of 64, 310 us: 20

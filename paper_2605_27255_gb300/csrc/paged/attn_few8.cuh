@@ -1,0 +1,416 @@
+// Attention of few rows per sequence over a paged cache of e4m3 codes.
+//
+// out = softmax(scale q . (s_k c_k)) (s_v c_v) for row tiles of 8 NT rows (tokens times the
+// query heads of one kv head).  With few rows the cache's bytes are the time, so codes go from
+// the copies' shared memory to registers once and become MMA operands there (mma.sync, fp16
+// with fp32 sums: an e4m3 code is an fp16 number), without a detour through an fp16
+// tile.  Entries and dims are the MMAs' rows, so that the few queries fill its 8 columns:
+//   S^T = C_k Q^T   16 entries x 8 rows, a step of 16 dims each; which dims a step takes is
+//                   free as long as both sides agree, so a lane reads 16 bytes of an entry
+//                   at a time;
+//   O^T += C_v^T P^T  16 dims x 8 rows; a lane reads 16 dims of four entries and pairs the
+//                   entries' bytes.  P^T comes from S^T's registers by movmatrix.
+// The queries are scaled by a power of two per row to fp16 (bf16's digits fit; what is below
+// 2^-24 of a row's largest is lost), scores get it back with the block's scale in fp32.  The values'
+// scales go into the weights, relative to the largest one so far: weights stay in
+// [0, 1] and keep fp16's 11 digits (2^-25 below 2^-14).
+//
+// A warp takes 16 entries of a 128-entry unit, with its own ring of copies, running maximum
+// and output; warps meet only at the end of an item, where their outputs are joined in
+// order.  Nothing waits on anything but its own copies.
+//
+// The pieces of work and the joining of shared items are those of work.cuh.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "codes.cuh"
+#include "work.cuh"
+
+namespace pipo {
+
+constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
+
+__host__ __device__ constexpr int few_ctas(int nt) { return nt <= 2 ? 2 : 1; }    // of an SM
+__host__ __device__ constexpr int few_stages(int nt) { return nt == 1 ? 3 : nt == 2 ? 2 : 4; }
+__host__ __device__ constexpr int few_stage_bytes(int dh) { return 2 * 16 * dh; }  // 16 entries' keys and values
+__host__ __device__ constexpr int few_ring_bytes(int dh, int nt) { return kFewWarps * few_stages(nt) * few_stage_bytes(dh); }
+__host__ __device__ constexpr int few_q_bytes(int dh, int nt) { return nt * 8 * dh * 2; }
+// half of the warps' outputs and their (maximum, sum); the 16-byte chunks of a row are swizzled by it
+__host__ __device__ constexpr int few_join_bytes(int dh, int nt) { return kFewWarps / 2 * nt * 8 * (dh + 2) * 4; }
+template <int DH>
+__device__ __forceinline__ int few_join_at(int r, int chunk) { return r * DH + ((chunk ^ ((r >> 1) & 3)) << 2); }
+__host__ __device__ constexpr size_t few_smem(int dh, int nt, int batch) {
+    const size_t n = (size_t)few_ring_bytes(dh, nt) + few_join_bytes(dh, nt) + (nt > 1 ? few_q_bytes(dh, nt) : 0);
+    const size_t find = ((size_t)find_ints(batch) * 4 + 15) / 16 * 16;
+    return n > find ? n : find;
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// byte offsets of 16-byte chunk c of entry r (0 .. 15) in a stage's keys or values: swizzled so that the
+// lanes' reads hit different banks (keys: lanes take neighbouring entries; values: every other one)
+template <int DH>
+__device__ __forceinline__ uint32_t few_k_off(int r, int c) {
+    return DH == 128 ? (uint32_t)(r * 128 + ((c ^ ((r & 1) << 2)) << 4)) : (uint32_t)(r * 64 + (c << 4));
+}
+template <int DH>
+__device__ __forceinline__ uint32_t few_v_off(int r, int c) {
+    return DH == 128 ? (uint32_t)(r * 128 + ((c ^ (r & 6)) << 4)) : (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+}
+
+template <int DH, int NT>
+__global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(AttnPagedArgs p, ItemShape shape, int S,
+                                                                             int part_rows, size_t part_off) {
+    constexpr int ST = few_stages(NT), SB = few_stage_bytes(DH), KS = DH / 16, MT = DH / 16, ROWS = 8 * NT;
+    constexpr int NC = 16 * DH / 16 / 32;  // 16-byte chunks of a lane, of a stage's keys or values
+    extern __shared__ __align__(128) unsigned char few_raw[];
+    __shared__ Piece piece[1];
+    __shared__ float row_scale[ROWS];
+    __shared__ float scales[kFewWarps][ST][2];  // of the block that a stage holds: keys', values'
+    unsigned char* ring = few_raw;
+    float* join_s = reinterpret_cast<float*>(few_raw + few_ring_bytes(DH, NT));
+    // queries in the order of the MMAs' registers; with one column tile they pass through the joining memory
+    uint2* q_s = reinterpret_cast<uint2*>(few_raw + few_ring_bytes(DH, NT) + (NT > 1 ? few_join_bytes(DH, NT) : 0));
+    const PagedArgs& c = p.c;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane >> 2, tig = lane & 3;
+    const int me = (int)blockIdx.x;
+    pdl_wait();
+    find_pieces<kFewThreads, 1>(c, shape, me, S, reinterpret_cast<int*>(few_raw), piece);
+    pdl_launch();
+    if (threadIdx.x == 0) reinterpret_cast<SharedItem*>(p.scratch)[me] = {0, 0, 0, -1};
+    __syncthreads();
+
+    const float c2 = p.scale * 1.4426950408889634f;  // exponents of two
+    unsigned char* mine_s = ring + (size_t)warp * ST * SB;
+
+    // ---- copies: this warp's 16 entries of unit lu of item ld
+    ItemWalk ld;
+    ld.start(c, shape, piece[0]);
+    int lu = ld.kv0, held = lu - 32, blocks = -1, slot_in = 0;  // lane l has the block of unit held + l
+    auto issue = [&]() {
+        if (ld.more()) {
+            const int first = first_seen(shape, ld.n, ld.len, ld.tile);
+            if (lu >= held + 32) {
+                held = lu;
+                const int page = (ld.t0 + lu + lane) * 2 + (warp >> 2);
+                blocks = lu + lane < ld.kv1 && (long long)page * kPage < ld.len && page >= first / kPage
+                             ? page_block(c, ld.b, page)
+                             : -1;
+            }
+            const int blk = __shfl_sync(0xffffffffu, blocks, lu - held);
+            const int e0 = (ld.t0 + lu) * kTileEnt + warp * 16;
+            const size_t head = (size_t)max(blk, 0) * c.n_kv + ld.g;
+            const size_t off = (head * kPage + (warp & 3) * 16) * DH;
+            unsigned char* dst = mine_s + slot_in * SB;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const int id = i * 32 + lane, r = id / (DH / 16), ch = id % (DH / 16), e = e0 + r;
+                const bool take = blk >= 0 && e >= first && e < ld.len;
+                cp_async16(dst + few_k_off<DH>(r, ch), static_cast<const uint8_t*>(c.k) + off + r * DH + ch * 16, take);
+                cp_async16(dst + 16 * DH + few_v_off<DH>(r, ch), static_cast<const uint8_t*>(c.v) + off + r * DH + ch * 16, take);
+            }
+            if (lane < 2) {
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&scales[warp][slot_in][lane]), nb = blk >= 0 ? 4u : 0u;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"((lane ? p.v_scale : p.k_scale) + head),
+                             "r"(nb)
+                             : "memory");
+            }
+            if (++lu == ld.kv1) {
+                ld.next(c, shape);
+                lu = ld.kv0;
+                held = lu - 32;
+            }
+        }
+        cp_async_commit();
+        slot_in = slot_in + 1 == ST ? 0 : slot_in + 1;
+    };
+#pragma unroll 1
+    for (int i = 0; i < ST - 1; ++i) issue();
+
+    ItemWalk it;
+    it.start(c, shape, piece[0]);
+    int slot = 0;
+    while (it.more()) {
+        const int rows = it.tokens(shape) * c.G, i0 = it.tile * shape.TP;
+        // ---- queries: a warp per row, four dims a lane
+        for (int r = warp; r < ROWS; r += kFewWarps) {
+            float x[4] = {0.f, 0.f, 0.f, 0.f}, most = 0.f;
+            if (r < rows && lane < DH / 4) {
+                const int t = r / c.G;
+                load_f<bf16_t, 4>(static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + i0 + t) * p.ld_q +
+                                      (size_t)(it.g * c.G + r - t * c.G) * DH + lane * 4,
+                                  x);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, finite_abs(x[i]));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            // 2^e with the largest magnitude in [2^e, 2^(e+1)) (e at least -126, so that 1 / 2^e is a number)
+            const float s = __uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), f = 1.f / s;
+            if (lane == 0) row_scale[r] = s;
+            if (lane < DH / 4) {  // dims 4 lane ..: chunk lane / 4, word lane % 4 of it
+                const int step = (lane >> 4) * 4 + (lane & 3), quad = (lane >> 2) & 3;
+                q_s[((r >> 3) * KS + step) * 32 + (r & 7) * 4 + quad] = make_uint2(half2_of(x[0] * f, x[1] * f), half2_of(x[2] * f, x[3] * f));
+            }
+        }
+        __syncthreads();
+        uint2 qf[NT == 1 ? KS : 1];
+        if (NT == 1) {
+#pragma unroll
+            for (int i = 0; i < KS; ++i) qf[i] = q_s[i * 32 + lane];
+        }
+        // ---- this lane's rows: 2 tig and 2 tig + 1 of every column tile
+        float cs[NT][2], m[NT][2], l[NT][2], o[NT][MT][4];
+        int pos[NT][2], lo[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = min(t * 8 + 2 * tig + h, rows - 1);
+                cs[t][h] = c2 * row_scale[t * 8 + 2 * tig + h];
+                pos[t][h] = it.len - it.n + i0 + r / c.G;
+                lo[t][h] = p.window > 0 ? pos[t][h] - p.window + 1 : 0;
+                m[t][h] = -INFINITY;
+                l[t][h] = 0.f;
+            }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
+        // entries that every row sees: all before `free_to`, from `free_from` on
+        const int free_to = it.len - it.n + i0 + 1;
+        const int free_from = p.window > 0 ? it.len - it.n + i0 + it.tokens(shape) - p.window : 0;
+        float v_ref = 0.f, v_inv = 0.f;  // the largest value scale so far
+        for (int u = it.kv0; u < it.kv1; ++u) {
+            cp_async_wait<ST - 2>();
+            __syncwarp();
+            issue();
+            const unsigned char* ks_s = mine_s + slot * SB;
+            const unsigned char* vs_s = ks_s + 16 * DH;
+            const float k_scale = scales[warp][slot][0], v_scale = scales[warp][slot][1];
+            slot = slot + 1 == ST ? 0 : slot + 1;
+            const int e0 = (it.t0 + u) * kTileEnt + warp * 16;
+            float s[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
+#pragma unroll
+            for (int half = 0; half < DH / 64; ++half) {
+                const uint4 ka = *reinterpret_cast<const uint4*>(ks_s + few_k_off<DH>(grp, tig + 4 * half));
+                const uint4 kb = *reinterpret_cast<const uint4*>(ks_s + few_k_off<DH>(grp + 8, tig + 4 * half));
+                const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a0 = decode_lo(wa[i]), a1 = decode_lo(wb[i]), a2 = decode_hi(wa[i]), a3 = decode_hi(wb[i]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint2 q = NT == 1 ? qf[NT == 1 ? half * 4 + i : 0] : q_s[(t * KS + half * 4 + i) * 32 + lane];
+                        mma_f16(s[t], a0, a1, a2, a3, q.x, q.y);
+                    }
+                }
+            }
+            // ---- softmax: s[t][0], s[t][1] are entry grp's scores for the lane's two rows, [2], [3] entry grp + 8's
+            const bool edge = e0 + 16 > free_to || e0 < free_from;
+            float top[NT][2];
+            bool move = v_scale > v_ref;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float f = cs[t][h] * k_scale;
+                    s[t][h] *= f;
+                    s[t][2 + h] *= f;
+                    if (edge) {
+                        if (e0 + grp > pos[t][h] || e0 + grp < lo[t][h]) s[t][h] = -INFINITY;
+                        if (e0 + grp + 8 > pos[t][h] || e0 + grp + 8 < lo[t][h]) s[t][2 + h] = -INFINITY;
+                    }
+                    float x = fmaxf(s[t][h], s[t][2 + h]);
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+                    top[t][h] = x;
+                    move |= x > m[t][h];
+                }
+            if (__any_sync(0xffffffffu, move)) {
+                const float v_new = fmaxf(v_ref, v_scale), fv = v_ref > 0.f ? v_ref / v_new : 0.f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float now = fmaxf(m[t][h], top[t][h]);
+                        const float f = now == -INFINITY ? 1.f : exp2f(m[t][h] - now);
+                        m[t][h] = now;
+                        l[t][h] *= f;
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) {
+                            o[t][i][h] *= f * fv;
+                            o[t][i][2 + h] *= f * fv;
+                        }
+                    }
+                v_ref = v_new;
+                v_inv = v_new > 0.f ? 1.f / v_new : 0.f;
+            }
+            const float vr = v_scale * v_inv;
+            uint32_t pb[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float w[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float ref = m[t][h] == -INFINITY ? 0.f : m[t][h];
+                    w[h] = exp2f(s[t][h] - ref);
+                    w[2 + h] = exp2f(s[t][2 + h] - ref);
+                    l[t][h] += w[h] + w[2 + h];
+                }
+                pb[t][0] = turn8x8(half2_of(w[0] * vr, w[1] * vr));
+                pb[t][1] = turn8x8(half2_of(w[2] * vr, w[3] * vr));
+            }
+            // ---- values: dims 16 grp .. (8 grp .. for 64) of entries 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9
+            uint32_t v[4][DH / 32];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 2 * tig + (e & 1) + (e >> 1) * 8;
+                if (DH == 128) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(vs_s + few_v_off<DH>(r, grp));
+                    v[e][0] = x.x;
+                    v[e][1] = x.y;
+                    v[e][DH / 32 - 2] = x.z;
+                    v[e][DH / 32 - 1] = x.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(vs_s + few_v_off<DH>(r, grp >> 1) + (grp & 1) * 8);
+                    v[e][0] = x.x;
+                    v[e][1] = x.y;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < DH / 32; ++i) {
+                // bytes of two entries side by side: (dim 0, dim 1), (dim 2, dim 3)
+                const uint32_t x0 = __byte_perm(v[0][i], v[1][i], 0x5140), x1 = __byte_perm(v[0][i], v[1][i], 0x7362);
+                const uint32_t y0 = __byte_perm(v[2][i], v[3][i], 0x5140), y1 = __byte_perm(v[2][i], v[3][i], 0x7362);
+                const uint32_t a0 = decode_lo(x0), a1 = decode_hi(x0), a2 = decode_lo(y0), a3 = decode_hi(y0);
+                const uint32_t b0 = decode_lo(x1), b1 = decode_hi(x1), b2 = decode_lo(y1), b3 = decode_hi(y1);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    mma_f16(o[t][2 * i], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+                    mma_f16(o[t][2 * i + 1], b0, b1, b2, b3, pb[t][0], pb[t][1]);
+                }
+            }
+        }
+        // ---- the warps' outputs, joined: warps 4 .. 7 hand theirs to 0 .. 3, whose four are added up in order
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int w = 4; w < 32; w <<= 1) l[t][h] += __shfl_xor_sync(0xffffffffu, l[t][h], w);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    o[t][i][h] *= v_ref;
+                    o[t][i][2 + h] *= v_ref;
+                }
+            }
+        float* my_o = join_s + (size_t)(warp & 3) * ROWS * DH;
+        float* my_ml = join_s + (size_t)(kFewWarps / 2) * ROWS * DH + (warp & 3) * ROWS * 2;
+        auto leave = [&]() {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = t * 8 + 2 * tig + h;
+#pragma unroll
+                    for (int i = 0; i < MT; i += 2)  // four dims: (i, 0), (i, 2), (i + 1, 0), (i + 1, 2)
+                        *reinterpret_cast<float4*>(my_o + few_join_at<DH>(r, grp * (MT / 2) + i / 2)) =
+                            make_float4(o[t][i][h], o[t][i][2 + h], o[t][i + 1][h], o[t][i + 1][2 + h]);
+                    if (grp == 0) *reinterpret_cast<float2*>(my_ml + 2 * r) = make_float2(m[t][h], l[t][h]);
+                }
+        };
+        if (NT == 1) __syncthreads();  // (every warp has its queries out of the joining memory)
+        if (warp >= 4) leave();
+        __syncthreads();
+        if (warp < 4) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = t * 8 + 2 * tig + h;
+                    const float2 e = *reinterpret_cast<const float2*>(my_ml + 2 * r);
+                    const float now = fmaxf(m[t][h], e.x), ref = now == -INFINITY ? 0.f : now;
+                    const float f = exp2f(m[t][h] - ref), w = exp2f(e.x - ref);
+                    m[t][h] = now;
+                    l[t][h] = l[t][h] * f + e.y * w;
+#pragma unroll
+                    for (int i = 0; i < MT; i += 2) {
+                        const float4 x = *reinterpret_cast<const float4*>(my_o + few_join_at<DH>(r, grp * (MT / 2) + i / 2));
+                        o[t][i][h] = o[t][i][h] * f + x.x * w;
+                        o[t][i][2 + h] = o[t][i][2 + h] * f + x.y * w;
+                        o[t][i + 1][h] = o[t][i + 1][h] * f + x.z * w;
+                        o[t][i + 1][2 + h] = o[t][i + 1][2 + h] * f + x.w * w;
+                    }
+                }
+            __syncwarp();
+            leave();
+        }
+        __syncthreads();
+        const bool whole = it.whole();
+        float* part = reinterpret_cast<float*>(p.scratch + part_off) + ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
+        if (it.begun() && threadIdx.x == 0)
+            reinterpret_cast<SharedItem*>(p.scratch)[me] = {it.q0 + i0, rows, it.g, it.last_worker(piece[0])};
+        const float* ml = join_s + (size_t)(kFewWarps / 2) * ROWS * DH;
+        for (int i = threadIdx.x; i < rows * (DH / 4); i += kFewThreads) {
+            const int r = i / (DH / 4), d = i % (DH / 4) * 4;
+            float2 e[4];
+            float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                e[w] = *reinterpret_cast<const float2*>(ml + (w * ROWS + r) * 2);
+                M = fmaxf(M, e[w].x);
+            }
+            const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = exp2f(e[w].x - ref);
+                const float4 y = *reinterpret_cast<const float4*>(join_s + (size_t)w * ROWS * DH + few_join_at<DH>(r, d / 4));
+                L += e[w].y * f;
+                x[0] += y.x * f;
+                x[1] += y.y * f;
+                x[2] += y.z * f;
+                x[3] += y.w * f;
+            }
+            if (whole) {
+                const float inv = L > 0.f ? 1.f / L : 0.f;
+                const int t = r / c.G;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] *= inv;
+                store_f<bf16_t, 4>(static_cast<bf16_t*>(p.out) + (size_t)(it.q0 + i0 + t) * p.ld_out +
+                                       (size_t)(it.g * c.G + r - t * c.G) * DH + d,
+                                   x);
+            } else {
+                *reinterpret_cast<float4*>(part + ((size_t)(d / 4) * part_rows + r) * 4) = make_float4(x[0], x[1], x[2], x[3]);
+                if (d == 0) *reinterpret_cast<float2*>(part + (size_t)part_rows * DH + 2 * r) = make_float2(M, L);
+            }
+        }
+        it.next(c, shape);
+        __syncthreads();  // the joining memory is read
+    }
+    cp_async_wait<0>();
+}
+
+}  // namespace pipo

@@ -1,0 +1,82 @@
+// Operators on caches of e4m3 codes, and block tables (a translation unit of its own).
+#include "append8.cuh"
+#include "attn_few8.cuh"
+#include "tables.cuh"
+
+namespace pipo {
+
+namespace {
+
+unsigned ceil_div(long long a, long long b) { return (unsigned)((a + b - 1) / b); }
+
+template <int DH>
+cudaError_t append8_as(const AppendArgs& a, cudaStream_t s) {
+    // pages that receive entries: a sequence with n new tokens spans at most n / 64 + 2
+    const long long t = a.c.n_tokens, most = t / kPage + 2LL * a.c.batch, runs = t < most ? t : most;
+    const int pages = (int)(runs * a.c.n_kv);
+    const dim3 grid(pages + (a.q_out ? ceil_div(t, kAppendWarps) : 0));
+    return a.in_bf16 ? launch_pdl(&kv_append8_kernel<DH, bf16_t>, grid, kAppendWarps * 32, 0, s, a, pages)
+                     : launch_pdl(&kv_append8_kernel<DH, float>, grid, kAppendWarps * 32, 0, s, a, pages);
+}
+
+template <int DH, int NT>
+cudaError_t few8_as(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
+    auto* fn = &attn_few8_kernel<DH, NT>;
+    static thread_local int ready = -1;  // the shared-memory limit is set per device
+    if (ready != pl.dev) {
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)few_smem(DH, NT, kPagedMaxBatch));
+        if (e != cudaSuccess) return e;
+        ready = pl.dev;
+    }
+    const ItemShape shape{pl.TP, a.window, 0};
+    const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kFewThreads, few_smem(DH, NT, a.c.batch), s, a, shape,
+                                     pl.workers, pl.part_rows, pl.part_off);
+    return e == cudaSuccess ? launch_combine<DH, bf16_t>(a, pl, s) : e;
+}
+
+}  // namespace
+
+cudaError_t launch_kv_append8(const AppendArgs& a, cudaStream_t s) {
+    return a.c.dh == 64 ? append8_as<64>(a, s) : append8_as<128>(a, s);
+}
+
+// The plan of attention over 8-bit pools: row tiles of 8, 16 or 32 rows by the rows (new tokens times query
+// heads of a kv head) that the batch's sequences have on average.
+AttnPlan plan_attn8(const PagedArgs& c, int dev, int sms) {
+    AttnPlan pl{};
+    pl.dev = dev;
+    const long long mine = (long long)c.n_tokens * c.G;
+    pl.rt = c.G <= 8 && mine <= 8LL * c.batch ? 1 : mine <= 16LL * c.batch ? 2 : 4;
+    pl.TP = 8 * pl.rt / c.G;
+    pl.tiles = tiles_bound(c.n_tokens, c.batch, pl.TP);
+    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each, all = (long long)sms * few_ctas(pl.rt);
+    pl.workers = pl.ctas = (int)(most < all ? most : all);
+    pl.join = each > 1;
+    pl.part_rows = (int)(mine < (long long)pl.TP * c.G ? mine : (long long)pl.TP * c.G);
+    pl.part_rows += pl.part_rows & 1;
+    pl.part_off = record_bytes(pl.workers);
+    pl.bits_off = pl.scratch = pl.part_off + (size_t)pl.workers * 2 * part_floats(pl.part_rows, c.dh) * sizeof(float);
+    return pl;
+}
+
+cudaError_t launch_attn_few8(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) {
+    if (a.c.dh == 64) return pl.rt == 1 ? few8_as<64, 1>(a, pl, s) : pl.rt == 2 ? few8_as<64, 2>(a, pl, s) : few8_as<64, 4>(a, pl, s);
+    return pl.rt == 1 ? few8_as<128, 1>(a, pl, s) : pl.rt == 2 ? few8_as<128, 2>(a, pl, s) : few8_as<128, 4>(a, pl, s);
+}
+
+cudaError_t launch_page_tables(const TablesArgs& a, cudaStream_t s) {
+    static thread_local int ready = -1;  // the shared-memory limit is set per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && ready != dev) {
+        e = cudaFuncSetAttribute(&page_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tables_smem(kPagedMaxBatch));
+        if (e == cudaSuccess) ready = dev;
+    }
+    if (e == cudaSuccess) e = launch_pdl(&page_tables_kernel, dim3(1), kTabThreads, tables_smem(a.batch), s, a);
+    if (e == cudaSuccess && a.n_tokens > kTabInline)
+        e = launch_pdl(&page_slots_kernel, dim3(ceil_div(a.n_tokens, 256)), 256, 0, s, a);
+    return e;
+}
+
+}  // namespace pipo

@@ -70,6 +70,19 @@ __device__ __forceinline__ Tok find_token(const PagedArgs& c, int t) {
     return {lo, max(-1, len - (end - t))};
 }
 
+// 16 bytes from global to shared memory, or zeros
+__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool take) {
+    const uint32_t n = take ? 16u : 0u;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+                 "r"(n)
+                 : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // a launch whose blocks may start while the kernel before ends (each waits for it before it reads)
 template <typename... P, typename... A>
 inline cudaError_t launch_pdl(void (*fn)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, const A&... args) {

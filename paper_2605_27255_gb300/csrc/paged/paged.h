@@ -31,6 +31,7 @@ struct AppendArgs {
     float eps;
     int in_bf16;
     void* q_out;                  // [n_tokens][n_q * dh] or nullptr
+    float *k_scale, *v_scale;     // 8-bit pools: [n_blocks][n_kv]
 };
 
 struct AttnPagedArgs {
@@ -45,6 +46,7 @@ struct AttnPagedArgs {
     int n_top;
     const uint32_t* bits;   // [token][n_kv][bit_words(max_pages)] the same as bits, for whole tiles, in place of the list; or nullptr
     unsigned char* scratch;
+    const float *k_scale, *v_scale;  // 8-bit pools: [n_blocks][n_kv]
 };
 
 struct ScoreArgs {
@@ -69,7 +71,7 @@ inline __host__ __device__ int bit_words(int max_pages) { return (max_pages + 31
 struct AttnPlan {
     int dev;
     bool pair;          // bf16: two 128-row tiles per item share the copies
-    int rt;             // fp32: rows of a tile / 16
+    int rt;             // fp32: rows of a tile / 16; 8-bit pools, few rows: rows of a tile / 8
     bool join;          // items may be shared between workers
     bool listed;        // selected pages: a token's own list; else whole tiles with bits
     int TP;             // tokens per row tile
@@ -82,6 +84,15 @@ struct AttnPlan {
 };
 
 AttnPlan plan_attn(const PagedArgs& c, int n_top, int dev, int sms);  // k_paged_tc.cu
+AttnPlan plan_attn8(const PagedArgs& c, int dev, int sms);            // k_paged8.cu
+
+// Block tables of a step (pipo_page_tables)
+struct TablesArgs {
+    int32_t *table, *held, *free_blocks, *n_free;
+    const int32_t *kept, *added;
+    int max_pages, n_blocks, batch, n_tokens;
+    int32_t *q_start, *kv_len, *slots, *positions;
+};
 
 // k_paged_tc.cu
 cudaError_t launch_attn_tile(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
@@ -93,5 +104,10 @@ cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t s);
 cudaError_t launch_page_scores(const ScoreArgs& a, cudaStream_t s);
 cudaError_t launch_page_select(const SelectArgs& a, cudaStream_t s);
 cudaError_t launch_attn_f32(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s);
+
+// k_paged8.cu
+cudaError_t launch_kv_append8(const AppendArgs& a, cudaStream_t s);
+cudaError_t launch_attn_few8(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s);
+cudaError_t launch_page_tables(const TablesArgs& a, cudaStream_t s);
 
 }  // namespace pipo

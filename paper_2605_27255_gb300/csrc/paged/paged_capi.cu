@@ -141,27 +141,19 @@ pipo_status run_attn(const char* who, AttnPagedArgs a, SelectArgs* sel, size_t s
     return st == PIPO_OK ? cuda_status(who, launch_attn_tile(a, pl, tk, tv, s)) : st;
 }
 
-}  // namespace
-
-extern "C" {
-
-pipo_status pipo_op_kv_append(const pipo_paged* c, int32_t n_tokens, int32_t in_dtype, const void* d_q, int64_t ld_q,
-                              const void* d_k, int64_t ld_k, const void* d_v, int64_t ld_v, const void* d_q_gain,
-                              const void* d_k_gain, float eps, const float* d_rope, int32_t n_rope, void* d_q_out,
-                              void* stream) {
-    if (!paged_ok(c, n_tokens) || (in_dtype != 0 && in_dtype != 1))
-        return fail(PIPO_EINVAL, "pipo_op_kv_append: bad cache description or token count");
-    if (c->batch == 0 || n_tokens == 0) return PIPO_OK;
+// the checked arguments of an append
+pipo_status append_args(const char* who, const pipo_paged* c, int32_t n_tokens, int32_t in_dtype, const void* d_q,
+                        int64_t ld_q, const void* d_k, int64_t ld_k, const void* d_v, int64_t ld_v, const void* d_q_gain,
+                        const void* d_k_gain, float eps, const float* d_rope, int32_t n_rope, void* d_q_out, AppendArgs* out) {
     const size_t es = in_dtype ? 2 : 4;
     const int64_t kd = (int64_t)c->n_kv_heads * c->head_dim;
     if (!batch_ok(c) || !pools_ok(c) || !rows_ok(d_k, ld_k, kd, es) || !rows_ok(d_v, ld_v, kd, es) ||
         (d_q != nullptr) != (d_q_out != nullptr) ||
         (d_q && (!rows_ok(d_q, ld_q, (int64_t)c->n_q_heads * c->head_dim, es) || !a16(d_q_out))) || !a16(c->means) ||
         !a16(d_q_gain) || !a16(d_k_gain) || !a16(d_rope) || !(eps >= 0.f) || !std::isfinite(eps))
-        return fail(PIPO_EINVAL, "pipo_op_kv_append: bad arguments");
+        return fail(PIPO_EINVAL, "%s: bad arguments", who);
     if (d_rope && (int64_t)n_rope < (int64_t)kPage * c->max_pages)
-        return fail(PIPO_EINVAL, "pipo_op_kv_append: %d rotations for %lld positions", n_rope,
-                    (long long)kPage * c->max_pages);
+        return fail(PIPO_EINVAL, "%s: %d rotations for %lld positions", who, n_rope, (long long)kPage * c->max_pages);
     AppendArgs a{};
     a.c = args_of(c, n_tokens);
     a.q = d_q;
@@ -176,6 +168,47 @@ pipo_status pipo_op_kv_append(const pipo_paged* c, int32_t n_tokens, int32_t in_
     a.eps = eps;
     a.in_bf16 = in_dtype;
     a.q_out = d_q_out;
+    *out = a;
+    return PIPO_OK;
+}
+
+// an 8-bit cache as the other calls' description (the checks of sizes are theirs)
+pipo_paged plain_of(const pipo_paged8* c) {
+    pipo_paged x{};
+    if (!c) return x;  // (page_size 0: refused)
+    x.dtype = 1;
+    x.n_q_heads = c->n_q_heads;
+    x.n_kv_heads = c->n_kv_heads;
+    x.head_dim = c->head_dim;
+    x.page_size = c->page_size;
+    x.n_blocks = c->n_blocks;
+    x.max_pages = c->max_pages;
+    x.batch = c->batch;
+    x.k = c->k;
+    x.v = c->v;
+    x.table = c->table;
+    x.q_start = c->q_start;
+    x.kv_len = c->kv_len;
+    return x;
+}
+
+bool scales_ok(const pipo_paged8* c) { return c->k_scale && c->v_scale && a4(c->k_scale) && a4(c->v_scale); }
+
+}  // namespace
+
+extern "C" {
+
+pipo_status pipo_op_kv_append(const pipo_paged* c, int32_t n_tokens, int32_t in_dtype, const void* d_q, int64_t ld_q,
+                              const void* d_k, int64_t ld_k, const void* d_v, int64_t ld_v, const void* d_q_gain,
+                              const void* d_k_gain, float eps, const float* d_rope, int32_t n_rope, void* d_q_out,
+                              void* stream) {
+    if (!paged_ok(c, n_tokens) || (in_dtype != 0 && in_dtype != 1))
+        return fail(PIPO_EINVAL, "pipo_op_kv_append: bad cache description or token count");
+    if (c->batch == 0 || n_tokens == 0) return PIPO_OK;
+    AppendArgs a{};
+    const pipo_status st = append_args("pipo_op_kv_append", c, n_tokens, in_dtype, d_q, ld_q, d_k, ld_k, d_v, ld_v, d_q_gain,
+                                       d_k_gain, eps, d_rope, n_rope, d_q_out, &a);
+    if (st != PIPO_OK) return st;
     return cuda_status("pipo_op_kv_append", launch_kv_append(a, static_cast<cudaStream_t>(stream)));
 }
 
@@ -262,6 +295,91 @@ pipo_status pipo_op_attn_pages(const pipo_paged* c, int32_t n_tokens, const void
     a.n_top = n_top;
     a.scratch = static_cast<unsigned char*>(d_scratch);
     return run_attn("pipo_op_attn_pages", a, &sel, scratch_bytes, static_cast<cudaStream_t>(stream));
+}
+
+pipo_status pipo_op_kv_append8(const pipo_paged8* c8, int32_t n_tokens, int32_t in_dtype, const void* d_q, int64_t ld_q,
+                               const void* d_k, int64_t ld_k, const void* d_v, int64_t ld_v, const void* d_q_gain,
+                               const void* d_k_gain, float eps, const float* d_rope, int32_t n_rope, void* d_q_out,
+                               void* stream) {
+    const pipo_paged desc = plain_of(c8), *c = &desc;
+    if (!paged_ok(c, n_tokens) || (in_dtype != 0 && in_dtype != 1))
+        return fail(PIPO_EINVAL, "pipo_op_kv_append8: bad cache description or token count");
+    if (c->batch == 0 || n_tokens == 0) return PIPO_OK;
+    AppendArgs a{};
+    const pipo_status st = append_args("pipo_op_kv_append8", c, n_tokens, in_dtype, d_q, ld_q, d_k, ld_k, d_v, ld_v, d_q_gain,
+                                       d_k_gain, eps, d_rope, n_rope, d_q_out, &a);
+    if (st != PIPO_OK) return st;
+    if (!scales_ok(c8)) return fail(PIPO_EINVAL, "pipo_op_kv_append8: bad scales");
+    a.k_scale = c8->k_scale;
+    a.v_scale = c8->v_scale;
+    return cuda_status("pipo_op_kv_append8", launch_kv_append8(a, static_cast<cudaStream_t>(stream)));
+}
+
+size_t pipo_op_attn_paged8_scratch(const pipo_paged8* c8, int32_t n_tokens) {
+    int dev = 0, sms = 0;
+    const pipo_paged desc = plain_of(c8), *c = &desc;
+    if (!paged_ok(c, n_tokens) || device_of(&dev, &sms) != cudaSuccess) return 0;
+    if (c->batch == 0 || n_tokens == 0) return 16;
+    return plan_attn8(args_of(c, n_tokens), dev, sms).scratch;
+}
+
+pipo_status pipo_op_attn_paged8(const pipo_paged8* c8, int32_t n_tokens, const void* d_q, int64_t ld_q, float scale,
+                                int32_t window, void* d_out, int64_t ld_out, void* d_scratch, size_t scratch_bytes,
+                                void* stream) {
+    const pipo_paged desc = plain_of(c8), *c = &desc;
+    if (!paged_ok(c, n_tokens) || window < 0)
+        return fail(PIPO_EINVAL, "pipo_op_attn_paged8: bad cache description, token count or window");
+    if (c->batch == 0 || n_tokens == 0) return PIPO_OK;
+    if (!attn_args_ok(c, n_tokens, d_q, ld_q, scale, d_out, ld_out) || !scales_ok(c8) || !d_scratch || !a16(d_scratch))
+        return fail(PIPO_EINVAL, "pipo_op_attn_paged8: bad arguments");
+    int dev = 0, sms = 0;
+    const cudaError_t e = device_of(&dev, &sms);
+    if (e != cudaSuccess) return cuda_status("pipo_op_attn_paged8", e);
+    AttnPagedArgs a{};
+    a.c = args_of(c, n_tokens);
+    const AttnPlan pl = plan_attn8(a.c, dev, sms);
+    if (scratch_bytes < pl.scratch)
+        return fail(PIPO_EINVAL, "pipo_op_attn_paged8: scratch needs %zu bytes, got %zu", pl.scratch, scratch_bytes);
+    a.q = d_q;
+    a.ld_q = ld_q;
+    a.out = d_out;
+    a.ld_out = ld_out;
+    a.scale = scale;
+    a.window = (long long)window < (long long)kPage * c->max_pages ? window : 0;
+    a.scratch = static_cast<unsigned char*>(d_scratch);
+    a.k_scale = c8->k_scale;
+    a.v_scale = c8->v_scale;
+    return cuda_status("pipo_op_attn_paged8", launch_attn_few8(a, pl, static_cast<cudaStream_t>(stream)));
+}
+
+pipo_status pipo_op_page_tables(const pipo_page_tables* p, const int32_t* d_kept, const int32_t* d_added, int32_t n_tokens,
+                                int32_t* d_q_start, int32_t* d_kv_len, int32_t* d_slots, int32_t* d_positions,
+                                void* stream) {
+    if (!p || p->batch < 0 || p->batch > kPagedMaxBatch || p->max_pages < 1 || p->max_pages > 65535 * kPage ||
+        p->n_blocks < 1 || (long long)p->n_blocks * kPage > 0x7fffffffLL || n_tokens < 0 || n_tokens > (1 << 30))
+        return fail(PIPO_EINVAL, "pipo_op_page_tables: bad sizes");
+    if (p->batch == 0) return PIPO_OK;
+    for (const void* x : {(const void*)p->table, (const void*)p->held, (const void*)p->free_blocks, (const void*)p->n_free,
+                          (const void*)d_kept, (const void*)d_added, (const void*)d_q_start, (const void*)d_kv_len})
+        if (!x || !a4(x)) return fail(PIPO_EINVAL, "pipo_op_page_tables: bad arguments");
+    if (n_tokens > 0 && (!d_slots || !d_positions || !a4(d_slots) || !a4(d_positions)))
+        return fail(PIPO_EINVAL, "pipo_op_page_tables: bad arguments");
+    TablesArgs a{};
+    a.table = p->table;
+    a.held = p->held;
+    a.free_blocks = p->free_blocks;
+    a.n_free = p->n_free;
+    a.kept = d_kept;
+    a.added = d_added;
+    a.max_pages = p->max_pages;
+    a.n_blocks = p->n_blocks;
+    a.batch = p->batch;
+    a.n_tokens = n_tokens;
+    a.q_start = d_q_start;
+    a.kv_len = d_kv_len;
+    a.slots = d_slots;
+    a.positions = d_positions;
+    return cuda_status("pipo_op_page_tables", launch_page_tables(a, static_cast<cudaStream_t>(stream)));
 }
 
 pipo_status pipo_op_paged_check(uint32_t* h_info) {

@@ -18,6 +18,13 @@ captured graph follows their values.  There is no backward pass: inputs that
 require gradients are refused unless gradients are off (``torch.no_grad``).
 Shapes and types are checked here, everything else by the library
 (``capi.PipoError``).
+
+``PagedCache8`` is the same over pools of 8-bit codes (append and attend), and
+``BlockTables`` keeps the block table itself on the device, from the sequences' lengths:
+
+    tables = BlockTables.new(batch, max_pages, n_blocks)
+    q_start, kv_len, slots, positions = tables.advance(kept, added, tokens)
+    cache = PagedCache8(k_pool, v_pool, k_scale, v_scale, tables.table, n_q=32)
 """
 from __future__ import annotations
 
@@ -52,34 +59,15 @@ def _no_backward(name: str, x: torch.Tensor) -> None:
         raise ValueError(f"{name} requires a gradient, and the paged-cache operators have none")
 
 
-class PagedCache:
-    """Pools ``k``, ``v`` [n_blocks, n_kv, 64, d_h] (bf16 or fp32), the block
-    table [batch, max_pages] (int32) and, for the page scores, the mean keys
-    ``means`` [n_blocks, n_kv, d_h] that ``append`` maintains.  The tensors stay
-    the caller's; nothing is copied.  ``attend`` and ``attend_pages`` keep a
-    scratch buffer per stream; a call that ``torch.cuda.graph`` captures takes
-    one from the graph's own pool instead, which lasts as long as the graph, so that
-    later calls, whatever their size, leave its replays alone.  Threads may
-    share an object."""
+class _Cache:
+    """What the handles share: the ragged batch's arguments, scratch, ``append`` and
+    ``attend``.  ``_c`` is the library's description, ``dtype`` the type of queries, gains
+    and outputs."""
 
-    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_q: int,
-                 means: Optional[torch.Tensor] = None):
-        if k.dtype not in _TYPES or v.dtype != k.dtype or k.dim() != 4 or k.shape != v.shape or k.shape[2] != PAGE \
-                or not k.is_contiguous() or not v.is_contiguous():
-            raise ValueError("pools must be contiguous [n_blocks, n_kv, 64, d_h] of one type (float32 or bfloat16)")
-        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
-            raise ValueError("the block table must be a contiguous int32 [batch, max_pages]")
-        if means is not None and (means.dtype != k.dtype or not means.is_contiguous() or
-                                  means.shape != (k.shape[0], k.shape[1], k.shape[3])):
-            raise ValueError("means must be contiguous [n_blocks, n_kv, d_h] of the pools' type")
-        if not k.is_cuda or any(t.device != k.device for t in (v, table) + (() if means is None else (means,))):
-            raise ValueError("pools, table and means must be on one CUDA device")
-        self.k, self.v, self.table, self.means = k, v, table, means
-        self.n_q, self.n_kv, self.d_h, self.dtype, self.device = n_q, k.shape[1], k.shape[3], k.dtype, k.device
+    def _keep(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_q: int, dtype: torch.dtype) -> None:
+        self.k, self.v, self.table = k, v, table
+        self.n_q, self.n_kv, self.d_h, self.dtype, self.device = n_q, k.shape[1], k.shape[3], dtype, k.device
         self.index = k.device.index
-        self._c = capi.pipo_paged(_TYPES[k.dtype], _int32(n_q), k.shape[1], k.shape[3], PAGE, k.shape[0],
-                                  table.shape[1], table.shape[0], k.data_ptr(), v.data_ptr(),
-                                  None if means is None else means.data_ptr(), table.data_ptr())
         self._seqs = table.shape[0]
         self._lock = threading.Lock()
         self._buffers: Dict[int, torch.Tensor] = {}  # scratch by stream
@@ -110,7 +98,7 @@ class PagedCache:
         capture it is new: the graph's pool keeps it for the replays, and calls of
         one capture take the same memory in turn."""
         if self._need_for != tokens:
-            self._need = max(capi.pipo_op_attn_paged_scratch(self._c, tokens), 16)
+            self._need = max(self._scratch_bytes(tokens), 16)
             self._need_for = tokens
         if torch.cuda.is_current_stream_capturing():
             return torch.empty(self._need, dtype=torch.uint8, device=self.device)
@@ -167,9 +155,9 @@ class PagedCache:
         p = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
         with self._lock:
             self._batch(q_start, kv_len)
-            capi.pipo_op_kv_append(self._c, tokens, _TYPES[k.dtype], p(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(),
-                                   ld_v, p(q_gain), p(k_gain), eps, p(rope), 0 if rope is None else rope.shape[0],
-                                   p(out), _raw_stream(self.index))
+            self._kv_append(tokens, _TYPES[k.dtype], p(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, p(q_gain),
+                            p(k_gain), eps, p(rope), 0 if rope is None else rope.shape[0], p(out),
+                            _raw_stream(self.index))
         return out
 
     def _out(self, q: torch.Tensor, out: Optional[torch.Tensor]) -> Tuple[torch.Tensor, int]:
@@ -195,10 +183,47 @@ class PagedCache:
         with self._lock:
             self._batch(q_start, kv_len)
             w = self._work(q.shape[0], stream)
-            capi.pipo_op_attn_paged(self._c, q.shape[0], q.data_ptr(), ld_q,
-                                    self.d_h ** -0.5 if scale is None else scale, _int32(window), out.data_ptr(),
-                                    ld_out, w.data_ptr(), w.numel(), stream)
+            self._attn(q.shape[0], q.data_ptr(), ld_q, self.d_h ** -0.5 if scale is None else scale, _int32(window),
+                       out.data_ptr(), ld_out, w.data_ptr(), w.numel(), stream)
         return out
+
+
+class PagedCache(_Cache):
+    """Pools ``k``, ``v`` [n_blocks, n_kv, 64, d_h] (bf16 or fp32), the block
+    table [batch, max_pages] (int32) and, for the page scores, the mean keys
+    ``means`` [n_blocks, n_kv, d_h] that ``append`` maintains.  The tensors stay
+    the caller's; nothing is copied.  ``attend`` and ``attend_pages`` keep a
+    scratch buffer per stream; a call that ``torch.cuda.graph`` captures takes
+    one from the graph's own pool instead, which lasts as long as the graph, so that
+    later calls, whatever their size, leave its replays alone.  Threads may
+    share an object."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_q: int,
+                 means: Optional[torch.Tensor] = None):
+        if k.dtype not in _TYPES or v.dtype != k.dtype or k.dim() != 4 or k.shape != v.shape or k.shape[2] != PAGE \
+                or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("pools must be contiguous [n_blocks, n_kv, 64, d_h] of one type (float32 or bfloat16)")
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("the block table must be a contiguous int32 [batch, max_pages]")
+        if means is not None and (means.dtype != k.dtype or not means.is_contiguous() or
+                                  means.shape != (k.shape[0], k.shape[1], k.shape[3])):
+            raise ValueError("means must be contiguous [n_blocks, n_kv, d_h] of the pools' type")
+        if not k.is_cuda or any(t.device != k.device for t in (v, table) + (() if means is None else (means,))):
+            raise ValueError("pools, table and means must be on one CUDA device")
+        self.means = means
+        self._keep(k, v, table, n_q, k.dtype)
+        self._c = capi.pipo_paged(_TYPES[k.dtype], _int32(n_q), k.shape[1], k.shape[3], PAGE, k.shape[0],
+                                  table.shape[1], table.shape[0], k.data_ptr(), v.data_ptr(),
+                                  None if means is None else means.data_ptr(), table.data_ptr())
+
+    def _scratch_bytes(self, *a) -> int:
+        return capi.pipo_op_attn_paged_scratch(self._c, *a)
+
+    def _kv_append(self, *a) -> None:
+        capi.pipo_op_kv_append(self._c, *a)
+
+    def _attn(self, *a) -> None:
+        capi.pipo_op_attn_paged(self._c, *a)
 
     def page_scores(self, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, *,
                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -249,3 +274,97 @@ class PagedCache:
                                     _int32(sink), _int32(local), out.data_ptr(), ld_out, pages.data_ptr(),
                                     w.data_ptr(), w.numel(), stream)
         return out, pages
+
+
+class PagedCache8(_Cache):
+    """The same with half the bytes: pools of e4m3 codes (``torch.float8_e4m3fn``) and scales
+    ``k_scale``, ``v_scale`` [n_blocks, n_kv] (fp32, powers of two between 2^-100 and 2^7; ``append``
+    chooses them).  An entry is its code times its block's scale.  Queries, gains and
+    outputs are bf16.  ``append`` and ``attend`` are those of ``PagedCache``; there are no page
+    scores.  ``encode`` makes pools from values."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                 table: torch.Tensor, n_q: int):
+        if k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype or k.dim() != 4 or k.shape != v.shape or \
+                k.shape[2] != PAGE or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("pools must be contiguous [n_blocks, n_kv, 64, d_h] of float8_e4m3fn")
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("the block table must be a contiguous int32 [batch, max_pages]")
+        for x in (k_scale, v_scale):
+            if x.dtype != torch.float32 or x.shape != k.shape[:2] or not x.is_contiguous():
+                raise ValueError("scales must be contiguous float32 [n_blocks, n_kv]")
+        if not k.is_cuda or any(t.device != k.device for t in (v, k_scale, v_scale, table)):
+            raise ValueError("pools, scales and table must be on one CUDA device")
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self._keep(k, v, table, n_q, torch.bfloat16)
+        self._c = capi.pipo_paged8(_int32(n_q), k.shape[1], k.shape[3], PAGE, k.shape[0], table.shape[1],
+                                   table.shape[0], k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                   table.data_ptr())
+
+    def _scratch_bytes(self, *a) -> int:
+        return capi.pipo_op_attn_paged8_scratch(self._c, *a)
+
+    def _kv_append(self, *a) -> None:
+        capi.pipo_op_kv_append8(self._c, *a)
+
+    def _attn(self, *a) -> None:
+        capi.pipo_op_attn_paged8(self._c, *a)
+
+
+def encode(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Values [blocks, heads, 64, d_h] as codes and scales of a ``PagedCache8``, as ``append`` chooses them."""
+    x = x.float()
+    most = x.abs().masked_fill(~x.isfinite(), 0).amax((2, 3))
+    e = torch.where(most > 0, torch.frexp(most)[1] - 6, -100).clamp(-100, 7)
+    scale = torch.ldexp(torch.ones_like(most), e)
+    return (x / scale[..., None, None]).clamp(-448, 448).to(torch.float8_e4m3fn), scale
+
+
+class BlockTables:
+    """Which blocks the sequences of a cache hold, kept on the device: ``table``
+    [batch, max_pages] (that of the cache's handle), pages held ``held`` [batch], the
+    stack of free blocks ``free`` [n_blocks] and how many lie on it, ``n_free`` [1], all int32.
+    ``advance`` changes them in place; calls have to follow one another on the device."""
+
+    def __init__(self, table: torch.Tensor, held: torch.Tensor, free: torch.Tensor, n_free: torch.Tensor):
+        for name, t, shape in (("table", table, None), ("held", held, table.shape[:1]), ("free", free, None),
+                               ("n_free", n_free, (1,))):
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != (2 if t is table else 1) or \
+                    (shape is not None and t.shape != shape) or t.device != table.device:
+                raise ValueError(f"{name} must be a contiguous int32 tensor of its shape on one device: table "
+                                 "[batch, max_pages], held [batch], free [n_blocks], n_free [1]")
+        if not table.is_cuda:
+            raise ValueError("block tables must be on a CUDA device")
+        self.table, self.held, self.free, self.n_free = table, held, free, n_free
+        self.device, self.index, self._seqs = table.device, table.device.index, table.shape[0]
+        self._p = capi.pipo_page_tables(free.shape[0], table.shape[1], self._seqs, table.data_ptr(), held.data_ptr(),
+                                        free.data_ptr(), n_free.data_ptr())
+
+    @classmethod
+    def new(cls, batch: int, max_pages: int, n_blocks: int, device="cuda") -> "BlockTables":
+        """Tables of sequences without entries; every block is free."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32), torch.arange(n_blocks, **i32),
+                   torch.full((1,), n_blocks, **i32))
+
+    def advance(self, kept: torch.Tensor, added: torch.Tensor, tokens: int) -> Tuple[torch.Tensor, ...]:
+        """Keep the first ``kept[b]`` entries of every sequence and make room for ``added[b]``
+        more.  Blocks past the kept entries become free, then sequences are served in order while
+        blocks, their rows and ``tokens`` token rows last.  Returns int32 ``q_start`` [batch + 1] and
+        ``kv_len`` [batch] for the cache's calls, and of every token row ``slots`` (block * 64 +
+        slot) and ``positions`` [tokens], -1 behind the last.  A sequence that was not served has no
+        rows, and ``kv_len[b]`` is ``kept[b]``."""
+        if _current_device() != self.index:
+            with torch.cuda.device(self.index):
+                return self.advance(kept, added, tokens)
+        n, i32 = self._seqs, torch.int32
+        for t in (kept, added):
+            if t.dtype is not i32 or t.shape != (n,) or not t.is_contiguous() or t.device != self.device:
+                raise ValueError(f"kept and added must be contiguous int32 [{n}] on the tables' device")
+        if not 0 <= tokens <= 1 << 30:
+            raise ValueError("tokens must lie between 0 and 2^30")
+        out = torch.empty((2 * n + 1 + 2 * tokens,), dtype=i32, device=self.device).split((n + 1, n, tokens, tokens))
+        q_start, kv_len, slots, positions = out
+        capi.pipo_op_page_tables(self._p, kept.data_ptr(), added.data_ptr(), tokens, q_start.data_ptr(),
+                                 kv_len.data_ptr(), slots.data_ptr(), positions.data_ptr(), _raw_stream(self.index))
+        return out
