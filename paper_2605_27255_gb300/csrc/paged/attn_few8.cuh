@@ -58,11 +58,6 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // byte offsets of 16-byte chunk c of entry r (0 .. 15) in a stage's keys or values: swizzled so that the
 // lanes' reads hit different banks (keys: lanes take neighbouring entries; values: every other one)
 template <int DH>
@@ -161,8 +156,7 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
             for (int i = 0; i < 4; ++i) most = fmaxf(most, finite_abs(x[i]));
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            // 2^e with the largest magnitude in [2^e, 2^(e+1)) (e at least -126, so that 1 / 2^e is a number)
-            const float s = __uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), f = 1.f / s;
+            const float s = query_scale(most), f = 1.f / s;
             if (lane == 0) row_scale[r] = s;
             if (lane < DH / 4) {  // dims 4 lane ..: chunk lane / 4, word lane % 4 of it
                 const int step = (lane >> 4) * 4 + (lane & 3), quad = (lane >> 2) & 3;

@@ -51,7 +51,10 @@
 // stops, and the copies and commits in flight are waited for before the CTA ends.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "../attn_prefill.cuh"
+#include "codes.cuh"
 #include "work.cuh"
 
 namespace pipo {
@@ -75,6 +78,17 @@ __host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
            (size_t)at_page_bytes(dh) * (at_k_pages(dh, pair) + at_v_pages(dh, pair)) * (pair ? 1 : 2);
 }
 
+// 8-bit pools: pages of key codes, of value operands and of value codes on their way to those
+__host__ __device__ constexpr int at8_k_pages(int dh) { return dh == 128 ? 5 : 8; }
+__host__ __device__ constexpr int at8_v_pages(int dh) { return dh == 128 ? 4 : 6; }
+__host__ __device__ constexpr int at8_raw_pages(int dh) { return dh == 128 ? 5 : 8; }
+constexpr int kAt8Convert = 3;  // converting warps: 2, 12 and 14
+__host__ __device__ constexpr int at8_codes(int dh) { return kPage * dh; }
+__host__ __device__ constexpr size_t at8_smem(int dh) {
+    return 1024 + 2 * (size_t)at_q_bytes(dh) + (size_t)at_page_bytes(dh) * at8_v_pages(dh) +
+           (size_t)at8_codes(dh) * (at8_k_pages(dh) + at8_raw_pages(dh));
+}
+
 // B operand [entries][dims] of a page (MN-major, 128-byte swizzle): 64-dim blocks kPageHalf apart,
 // groups of 8 entries 1024 bytes apart
 __device__ __forceinline__ uint64_t umma_desc_mn_page(uint32_t saddr) {
@@ -85,6 +99,26 @@ __device__ __forceinline__ uint64_t umma_desc_mn_page(uint32_t saddr) {
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;
     return d;
+}
+
+// K-major with 64-byte rows: 64-byte swizzle, 8-row groups 512 bytes apart
+__device__ __forceinline__ uint64_t umma_desc_sw64(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+    d |= (uint64_t)1 << 16;
+    d |= (uint64_t)(512 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)4 << 61;  // 64-byte swizzle
+    return d;
+}
+
+// D += A B of e4m3 numbers from shared memory, 32 bytes of a row at a time
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(
+            d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
 }
 
 // x / G for x < 256 and G <= 16, magic = ceil(2^16 / G): off by less than 256 / 2^16 < 1 / G
@@ -152,21 +186,67 @@ __device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
     for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
 }
 
-// SEL: whole tiles over selected pages (AttnPagedArgs::bits), PAIR only
-template <int DH, bool PAIR, bool SEL>
+// The codes of a page as an fp16 operand tile: rows of 64 entries, dims in blocks of 64, 128-byte
+// swizzle.  A quarter of the warp takes half of two neighbouring rows (128-dim rows: opposite halves), so that
+// neither its loads nor its stores meet in a bank.  (Two loads in flight: with four or eight unrolled the
+// kernel's warps wait for instructions, 550 us for the 2048-token chunk against 452.)
+template <int DH>
+__device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsigned char* src) {
+    constexpr int N = kPage * DH / 16 / 32, B = 2;  // 16-byte chunks of a lane, loads in flight
+    const int lane = threadIdx.x & 31, sub = lane >> 2 & 1, quad = lane & 3, q = lane >> 3;
+    auto row = [&](int i) { return (DH == 128 ? i >> 1 : i) * 8 + q * 2 + sub; };
+    auto half = [&](int i) { return DH == 128 ? sub ^ (i & 1) : 0; };
+#pragma unroll 1
+    for (int i0 = 0; i0 < N; i0 += B) {
+        uint4 x[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) x[i] = *reinterpret_cast<const uint4*>(src + row(i0 + i) * DH + half(i0 + i) * 64 + quad * 16);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int r = row(i0 + i);
+            unsigned char* d = dst + half(i0 + i) * kPageHalf + r * 128;
+            *reinterpret_cast<uint4*>(d + (((2 * quad) ^ (r & 7)) << 4)) =
+                make_uint4(decode_lo(x[i].x), decode_hi(x[i].x), decode_lo(x[i].y), decode_hi(x[i].y));
+            *reinterpret_cast<uint4*>(d + (((2 * quad + 1) ^ (r & 7)) << 4)) =
+                make_uint4(decode_lo(x[i].z), decode_hi(x[i].z), decode_lo(x[i].w), decode_hi(x[i].w));
+        }
+    }
+}
+
+// SEL: whole tiles over selected pages (AttnPagedArgs::bits), PAIR only.
+// E8: pools of e4m3 codes, PAIR only.  Key codes are operands as they are (kind::f8f6f4): queries are scaled
+// by a power of two per row to below 256 and meet them as two e4m3 parts, which hold all digits of
+// a bf16 number down to 2^-10 of the row's largest (below that 2^-18 of the largest are lost).  The two
+// parts cost what one bf16 operand does.  The row's and the block's scale meet the
+// scores in fp32.  Value codes become fp16 tiles (a code is an fp16 number) by warps 2, 12 and 14; their
+// scales go into the weights, relative to the largest so far (2^-24 at least: what that
+// adds to an output is below 2^-20 of its largest value), and weights keep fp16's 11 digits.
+// (Weights as e4m3 parts, so that values need no conversion either, would lose the small ones: a
+// long tail of 2^-17 each next to one large weight.)  Measured for 2048 tokens behind 14336 entries, 32
+// query and 8 kv heads of 128: 2559 us with row tiles of 32 on mma.sync, 692 with keys converted too (by two
+// warps; 592 by three), 541 with key codes as operands, 452 with the scales by shuffles in place of a
+// barrier and a smaller conversion loop; the bf16 pools take 370.  What is left: the scales' part of
+// every page (20 us), key codes in two products' time (20), instruction fetch.
+template <int DH, bool PAIR, bool SEL, bool E8 = false>
 __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs p, ItemShape shape, int S,
                                                                   int part_rows, size_t part_off,
                                                                   const __grid_constant__ CUtensorMap tmK,
                                                                   const __grid_constant__ CUtensorMap tmV) {
     constexpr int kTile = at_q_bytes(DH), kPg = at_page_bytes(DH), NR = PAIR ? 1 : 2;  // NR: pairs of rings
     constexpr int PARTS = PAIR ? 1 : 2;  // bf16 parts of the weights
-    constexpr int SK = at_k_pages(DH, PAIR), SV = at_v_pages(DH, PAIR);
+    constexpr int SK = E8 ? at8_k_pages(DH) : at_k_pages(DH, PAIR), SV = E8 ? at8_v_pages(DH) : at_v_pages(DH, PAIR);
+    constexpr int SR = at8_raw_pages(DH), kCodes = at8_codes(DH);
+    static_assert(!E8 || (PAIR && !SEL), "8-bit pools: chunks");
     extern __shared__ __align__(1024) unsigned char at_smem_raw[];
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t k_full[NR][SK], k_empty[NR][SK], v_full[NR][SV], v_empty[NR][SV];
     __shared__ __align__(8) uint64_t q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained[4];
     __shared__ Piece pieces[NR];
     __shared__ int give_up;
+    // 8-bit pools: ring of value codes, the queries' row scales
+    __shared__ __align__(8) uint64_t raw_full[E8 ? SR : 1], raw_empty[E8 ? SR : 1];
+    __shared__ bool raw_live[E8 ? SR : 1];
+    __shared__ float row_scale[E8 ? 2 : 1][E8 ? 2 : 1][E8 ? 128 : 1];  // [item's parity][pipeline][row]
 
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* q_s = sm;              // two query tiles
@@ -198,6 +278,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             mbar_init(drained + 2 * w, 1);
             mbar_init(drained + 2 * w + 1, 1);
         }
+        if (E8) {
+            for (int i = 0; i < SR; ++i) {
+                mbar_init(raw_full + i, 1);
+                mbar_init(raw_empty + i, 1);
+            }
+        }
         give_up = 0;
         mbar_init_fence();
     }
@@ -226,9 +312,65 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         if ((warp & 1) ? true : warp < 4 && !(PAIR && warp == 2)) {
             ItemWalk it;
             it.start(c, shape, pieces[ring]);
-            unsigned char* k_s = ring_s + (size_t)ring * (SK + SV) * kPg;
-            unsigned char* v_s = k_s + SK * kPg;
-            if ((warp & 1) == 0) {
+            // (8-bit pools: value operands, key codes, value codes)
+            unsigned char* k_s = E8 ? ring_s + SV * kPg : ring_s + (size_t)ring * (SK + SV) * kPg;
+            unsigned char* v_s = E8 ? ring_s : k_s + SK * kPg;
+            if (E8 && (warp & 1) == 0) {
+                // ---- copies of codes: the keys one page ahead of the values
+                unsigned char* raw_s = k_s + SK * kCodes;
+                int kn = 0, vn = 0;  // pages issued
+                bool ok = true;
+                for (; it.more() && ok; it.next(c, shape)) {
+                    const int np = it.pages(), pg0 = (it.t0 + it.kv0) * 2;
+                    const int gone = first_seen(shape, it.n, it.len, it.tile) / kPage;  // pages that no row sees
+                    int held = -32, mine = -1, prev = -1;  // lane l holds the block of page held + l
+                    for (int j = 0; j <= np; ++j) {
+                        int blk = -1;
+                        if (j < np) {
+                            if (j >= held + 32) {
+                                held = j;
+                                const int i = pg0 + j + lane;
+                                mine = j + lane < np && i * kPage < it.len && i >= gone ? page_block(c, it.b, i) : -1;
+                            }
+                            blk = __shfl_sync(0xffffffffu, mine, j - held);
+                            const int st = kn % SK;
+                            ok = kn < SK || wait(&k_empty[0][st], (uint32_t)(((kn / SK) & 1) ^ 1), 51, kn);
+                            if (!ok) break;
+                            if (lane == 0) {
+                                if (blk < 0) {
+                                    mbar_arrive(&k_full[0][st]);
+                                } else {
+                                    mbar_arrive_expect_tx(&k_full[0][st], (uint32_t)kCodes);
+                                    tma_load_2d(k_s + st * kCodes, &tmK, 0, (blk * c.n_kv + it.g) * kPage, &k_full[0][st]);
+                                }
+                            }
+                            ++kn;
+                            __syncwarp();
+                        }
+                        if (j > 0) {
+                            const int st = vn % SR;
+                            ok = vn < SR || wait(raw_empty + st, (uint32_t)(((vn / SR) & 1) ^ 1), 51, vn);
+                            if (!ok) break;
+                            if (lane == 0) {
+                                raw_live[st] = prev >= 0;
+                                if (prev < 0) {
+                                    mbar_arrive(raw_full + st);
+                                } else {
+                                    mbar_arrive_expect_tx(raw_full + st, (uint32_t)kCodes);
+                                    tma_load_2d(raw_s + st * kCodes, &tmV, 0, (prev * c.n_kv + it.g) * kPage, raw_full + st);
+                                }
+                            }
+                            ++vn;
+                            __syncwarp();
+                        }
+                        prev = blk;
+                    }
+                }
+                if (lane == 0) {
+                    ring_drain<SK>(kn, [&](int st, uint32_t ph, int i) { mbar_wait(&k_full[0][st], ph, 52, (unsigned)i); });
+                    ring_drain<SR>(vn, [&](int st, uint32_t ph, int i) { mbar_wait(raw_full + st, ph, 52, (unsigned)i); });
+                }
+            } else if ((warp & 1) == 0) {
                 // ---- copies: the keys one page ahead of the values
                 int kn = 0, vn = 0;  // pages issued
                 bool ok = true;
@@ -307,9 +449,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         continue;
                     }
                     if (!values) {
-                        constexpr uint32_t id_s = umma_idesc_bf16(128, kPage);
+                        constexpr uint32_t id_s = E8 ? umma_idesc_e4m3(128, kPage) : umma_idesc_bf16(128, kPage);
                         // descriptors count in 16 bytes: a step along a tile is an addition
-                        const uint64_t dq = umma_desc_sw128(smem_u32(q_s) + chain * kTile), dk = umma_desc_sw128(smem_u32(k_s));
+                        constexpr int kPgK = E8 ? kCodes : kPg;
+                        const uint32_t q_at = smem_u32(q_s) + chain * kTile, k_at = smem_u32(k_s);
+                        const uint64_t dq = E8 && DH == 64 ? umma_desc_sw64(q_at) : umma_desc_sw128(q_at);
+                        const uint64_t dk = E8 && DH == 64 ? umma_desc_sw64(k_at) : umma_desc_sw128(k_at);
                         ok = wait(q_full + chain, (uint32_t)(items & 1), 53, items);
                         for (int j = 0; j < np && ok; ++j, ++pv, ++n) {
                             const int st = n % SK, buf = pv & 1;
@@ -318,8 +463,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
-                                uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)((st * kPg) >> 4);
+                                uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)((st * kPgK) >> 4);
                                 asm volatile("" : "+r"(qb), "+r"(kb));  // eight sums now, not sixteen kept over the loop
+                                if constexpr (E8) {  // 32 dims a step; the queries' second part lies behind the first
+#pragma unroll
+                                    for (int i = 0; i < 2 * DH / 32; ++i)
+                                        umma_f8(s_at + buf * 64,
+                                                u32x2(qb + ((i / (DH / 32) * 128 * DH + i % (DH / 32) * 32) >> 4), (uint32_t)(dq >> 32)),
+                                                u32x2(kb + ((i % (DH / 32) * 32) >> 4), (uint32_t)(dk >> 32)), id_s, i > 0 ? 1u : 0u);
+                                } else
 #pragma unroll
                                 for (int i = 0; i < DH / 16; ++i)
                                     umma_bf16(s_at + buf * 64,
@@ -332,7 +484,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             __syncwarp();
                         }
                     } else {
-                        constexpr uint32_t id_o = umma_idesc_bf16(128, DH) | (1u << 16);  // B MN-major
+                        constexpr uint32_t id_o = (E8 ? umma_idesc_f16(128, DH) : umma_idesc_bf16(128, DH)) | (1u << 16);  // B MN-major
                         const uint64_t dv = umma_desc_mn_page(smem_u32(v_s));
                         // entries whose values may be anything: those before the window and past the
                         // sequence's (or the list's) end
@@ -386,6 +538,32 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     mbar_wait(drained + 2 * chain + values, 0, 57);
                 }
             }
+        } else if (E8) {
+            // ---- value codes to operands: the converting warps take the pages in turn
+            ItemWalk it;
+            it.start(c, shape, pieces[0]);
+            const int me = warp == 2 ? 2 : (warp - 12) >> 1;
+            unsigned char *v_s = ring_s, *raw_s = ring_s + SV * kPg + SK * kCodes;
+            int n = 0;  // pages before the present item
+            bool ok = true;
+            for (; it.more() && ok; it.next(c, shape)) {
+                const int end = n + it.pages();
+                for (int i = n + (me + kAt8Convert - n % kAt8Convert) % kAt8Convert; i < end; i += kAt8Convert) {
+                    const int st = i % SR, to = i % SV;
+                    ok = wait(raw_full + st, (uint32_t)((i / SR) & 1), 61, i) &&
+                         (i < SV || wait(&v_empty[0][to], (uint32_t)(((i / SV) & 1) ^ 1), 62, i));
+                    if (!ok) break;
+                    if (raw_live[st]) page_from_codes<DH>(v_s + to * kPg, raw_s + st * kCodes);
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&v_full[0][to]);
+                        mbar_arrive(raw_empty + st);
+                    }
+                    __syncwarp();
+                }
+                n = end;
+            }
         }
         __syncwarp();
     } else {
@@ -400,6 +578,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         it.start(c, shape, pieces[PAIR ? 0 : w]);
         const uint32_t g_magic = (65536u + (uint32_t)c.G - 1) / (uint32_t)c.G;
         const int row0 = PAIR ? w * 128 : 0;
+        int begun = 0;  // 8-bit pools: items with queries loaded
         // the next item with rows for this warpgroup, its queries in shared memory (rows past the last one
         // are zero).  Every load is in flight before the first is stored (one after the other they
         // took 19000 cycles).
@@ -418,10 +597,44 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 x[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (v < rows) x[i] = *reinterpret_cast<const uint4*>(q + (size_t)t * p.ld_q + (row0 + v - t * c.G) * DH);
             }
+            if constexpr (E8) {  // two e4m3 parts, a power of two per row (the C lanes of a row are neighbours)
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int v = v0 + i * RS;
-                *reinterpret_cast<uint4*>(q_s + w * kTile + (ch >> 3) * kAtHalf + v * 128 + (((ch & 7) ^ (v & 7)) << 4)) = x[i];
+                for (int i = 0; i < NI; ++i) {
+                    const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                    float y[8], most = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        y[2 * k] = bf_lo(u[k]);
+                        y[2 * k + 1] = bf_hi(u[k]);
+                        most = fmaxf(most, fmaxf(finite_abs(y[2 * k]), finite_abs(y[2 * k + 1])));
+                    }
+#pragma unroll
+                    for (int o = C / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                    const float sc = query_scale(most), f = 128.f / sc;  // the largest magnitude ends in [128, 256)
+                    const int v = v0 + i * RS;
+                    if (ch == 0) row_scale[begun & 1][w][v] = sc * (1.f / 128.f);
+                    uint32_t a[2], b[2];
+#pragma unroll
+                    for (int k = 0; k < 8; k += 4) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[k + e] *= f;
+                        a[k / 4] = encode4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+                        const uint32_t lo = decode_lo(a[k / 4]), hi = decode_hi(a[k / 4]);
+                        const float2 l2 = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+                        const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                        b[k / 4] = encode4(y[k] - l2.x, y[k + 1] - l2.y, y[k + 2] - h2.x, y[k + 3] - h2.y);
+                    }
+                    unsigned char* d = q_s + w * kTile + v * DH + (((ch >> 1) ^ (DH == 128 ? v & 7 : v >> 1 & 3)) << 4) + (ch & 1) * 8;
+                    *reinterpret_cast<uint2*>(d) = make_uint2(a[0], a[1]);
+                    *reinterpret_cast<uint2*>(d + 128 * DH) = make_uint2(b[0], b[1]);
+                }
+                ++begun;
+            } else {
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int v = v0 + i * RS;
+                    *reinterpret_cast<uint4*>(q_s + w * kTile + (ch >> 3) * kAtHalf + v * 128 + (((ch & 7) ^ (v & 7)) << 4)) = x[i];
+                }
             }
             fence_proxy_async();  // the generic stores above, before the MMAs read them
             __syncwarp();
@@ -452,6 +665,30 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 if (kept > 0) pos = (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage : kPage - 1);
             }
             float m_ref = -INFINITY, l = 0.f;
+            float v_ref = 0.f, c_row = c2;  // 8-bit pools: the largest value scale so far, what the row's raw scores are worth
+            if (E8) {
+                ok = wait(q_full + w, (uint32_t)((begun - 1) & 1), 60, begun);
+                if (!ok) break;
+                c_row = c2 * row_scale[(begun - 1) & 1][w][r];
+            }
+            // 8-bit pools: lane l holds the scales of page l of 32, those of the next 32 are on their way: blocks first,
+            // scales eight pages later, so that no page waits for them
+            const int pg0 = (it.t0 + it.kv0) * 2, gone = E8 ? first_seen(shape, it.n, it.len, it.tile) / kPage : 0;
+            int next_blk = -1;
+            float k_sc = 1.f, v_sc = 0.f, next_k = 1.f, next_v = 0.f;
+            auto block_at = [&](int j) {  // (-1: gone, masked; scales of 1 and 0 change nothing)
+                const int i = pg0 + j + lane;
+                return j + lane < it.pages() && i * kPage < it.len && i >= gone ? page_block(c, it.b, i) : -1;
+            };
+            auto scales_at = [&](int blk) {
+                next_k = 1.f;
+                next_v = 0.f;
+                if (blk >= 0) {
+                    next_k = p.k_scale[(size_t)blk * c.n_kv + it.g];
+                    next_v = p.v_scale[(size_t)blk * c.n_kv + it.g];
+                }
+            };
+            if (E8) scales_at(block_at(0));
             // whole tiles over selected pages: this row's bits, 32 pages at a time
             const uint32_t* bits =
                 SEL ? p.bits + ((size_t)(it.q0 + tok) * c.n_kv + it.g) * bit_words(c.max_pages) : nullptr;
@@ -459,6 +696,18 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             const int np = it.pages();
             for (int j = 0; j < np; ++j, ++sn) {
                 const uint32_t s_buf = s_col + (uint32_t)((sn & 1) * 64);
+                float cs = c2, v_now = 0.f;
+                if (E8) {
+                    if ((j & 31) == 0) {
+                        k_sc = next_k;
+                        v_sc = next_v;
+                        next_blk = block_at(j + 32);
+                    } else if ((j & 31) == 8) {
+                        scales_at(next_blk);
+                    }
+                    cs = fmaxf(c_row * __shfl_sync(0xffffffffu, k_sc, j & 31), 1.17549435e-38f);  // (never 0: masked scores are -infinity)
+                    v_now = __shfl_sync(0xffffffffu, v_sc, j & 31);
+                }
                 ok = wait(&s_full[w][sn & 1], (uint32_t)((sn >> 1) & 1), 58, sn);
                 if (!ok) break;
                 tc_fence_after();
@@ -487,13 +736,17 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         for (int i = 0; i < kPage; ++i)
                             if (e0 + i > pos || e0 + i < lo) s[i >> 5][i & 31] = 0xff800000u;
                     }
-                    const float top = SEL && !sel ? -INFINITY : fmaxf(max32(s[0]), max32(s[1])) * c2;
+                    const float top = SEL && !sel ? -INFINITY : fmaxf(max32(s[0]), max32(s[1])) * cs;
                     // the reference moves when the maximum has passed it by the slack (or it is the first one)
                     const bool move = top > m_ref + kAtSlack;
-                    if (__any_sync(0xffffffffu, move)) {
-                        const float f = move ? (m_ref == -INFINITY ? 0.f : ex2(m_ref - top)) : 1.f;
+                    if (__any_sync(0xffffffffu, move) || (E8 && v_now > v_ref)) {
+                        float f = move ? (m_ref == -INFINITY ? 0.f : ex2(m_ref - top)) : 1.f;
                         if (move) m_ref = top;
                         l *= f;
+                        if (E8 && v_now > v_ref) {
+                            f *= v_ref / v_now;
+                            v_ref = v_now;
+                        }
                         if (j > 0) {  // the output so far, once the values of the page before are in it
                             ok = wait(&o_full[w][(sn - 1) & 1], (uint32_t)(((sn - 1) >> 1) & 1), 59, sn);
                             if (!ok) break;
@@ -511,9 +764,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         }
                     }
                     // (a page that the row has not selected: exponents of -infinity)
-                    const float neg = SEL && !sel ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
+                    float neg = SEL && !sel ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
+                    int dv = 0;  // 8-bit pools: the page's value scale against the largest, as an exponent
+                    if (E8) {
+                        dv = max((int)(__float_as_uint(v_now) >> 23) - (int)(__float_as_uint(v_ref) >> 23), -24);
+                        neg += (float)dv;
+                    }
                     // two columns at a time (paired fp32 instructions)
-                    const uint64_t c22 = f32x2(c2, c2), neg2 = f32x2(neg, neg);
+                    const uint64_t c22 = f32x2(cs, cs), neg2 = f32x2(neg, neg);
                     uint64_t sum[2] = {0ull, 0ull};
                     uint32_t pk[32], pl[32];
 #pragma unroll
@@ -521,13 +779,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         const uint64_t e = fma_f32x2(u32x2(s[i >> 4][2 * (i & 15)], s[i >> 4][2 * (i & 15) + 1]), c22, neg2);
                         const float p0 = ex2(__uint_as_float((uint32_t)e)), p1 = ex2(__uint_as_float((uint32_t)(e >> 32)));
                         sum[i & 1] = add_f32x2(sum[i & 1], f32x2(p0, p1));
-                        pk[i] = pack_bf16x2(p0, p1);
+                        pk[i] = E8 ? half2_of(p0, p1) : pack_bf16x2(p0, p1);
                         if (PARTS == 2) pl[i] = pack_bf16x2(p0 - bf_lo(pk[i]), p1 - bf_hi(pk[i]));
                     }
                     tmem_st32(s_buf, pk);
                     if (PARTS == 2) tmem_st32(s_buf + 32, pl);
                     sum[0] = add_f32x2(sum[0], sum[1]);
-                    l += __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
+                    float part = __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
+                    if (E8) part *= __uint_as_float((uint32_t)(127 - dv) << 23);
+                    l += part;
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 }
                 tc_fence_before();
@@ -551,13 +811,17 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             if (!ok) break;
             tc_fence_after();
             if (live) {
-                const float inv = l > 0.f ? 1.0f / l : 0.f;
+                const float unit = E8 ? v_ref : 1.f, inv = l > 0.f ? unit / l : 0.f;
 #pragma unroll
                 for (int h = 0; h < DH / 32; ++h) {
                     uint32_t v[32];
                     tmem_ld32_issue(o_col + 32 * h, v);
                     tmem_ld_wait();
                     pin32(v);
+                    if (E8 && !whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * unit);
+                    }
                     if (r < rows && whole) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {

@@ -7,6 +7,8 @@
 // round every held entry again whenever a later one is larger.)
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "paged.cuh"
 
 namespace pipo {
@@ -41,5 +43,17 @@ __device__ __forceinline__ uint32_t decode2(uint16_t x) {
 }
 __device__ __forceinline__ uint32_t decode_lo(uint32_t w) { return decode2((uint16_t)w); }
 __device__ __forceinline__ uint32_t decode_hi(uint32_t w) { return decode2((uint16_t)(w >> 16)); }
+
+// two values as fp16, the first one in the low half
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The power of two that queries of largest magnitude `most` are divided by on their way to fp16: they end below
+// 2 and above 2^-126 of themselves (1 for zeros)
+__device__ __forceinline__ float query_scale(float most) {
+    return most > 0.f ? __uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)) : 1.f;
+}
 
 }  // namespace pipo

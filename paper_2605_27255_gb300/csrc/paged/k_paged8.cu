@@ -41,16 +41,22 @@ cudaError_t launch_kv_append8(const AppendArgs& a, cudaStream_t s) {
     return a.c.dh == 64 ? append8_as<64>(a, s) : append8_as<128>(a, s);
 }
 
-// The plan of attention over 8-bit pools: row tiles of 8, 16 or 32 rows by the rows (new tokens times query
-// heads of a kv head) that the batch's sequences have on average.
+// The plan of attention over 8-bit pools by the rows (new tokens times query heads of a kv head) that the
+// batch's sequences have on average: row tiles of 8, 16 or 32 rows, and above kFewRows pairs of 128 on tcgen05.
+constexpr int kFewRows = 64;
 AttnPlan plan_attn8(const PagedArgs& c, int dev, int sms) {
     AttnPlan pl{};
     pl.dev = dev;
     const long long mine = (long long)c.n_tokens * c.G;
-    pl.rt = c.G <= 8 && mine <= 8LL * c.batch ? 1 : mine <= 16LL * c.batch ? 2 : 4;
-    pl.TP = 8 * pl.rt / c.G;
+    if (mine > (long long)kFewRows * c.batch) {
+        pl.pair = true;
+        pl.TP = 256 / c.G;
+    } else {
+        pl.rt = c.G <= 8 && mine <= 8LL * c.batch ? 1 : mine <= 16LL * c.batch ? 2 : 4;
+        pl.TP = 8 * pl.rt / c.G;
+    }
     pl.tiles = tiles_bound(c.n_tokens, c.batch, pl.TP);
-    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each, all = (long long)sms * few_ctas(pl.rt);
+    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each, all = (long long)sms * (pl.pair ? 1 : few_ctas(pl.rt));
     pl.workers = pl.ctas = (int)(most < all ? most : all);
     pl.join = each > 1;
     pl.part_rows = (int)(mine < (long long)pl.TP * c.G ? mine : (long long)pl.TP * c.G);

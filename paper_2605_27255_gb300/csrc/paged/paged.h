@@ -97,6 +97,8 @@ struct TablesArgs {
 // k_paged_tc.cu
 cudaError_t launch_attn_tile(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
                              cudaStream_t s);
+cudaError_t launch_attn_tile8(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
+                              cudaStream_t s);
 cudaError_t take_error_paged(unsigned* code, unsigned* info);
 
 // k_paged.cu

@@ -99,8 +99,11 @@ cudaError_t device_of(int* dev, int* sms) {
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 std::mutex g_encode_lock;
 
-// a pool as [n_blocks * n_kv * 64][d_h] bf16: boxes of one page x 64 dims, 128-byte swizzle
-pipo_status pool_map(const char* who, CUtensorMap* tm, void* pool, const PagedArgs& a) {
+// a pool as [n_blocks * n_kv * 64][d_h]: bf16 in boxes of one page x 64 dims, 128-byte swizzle; codes in
+// boxes of one page, swizzled by the row's length (key codes) or as they lie there
+enum class PoolKind { kBf16, kKeyCodes, kValueCodes };
+pipo_status pool_map(const char* who, CUtensorMap* tm, void* pool, const PagedArgs& a, PoolKind kind = PoolKind::kBf16) {
+    const bool codes = kind != PoolKind::kBf16;
     {
         std::lock_guard<std::mutex> lk(g_encode_lock);
         if (!g_encode) {
@@ -113,11 +116,15 @@ pipo_status pool_map(const char* who, CUtensorMap* tm, void* pool, const PagedAr
         }
     }
     const cuuint64_t dims[2] = {(cuuint64_t)a.dh, (cuuint64_t)a.n_blocks * a.n_kv * kPage};
-    const cuuint64_t strides[1] = {(cuuint64_t)a.dh * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)kPage}, es[2] = {1, 1};
-    const CUresult r = g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, pool, dims, strides, box, es,
-                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const CUtensorMapSwizzle swizzle = kind == PoolKind::kValueCodes ? CU_TENSOR_MAP_SWIZZLE_NONE
+                                       : codes && a.dh == 64         ? CU_TENSOR_MAP_SWIZZLE_64B
+                                                                     : CU_TENSOR_MAP_SWIZZLE_128B;
+    const cuuint64_t strides[1] = {(cuuint64_t)a.dh * (codes ? 1 : 2)};
+    const cuuint32_t box[2] = {codes ? (cuuint32_t)a.dh : 64, (cuuint32_t)kPage}, es[2] = {1, 1};
+    const CUresult r = g_encode(tm, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, pool, dims,
+                                strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                swizzle,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? PIPO_OK : fail(PIPO_ECUDA, "%s: cuTensorMapEncodeTiled: error %d", who, (int)r);
 }
 
@@ -349,7 +356,12 @@ pipo_status pipo_op_attn_paged8(const pipo_paged8* c8, int32_t n_tokens, const v
     a.scratch = static_cast<unsigned char*>(d_scratch);
     a.k_scale = c8->k_scale;
     a.v_scale = c8->v_scale;
-    return cuda_status("pipo_op_attn_paged8", launch_attn_few8(a, pl, static_cast<cudaStream_t>(stream)));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (!pl.pair) return cuda_status("pipo_op_attn_paged8", launch_attn_few8(a, pl, s));
+    CUtensorMap tk, tv;
+    pipo_status st = pool_map("pipo_op_attn_paged8", &tk, a.c.k, a.c, PoolKind::kKeyCodes);
+    if (st == PIPO_OK) st = pool_map("pipo_op_attn_paged8", &tv, a.c.v, a.c, PoolKind::kValueCodes);
+    return st == PIPO_OK ? cuda_status("pipo_op_attn_paged8", launch_attn_tile8(a, pl, tk, tv, s)) : st;
 }
 
 pipo_status pipo_op_page_tables(const pipo_page_tables* p, const int32_t* d_kept, const int32_t* d_added, int32_t n_tokens,
