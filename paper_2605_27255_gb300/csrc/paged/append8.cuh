@@ -1,7 +1,7 @@
 // Norm, rotation and append of the new tokens to a cache of e4m3 codes.
 //
-// As append.cuh, but keys and values become codes: of a block and kv head all new
-// entries are held in registers by one CTA, their largest magnitude sets the
+// As append.cuh, but keys and values become codes: all new keys (or values) of a block and kv
+// head are held in registers by one CTA, their largest magnitude sets the
 // scale, and they are rounded once.  A block's first entry (slot 0 among the new ones)
 // starts a new scale.  Later entries keep it while they fit (up to 448 times the scale);
 // else it is chosen anew from them, and the codes that the block holds move by the
@@ -34,99 +34,92 @@ __device__ __forceinline__ void move_codes(uint8_t* block, int n, float f) {
     }
 }
 
-// grid: page_ctas = runs * n_kv CTAs of (page, kv head), then kAppendWarps tokens' queries each
+// grid: CTAs of kAppendWarps tokens' queries each, then page_ctas = runs * n_kv * 2 of (page, kv head, keys or
+// values).  Keys and values apart, so that 64 registers hold a block's entries and four CTAs fit an SM: two
+// 8191-token prompts with 32 query and 8 kv heads of 128 in bf16 117 us with both in one CTA (128 registers, two
+// CTAs), 81 apart, 78 with the queries first (the other order ends in a tail of long CTAs).
 template <int DH, typename TI>
-__global__ void __launch_bounds__(kAppendWarps * 32, 2) kv_append8_kernel(AppendArgs p, int page_ctas) {
+__global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append8_kernel(AppendArgs p, int page_ctas) {
     using HL = HeadLane<DH>;
     constexpr int E = kAppendWarps * HL::H, R = kPage / E;  // entries a round, rounds
-    __shared__ float most[2][kAppendWarps];
+    __shared__ float most[kAppendWarps];
     const PagedArgs& c = p.c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = HL::dim(), hl = HL::head();
     pdl_launch();
     pdl_wait();
-    if ((int)blockIdx.x >= page_ctas) {
-        append_queries<DH, TI, bf16_t>(p, ((long long)blockIdx.x - page_ctas) * kAppendWarps + warp);
+    const int query_ctas = (int)gridDim.x - page_ctas, x0 = (int)blockIdx.x - query_ctas;
+    if (x0 < 0) {
+        append_queries<DH, TI, bf16_t>(p, (long long)blockIdx.x * kAppendWarps + warp);
         return;
     }
-    const int g = blockIdx.x % c.n_kv;
+    const bool keys = (x0 & 1) == 0;
+    const int g = x0 / 2 % c.n_kv;
     int b, page;
-    if (!find_run(c, blockIdx.x / c.n_kv, b, page)) return;
+    if (!find_run(c, x0 / 2 / c.n_kv, b, page)) return;
     const int len = seq_len(c, b), end = q_row(c, b + 1), n = end - q_row(c, b);
     const int j0 = max(page * kPage, len - n), j1 = min(len, (page + 1) * kPage);  // the new entries
     const int blk = c.table[(size_t)b * c.max_pages + page];
     if (blk < 0 || blk >= c.n_blocks) return;
     const size_t head = (size_t)blk * c.n_kv + g;
-    const float old_k = p.k_scale[head], old_v = p.v_scale[head];
-    float gain[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-    load_gain<DH, bf16_t>(static_cast<const bf16_t*>(p.k_gain), gain);
-    float ka[R][4], kb[R][4], va[R][4], vb[R][4];
+    float* scale = (keys ? p.k_scale : p.v_scale) + head;
+    const float old = *scale;
+    const long long ld = keys ? p.ld_k : p.ld_v;
+    const TI* src = static_cast<const TI*>(keys ? p.kn : p.vn) + (size_t)g * DH + d;
+    float x[R][4], y[R][4];  // dims d .. and DH / 2 + d ..
     const int at = warp * HL::H + hl;  // this lane's entry of a round
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int j = j0 + r * E + at;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ka[r][i] = kb[r][i] = va[r][i] = vb[r][i] = 0.f;
+        for (int i = 0; i < 4; ++i) x[r][i] = y[r][i] = 0.f;
         if (j < j1) {
-            const size_t t = (size_t)(end - (len - j));
-            const TI* ks = static_cast<const TI*>(p.kn) + t * p.ld_k + (size_t)g * DH + d;
-            const TI* vs = static_cast<const TI*>(p.vn) + t * p.ld_v + (size_t)g * DH + d;
-            load_f<TI, 4>(ks, ka[r]);
-            load_f<TI, 4>(ks + DH / 2, kb[r]);
-            load_f<TI, 4>(vs, va[r]);
-            load_f<TI, 4>(vs + DH / 2, vb[r]);
+            const TI* s = src + (size_t)(end - (len - j)) * ld;
+            load_f<TI, 4>(s, x[r]);
+            load_f<TI, 4>(s + DH / 2, y[r]);
         }
     }
-    float mk = 0.f, mv = 0.f;
+    if (keys) {
+        float gain[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        load_gain<DH, bf16_t>(static_cast<const bf16_t*>(p.k_gain), gain);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int j = j0 + r * E + at;
-        if (j0 + r * E >= j1) break;  // (the same for every lane: the norm's shuffles need them all)
-        const Angles an = load_angles<DH>(j < j1 ? p.rope : nullptr, j);
-        // (without angles nothing is turned: infinity times a sine of zero would be NaN in its partner)
-        norm_turn<DH>(ka[r], kb[r], p.k_gain != nullptr, gain, j < j1 ? p.eps : 1.f, an, p.rope != nullptr);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            mk = fmaxf(mk, fmaxf(finite_abs(ka[r][i]), finite_abs(kb[r][i])));
-            mv = fmaxf(mv, fmaxf(finite_abs(va[r][i]), finite_abs(vb[r][i])));
+        for (int r = 0; r < R; ++r) {
+            const int j = j0 + r * E + at;
+            if (j0 + r * E >= j1) break;  // (the same for every lane: the norm's shuffles need them all)
+            const Angles an = load_angles<DH>(j < j1 ? p.rope : nullptr, j);
+            // (without angles nothing is turned: infinity times a sine of zero would be NaN in its partner)
+            norm_turn<DH>(x[r], y[r], p.k_gain != nullptr, gain, j < j1 ? p.eps : 1.f, an, p.rope != nullptr);
         }
     }
+    float m = 0.f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        mk = fmaxf(mk, __shfl_xor_sync(0xffffffffu, mk, o));
-        mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, o));
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, fmaxf(fabsf(x[r][i]), fabsf(y[r][i])));
+    if (m > 3.402823466e38f) {  // an infinity (NaN is not seen): it does not count
+        m = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = fmaxf(m, fmaxf(finite_abs(x[r][i]), finite_abs(y[r][i])));
     }
-    if (lane == 0) {
-        most[0][warp] = mk;
-        most[1][warp] = mv;
-    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) most[warp] = m;
     __syncthreads();
-    mk = mv = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAppendWarps; ++w) {
-        mk = fmaxf(mk, most[0][w]);
-        mv = fmaxf(mv, most[1][w]);
-    }
+    for (int w = 0; w < kAppendWarps; ++w) m = fmaxf(m, most[w]);
     const int slot0 = j0 - page * kPage;  // entries held before
-    const float new_k = slot0 == 0 || mk > kCodeMax * old_k ? scale_of(mk) : old_k;
-    const float new_v = slot0 == 0 || mv > kCodeMax * old_v ? scale_of(mv) : old_v;
-    uint8_t* kd = static_cast<uint8_t*>(c.k) + head * kPage * DH;
-    uint8_t* vd = static_cast<uint8_t*>(c.v) + head * kPage * DH;
-    if (slot0 > 0 && new_k != old_k) move_codes<DH>(kd, slot0, old_k / new_k);
-    if (slot0 > 0 && new_v != old_v) move_codes<DH>(vd, slot0, old_v / new_v);
-    if (threadIdx.x == 0) {  // (every thread has read the old ones before the barrier)
-        p.k_scale[head] = new_k;
-        p.v_scale[head] = new_v;
-    }
-    const float fk = 1.f / new_k, fv = 1.f / new_v;
+    const float now = slot0 == 0 || m > kCodeMax * old ? scale_of(m) : old, f = 1.f / now;
+    uint8_t* dst = static_cast<uint8_t*>(keys ? c.k : c.v) + head * kPage * DH;
+    if (slot0 > 0 && now != old) move_codes<DH>(dst, slot0, old / now);
+    if (threadIdx.x == 0) *scale = now;  // (every thread has read the old one before the barrier)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int j = j0 + r * E + at;
         if (j >= j1) continue;
-        const size_t o = (size_t)(j % kPage) * DH + d;
-        *reinterpret_cast<uint32_t*>(kd + o) = encode4(ka[r][0] * fk, ka[r][1] * fk, ka[r][2] * fk, ka[r][3] * fk);
-        *reinterpret_cast<uint32_t*>(kd + o + DH / 2) = encode4(kb[r][0] * fk, kb[r][1] * fk, kb[r][2] * fk, kb[r][3] * fk);
-        *reinterpret_cast<uint32_t*>(vd + o) = encode4(va[r][0] * fv, va[r][1] * fv, va[r][2] * fv, va[r][3] * fv);
-        *reinterpret_cast<uint32_t*>(vd + o + DH / 2) = encode4(vb[r][0] * fv, vb[r][1] * fv, vb[r][2] * fv, vb[r][3] * fv);
+        uint8_t* o = dst + (size_t)(j % kPage) * DH + d;
+        *reinterpret_cast<uint32_t*>(o) = encode4(x[r][0] * f, x[r][1] * f, x[r][2] * f, x[r][3] * f);
+        *reinterpret_cast<uint32_t*>(o + DH / 2) = encode4(y[r][0] * f, y[r][1] * f, y[r][2] * f, y[r][3] * f);
     }
 }
 

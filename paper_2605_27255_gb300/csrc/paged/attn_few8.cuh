@@ -12,10 +12,10 @@
 //                   entries' bytes.  P^T comes from S^T's registers by movmatrix.
 // The queries are scaled by a power of two per row to fp16 (bf16's digits fit; what is below
 // 2^-24 of a row's largest is lost), scores get it back with the block's scale in fp32.  The values'
-// scales go into the weights, relative to the largest one so far: weights stay in
-// [0, 1] and keep fp16's 11 digits (2^-25 below 2^-14).
+// scales go into the weights, relative to the largest one so far: weights stay below
+// 2^8 and keep fp16's 11 digits (2^-25 below 2^-14).
 //
-// A warp takes 16 entries of a 128-entry unit, with its own ring of copies, running maximum
+// A warp takes 16 (or 32) entries of a 128-entry unit, with its own ring of copies, running maximum
 // and output; warps meet only at the end of an item, where their outputs are joined in
 // order.  Nothing waits on anything but its own copies.
 //
@@ -29,19 +29,26 @@
 
 namespace pipo {
 
-constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
+constexpr float kFewSlack = 8.f;  // exponents above the reference before it moves
 
-__host__ __device__ constexpr int few_ctas(int nt) { return nt <= 2 ? 2 : 1; }    // of an SM
-__host__ __device__ constexpr int few_stages(int nt) { return nt == 1 ? 3 : nt == 2 ? 2 : 4; }
-__host__ __device__ constexpr int few_stage_bytes(int dh) { return 2 * 16 * dh; }  // 16 entries' keys and values
-__host__ __device__ constexpr int few_ring_bytes(int dh, int nt) { return kFewWarps * few_stages(nt) * few_stage_bytes(dh); }
-__host__ __device__ constexpr int few_q_bytes(int dh, int nt) { return nt * 8 * dh * 2; }
-// half of the warps' outputs and their (maximum, sum); the 16-byte chunks of a row are swizzled by it
-__host__ __device__ constexpr int few_join_bytes(int dh, int nt) { return kFewWarps / 2 * nt * 8 * (dh + 2) * 4; }
+// Entries of a warp's step: 16 fill an MMA's rows, 32 share a step's other work (eight sequences of 15.5 K
+// entries 49.1 -> 47.7 us); with more than one column tile their scores would not fit the registers.
+__host__ __device__ constexpr int few_entries(int, int nt) { return nt == 1 ? 32 : 16; }
+__host__ __device__ constexpr int few_warps(int dh, int nt) { return kTileEnt / few_entries(dh, nt); }
+__host__ __device__ constexpr int few_threads(int dh, int nt) { return 32 * few_warps(dh, nt); }
+__host__ __device__ constexpr int few_ctas(int dh, int nt) { return nt > 2 ? 1 : dh == 64 && nt == 1 ? 4 : 2; }  // of an SM
+__host__ __device__ constexpr int few_stages(int dh, int nt) { return nt > 2 ? 4 : nt == 1 && dh == 128 ? 3 : 2; }
+__host__ __device__ constexpr int few_stage_bytes(int dh, int nt) { return 2 * few_entries(dh, nt) * dh; }  // a step's keys and values
+__host__ __device__ constexpr int few_ring_bytes(int dh, int nt) {
+    return few_warps(dh, nt) * few_stages(dh, nt) * few_stage_bytes(dh, nt);
+}
+__host__ __device__ constexpr int few_q_bytes(int dh, int nt) { return nt > 1 ? nt * 8 * dh * 2 : 0; }
+// four warps' outputs and their (maximum, sum); the 16-byte chunks of a row are swizzled by it
+__host__ __device__ constexpr int few_join_bytes(int dh, int nt) { return 4 * nt * 8 * (dh + 2) * 4; }
 template <int DH>
 __device__ __forceinline__ int few_join_at(int r, int chunk) { return r * DH + ((chunk ^ ((r >> 1) & 3)) << 2); }
 __host__ __device__ constexpr size_t few_smem(int dh, int nt, int batch) {
-    const size_t n = (size_t)few_ring_bytes(dh, nt) + few_join_bytes(dh, nt) + (nt > 1 ? few_q_bytes(dh, nt) : 0);
+    const size_t n = (size_t)few_ring_bytes(dh, nt) + few_join_bytes(dh, nt) + few_q_bytes(dh, nt);
     const size_t find = ((size_t)find_ints(batch) * 4 + 15) / 16 * 16;
     return n > find ? n : find;
 }
@@ -58,6 +65,16 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
+// 16 bytes (or the first n of them, then zeros) into shared memory
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, uint32_t n) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
+}
+__device__ __forceinline__ float few_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // byte offsets of 16-byte chunk c of entry r (0 .. 15) in a stage's keys or values: swizzled so that the
 // lanes' reads hit different banks (keys: lanes take neighbouring entries; values: every other one)
 template <int DH>
@@ -70,23 +87,25 @@ __device__ __forceinline__ uint32_t few_v_off(int r, int c) {
 }
 
 template <int DH, int NT>
-__global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(AttnPagedArgs p, ItemShape shape, int S,
+__global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_few8_kernel(AttnPagedArgs p, ItemShape shape, int S,
                                                                              int part_rows, size_t part_off) {
-    constexpr int ST = few_stages(NT), SB = few_stage_bytes(DH), KS = DH / 16, MT = DH / 16, ROWS = 8 * NT;
-    constexpr int NC = 16 * DH / 16 / 32;  // 16-byte chunks of a lane, of a stage's keys or values
+    constexpr int EW = few_entries(DH, NT), WARPS = few_warps(DH, NT), THREADS = 32 * WARPS, ET = EW / 16;
+    constexpr int ST = few_stages(DH, NT), SB = few_stage_bytes(DH, NT), KS = DH / 16, MT = DH / 16, ROWS = 8 * NT;
+    constexpr int NC = EW * DH / 16 / 32;  // 16-byte chunks of a lane, of a stage's keys or values
+    constexpr int VS = EW * DH;            // the values' place in a stage
     extern __shared__ __align__(128) unsigned char few_raw[];
     __shared__ Piece piece[1];
-    __shared__ float row_scale[ROWS];
-    __shared__ float scales[kFewWarps][ST][2];  // of the block that a stage holds: keys', values'
+    __shared__ float row_scale[NT > 1 ? ROWS : 1];
+    __shared__ float scales[WARPS][ST][2];  // of the block that a stage holds: keys', values'
     unsigned char* ring = few_raw;
     float* join_s = reinterpret_cast<float*>(few_raw + few_ring_bytes(DH, NT));
-    // queries in the order of the MMAs' registers; with one column tile they pass through the joining memory
-    uint2* q_s = reinterpret_cast<uint2*>(few_raw + few_ring_bytes(DH, NT) + (NT > 1 ? few_join_bytes(DH, NT) : 0));
+    // queries in the order of the MMAs' registers (with one column tile every warp has them in registers)
+    uint2* q_s = reinterpret_cast<uint2*>(few_raw + few_ring_bytes(DH, NT) + few_join_bytes(DH, NT));
     const PagedArgs& c = p.c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane >> 2, tig = lane & 3;
     const int me = (int)blockIdx.x;
     pdl_wait();
-    find_pieces<kFewThreads, 1>(c, shape, me, S, reinterpret_cast<int*>(few_raw), piece);
+    find_pieces<THREADS, 1>(c, shape, me, S, reinterpret_cast<int*>(few_raw), piece);
     pdl_launch();
     if (threadIdx.x == 0) reinterpret_cast<SharedItem*>(p.scratch)[me] = {0, 0, 0, -1};
     __syncthreads();
@@ -94,7 +113,14 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
     const float c2 = p.scale * 1.4426950408889634f;  // exponents of two
     unsigned char* mine_s = ring + (size_t)warp * ST * SB;
 
-    // ---- copies: this warp's 16 entries of unit lu of item ld
+    // ---- copies: this warp's entries of unit lu of item ld.  They lie side by side, 16 bytes of a lane 512 apart,
+    // in the cache and (swizzled within) in the stage.
+    constexpr int RS = 512 / DH;  // entries between a lane's chunks
+    const int r0 = lane / (DH / 16), ch = lane % (DH / 16);
+    const uint32_t stage_at = (uint32_t)__cvta_generic_to_shared(mine_s), k_to = stage_at + few_k_off<DH>(r0, ch);
+    const uint32_t v_to[2] = {stage_at + VS + few_v_off<DH>(r0, ch), stage_at + VS + few_v_off<DH>(RS + r0, ch) - 512};
+    const uint32_t scale_to = (uint32_t)__cvta_generic_to_shared(&scales[warp][0][lane & 1]);
+    const float* scale_from = lane ? p.v_scale : p.k_scale;
     ItemWalk ld;
     ld.start(c, shape, piece[0]);
     int lu = ld.kv0, held = lu - 32, blocks = -1, slot_in = 0;  // lane l has the block of unit held + l
@@ -103,29 +129,35 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
             const int first = first_seen(shape, ld.n, ld.len, ld.tile);
             if (lu >= held + 32) {
                 held = lu;
-                const int page = (ld.t0 + lu + lane) * 2 + (warp >> 2);
+                const int page = (ld.t0 + lu + lane) * 2 + warp * EW / kPage;
                 blocks = lu + lane < ld.kv1 && (long long)page * kPage < ld.len && page >= first / kPage
                              ? page_block(c, ld.b, page)
                              : -1;
             }
             const int blk = __shfl_sync(0xffffffffu, blocks, lu - held);
-            const int e0 = (ld.t0 + lu) * kTileEnt + warp * 16;
-            const size_t head = (size_t)max(blk, 0) * c.n_kv + ld.g;
-            const size_t off = (head * kPage + (warp & 3) * 16) * DH;
-            unsigned char* dst = mine_s + slot_in * SB;
+            const int e0 = (ld.t0 + lu) * kTileEnt + warp * EW;
+            const size_t head = (size_t)max(blk, 0) * c.n_kv + ld.g, off = (head * kPage + warp * EW % kPage) * DH + lane * 16;
+            const uint8_t *k = static_cast<const uint8_t*>(c.k) + off, *v = static_cast<const uint8_t*>(c.v) + off;
+            const uint32_t to = slot_in * SB;
+            if (blk >= 0 && e0 >= first && e0 + EW <= ld.len) {
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const int id = i * 32 + lane, r = id / (DH / 16), ch = id % (DH / 16), e = e0 + r;
-                const bool take = blk >= 0 && e >= first && e < ld.len;
-                cp_async16(dst + few_k_off<DH>(r, ch), static_cast<const uint8_t*>(c.k) + off + r * DH + ch * 16, take);
-                cp_async16(dst + 16 * DH + few_v_off<DH>(r, ch), static_cast<const uint8_t*>(c.v) + off + r * DH + ch * 16, take);
+                for (int i = 0; i < NC; ++i) {
+                    copy16(k_to + to + i * 512, k + i * 512, 16u);
+                    copy16(v_to[i & 1] + to + i * 512, v + i * 512, 16u);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    const int e = e0 + r0 + i * RS;
+                    const uint32_t nb = blk >= 0 && e >= first && e < ld.len ? 16u : 0u;
+                    copy16(k_to + to + i * 512, k + i * 512, nb);
+                    copy16(v_to[i & 1] + to + i * 512, v + i * 512, nb);
+                }
             }
-            if (lane < 2) {
-                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&scales[warp][slot_in][lane]), nb = blk >= 0 ? 4u : 0u;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"((lane ? p.v_scale : p.k_scale) + head),
-                             "r"(nb)
+            if (lane < 2)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(scale_to + slot_in * 8), "l"(scale_from + head),
+                             "r"(blk >= 0 ? 4u : 0u)
                              : "memory");
-            }
             if (++lu == ld.kv1) {
                 ld.next(c, shape);
                 lu = ld.kv0;
@@ -143,31 +175,65 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
     int slot = 0;
     while (it.more()) {
         const int rows = it.tokens(shape) * c.G, i0 = it.tile * shape.TP;
-        // ---- queries: a warp per row, four dims a lane
-        for (int r = warp; r < ROWS; r += kFewWarps) {
-            float x[4] = {0.f, 0.f, 0.f, 0.f}, most = 0.f;
-            if (r < rows && lane < DH / 4) {
-                const int t = r / c.G;
-                load_f<bf16_t, 4>(static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + i0 + t) * p.ld_q +
-                                      (size_t)(it.g * c.G + r - t * c.G) * DH + lane * 4,
-                                  x);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, finite_abs(x[i]));
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            const float s = query_scale(most), f = 1.f / s;
-            if (lane == 0) row_scale[r] = s;
-            if (lane < DH / 4) {  // dims 4 lane ..: chunk lane / 4, word lane % 4 of it
-                const int step = (lane >> 4) * 4 + (lane & 3), quad = (lane >> 2) & 3;
-                q_s[((r >> 3) * KS + step) * 32 + (r & 7) * 4 + quad] = make_uint2(half2_of(x[0] * f, x[1] * f), half2_of(x[2] * f, x[3] * f));
-            }
-        }
-        __syncthreads();
+        // ---- queries
         uint2 qf[NT == 1 ? KS : 1];
-        if (NT == 1) {
+        float scale_of_row[2] = {1.f, 1.f};  // (one column tile) of this lane's rows 2 tig, 2 tig + 1
+        if constexpr (NT == 1) {
+            // every warp for itself: a lane has row grp, 16 dims from 16 tig (and 64 + 16 tig) on, as its keys
+            const int t = grp / c.G;
+            const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + i0 + (grp < rows ? t : 0)) * p.ld_q +
+                              (size_t)(it.g * c.G + (grp < rows ? grp - t * c.G : 0)) * DH + tig * 16;
+            uint4 x[DH / 64][2];
+            float most = 0.f;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) qf[i] = q_s[i * 32 + lane];
+            for (int h = 0; h < DH / 64; ++h)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    x[h][k] = grp < rows ? *reinterpret_cast<const uint4*>(q + h * 64 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int h = 0; h < DH / 64; ++h)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t u[4] = {x[h][k].x, x[h][k].y, x[h][k].z, x[h][k].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(finite_abs(bf_lo(u[e])), finite_abs(bf_hi(u[e]))));
+                }
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const float sc = query_scale(most), f = 1.f / sc;
+            scale_of_row[0] = __shfl_sync(0xffffffffu, sc, 8 * tig);
+            scale_of_row[1] = __shfl_sync(0xffffffffu, sc, 8 * tig + 4);
+#pragma unroll
+            for (int h = 0; h < DH / 64; ++h)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    qf[NT == 1 ? h * 4 + 2 * k : 0] = make_uint2(half2_of(bf_lo(x[h][k].x) * f, bf_hi(x[h][k].x) * f),
+                                                                half2_of(bf_lo(x[h][k].y) * f, bf_hi(x[h][k].y) * f));
+                    qf[NT == 1 ? h * 4 + 2 * k + 1 : 0] = make_uint2(half2_of(bf_lo(x[h][k].z) * f, bf_hi(x[h][k].z) * f),
+                                                                    half2_of(bf_lo(x[h][k].w) * f, bf_hi(x[h][k].w) * f));
+                }
+        } else {
+            // a warp per row, four dims a lane
+            for (int r = warp; r < ROWS; r += WARPS) {
+                float x[4] = {0.f, 0.f, 0.f, 0.f}, most = 0.f;
+                if (r < rows && lane < DH / 4) {
+                    const int t = r / c.G;
+                    load_f<bf16_t, 4>(static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + i0 + t) * p.ld_q +
+                                          (size_t)(it.g * c.G + r - t * c.G) * DH + lane * 4,
+                                      x);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, finite_abs(x[i]));
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                const float sc = query_scale(most), f = 1.f / sc;
+                if (lane == 0) row_scale[r] = sc;
+                if (lane < DH / 4) {  // dims 4 lane ..: chunk lane / 4, word lane % 4 of it
+                    const int step = (lane >> 4) * 4 + (lane & 3), quad = (lane >> 2) & 3;
+                    q_s[((r >> 3) * KS + step) * 32 + (r & 7) * 4 + quad] = make_uint2(half2_of(x[0] * f, x[1] * f), half2_of(x[2] * f, x[3] * f));
+                }
+            }
+            __syncthreads();
         }
         // ---- this lane's rows: 2 tig and 2 tig + 1 of every column tile
         float cs[NT][2], m[NT][2], l[NT][2], o[NT][MT][4];
@@ -177,7 +243,7 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int r = min(t * 8 + 2 * tig + h, rows - 1);
-                cs[t][h] = c2 * row_scale[t * 8 + 2 * tig + h];
+                cs[t][h] = c2 * (NT == 1 ? scale_of_row[h] : row_scale[NT > 1 ? t * 8 + 2 * tig + h : 0]);
                 pos[t][h] = it.len - it.n + i0 + r / c.G;
                 lo[t][h] = p.window > 0 ? pos[t][h] - p.window + 1 : 0;
                 m[t][h] = -INFINITY;
@@ -198,50 +264,67 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
             __syncwarp();
             issue();
             const unsigned char* ks_s = mine_s + slot * SB;
-            const unsigned char* vs_s = ks_s + 16 * DH;
+            const unsigned char* vs_s = ks_s + VS;
             const float k_scale = scales[warp][slot][0], v_scale = scales[warp][slot][1];
             slot = slot + 1 == ST ? 0 : slot + 1;
-            const int e0 = (it.t0 + u) * kTileEnt + warp * 16;
-            float s[NT][4];
+            const int e0 = (it.t0 + u) * kTileEnt + warp * EW;
+            // (the sums of the two halves of the dims apart where registers allow: shorter chains)
+            constexpr int CH = DH == 128 && NT <= 2 ? 2 : 1;
+            float s[ET][NT][4], s2[CH][ET][NT][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int x = 0; x < ET; ++x)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int half = 0; half < DH / 64; ++half) {
-                const uint4 ka = *reinterpret_cast<const uint4*>(ks_s + few_k_off<DH>(grp, tig + 4 * half));
-                const uint4 kb = *reinterpret_cast<const uint4*>(ks_s + few_k_off<DH>(grp + 8, tig + 4 * half));
-                const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+                    for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = decode_lo(wa[i]), a1 = decode_lo(wb[i]), a2 = decode_hi(wa[i]), a3 = decode_hi(wb[i]);
+                        for (int h = 0; h < CH; ++h) s2[h][x][t][e] = 0.f;
+            uint4 kw[ET][2][DH / 64];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const uint2 q = NT == 1 ? qf[NT == 1 ? half * 4 + i : 0] : q_s[(t * KS + half * 4 + i) * 32 + lane];
-                        mma_f16(s[t], a0, a1, a2, a3, q.x, q.y);
-                    }
+            for (int x = 0; x < ET; ++x)
+#pragma unroll
+                for (int half = 0; half < DH / 64; ++half) {
+                    kw[x][0][half] = *reinterpret_cast<const uint4*>(ks_s + few_k_off<DH>(16 * x + grp, tig + 4 * half));
+                    kw[x][1][half] = *reinterpret_cast<const uint4*>(ks_s + few_k_off<DH>(16 * x + grp + 8, tig + 4 * half));
                 }
-            }
-            // ---- softmax: s[t][0], s[t][1] are entry grp's scores for the lane's two rows, [2], [3] entry grp + 8's
-            const bool edge = e0 + 16 > free_to || e0 < free_from;
-            float top[NT][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int half = 0; half < DH / 64; ++half)
+#pragma unroll
+                    for (int x = 0; x < ET; ++x) {
+                        const uint4 ka = kw[x][0][half], kb = kw[x][1][half];
+                        const uint32_t a = i == 0 ? ka.x : i == 1 ? ka.y : i == 2 ? ka.z : ka.w;
+                        const uint32_t b = i == 0 ? kb.x : i == 1 ? kb.y : i == 2 ? kb.z : kb.w;
+                        const uint32_t a0 = decode_lo(a), a1 = decode_lo(b), a2 = decode_hi(a), a3 = decode_hi(b);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const uint2 q = NT == 1 ? qf[NT == 1 ? half * 4 + i : 0] : q_s[(t * KS + half * 4 + i) * 32 + lane];
+                            mma_f16(s2[half % CH][x][t], a0, a1, a2, a3, q.x, q.y);
+                        }
+                    }
+            // ---- softmax: s[.][t][0], s[.][t][1] are entry grp's scores for the lane's two rows, [2], [3] entry
+            // grp + 8's.  The reference of the exponents moves when a score has passed it by 2^8 (as in the tile
+            // kernel); only then the warp agrees on its maxima.
+            const bool edge = e0 + EW > free_to || e0 < free_from;
             bool move = v_scale > v_ref;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float f = cs[t][h] * k_scale;
-                    s[t][h] *= f;
-                    s[t][2 + h] *= f;
-                    if (edge) {
-                        if (e0 + grp > pos[t][h] || e0 + grp < lo[t][h]) s[t][h] = -INFINITY;
-                        if (e0 + grp + 8 > pos[t][h] || e0 + grp + 8 < lo[t][h]) s[t][2 + h] = -INFINITY;
-                    }
-                    float x = fmaxf(s[t][h], s[t][2 + h]);
 #pragma unroll
-                    for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
-                    top[t][h] = x;
-                    move |= x > m[t][h];
+                    for (int x = 0; x < ET; ++x) {
+#pragma unroll
+                        for (int e = h; e < 4; e += 2)
+                            s[x][t][e] = (CH == 2 ? s2[0][x][t][e] + s2[CH - 1][x][t][e] : s2[0][x][t][e]) * f;
+                        if (edge) {
+                            const int a = e0 + 16 * x + grp;
+                            if (a > pos[t][h] || a < lo[t][h]) s[x][t][h] = -INFINITY;
+                            if (a + 8 > pos[t][h] || a + 8 < lo[t][h]) s[x][t][2 + h] = -INFINITY;
+                        }
+                        move |= fmaxf(s[x][t][h], s[x][t][2 + h]) > m[t][h] + kFewSlack;
+                    }
                 }
             if (__any_sync(0xffffffffu, move)) {
                 const float v_new = fmaxf(v_ref, v_scale), fv = v_ref > 0.f ? v_ref / v_new : 0.f;
@@ -249,8 +332,12 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float now = fmaxf(m[t][h], top[t][h]);
-                        const float f = now == -INFINITY ? 1.f : exp2f(m[t][h] - now);
+                        float now = m[t][h];
+#pragma unroll
+                        for (int x = 0; x < ET; ++x) now = fmaxf(now, fmaxf(s[x][t][h], s[x][t][2 + h]));
+#pragma unroll
+                        for (int w = 4; w < 32; w <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, w));
+                        const float f = now == -INFINITY ? 1.f : few_ex2(m[t][h] - now);
                         m[t][h] = now;
                         l[t][h] *= f;
 #pragma unroll
@@ -263,52 +350,56 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
                 v_inv = v_new > 0.f ? 1.f / v_new : 0.f;
             }
             const float vr = v_scale * v_inv;
-            uint32_t pb[NT][2];
+            uint32_t pb[ET][NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                float w[4];
+                const float ref[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float ref = m[t][h] == -INFINITY ? 0.f : m[t][h];
-                    w[h] = exp2f(s[t][h] - ref);
-                    w[2 + h] = exp2f(s[t][2 + h] - ref);
-                    l[t][h] += w[h] + w[2 + h];
+                for (int x = 0; x < ET; ++x) {
+                    float w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = few_ex2(s[x][t][e] - ref[e & 1]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) l[t][h] += w[h] + w[2 + h];
+                    pb[x][t][0] = turn8x8(half2_of(w[0] * vr, w[1] * vr));
+                    pb[x][t][1] = turn8x8(half2_of(w[2] * vr, w[3] * vr));
                 }
-                pb[t][0] = turn8x8(half2_of(w[0] * vr, w[1] * vr));
-                pb[t][1] = turn8x8(half2_of(w[2] * vr, w[3] * vr));
             }
             // ---- values: dims 16 grp .. (8 grp .. for 64) of entries 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9
-            uint32_t v[4][DH / 32];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 2 * tig + (e & 1) + (e >> 1) * 8;
-                if (DH == 128) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(vs_s + few_v_off<DH>(r, grp));
-                    v[e][0] = x.x;
-                    v[e][1] = x.y;
-                    v[e][DH / 32 - 2] = x.z;
-                    v[e][DH / 32 - 1] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(vs_s + few_v_off<DH>(r, grp >> 1) + (grp & 1) * 8);
-                    v[e][0] = x.x;
-                    v[e][1] = x.y;
+            for (int xt = 0; xt < ET; ++xt) {
+                uint32_t v[4][DH / 32];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 16 * xt + 2 * tig + (e & 1) + (e >> 1) * 8;
+                    if (DH == 128) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(vs_s + few_v_off<DH>(r, grp));
+                        v[e][0] = x.x;
+                        v[e][1] = x.y;
+                        v[e][DH / 32 - 2] = x.z;
+                        v[e][DH / 32 - 1] = x.w;
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2*>(vs_s + few_v_off<DH>(r, grp >> 1) + (grp & 1) * 8);
+                        v[e][0] = x.x;
+                        v[e][1] = x.y;
+                    }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < DH / 32; ++i) {
-                // bytes of two entries side by side: (dim 0, dim 1), (dim 2, dim 3)
-                const uint32_t x0 = __byte_perm(v[0][i], v[1][i], 0x5140), x1 = __byte_perm(v[0][i], v[1][i], 0x7362);
-                const uint32_t y0 = __byte_perm(v[2][i], v[3][i], 0x5140), y1 = __byte_perm(v[2][i], v[3][i], 0x7362);
-                const uint32_t a0 = decode_lo(x0), a1 = decode_hi(x0), a2 = decode_lo(y0), a3 = decode_hi(y0);
-                const uint32_t b0 = decode_lo(x1), b1 = decode_hi(x1), b2 = decode_lo(y1), b3 = decode_hi(y1);
+                for (int i = 0; i < DH / 32; ++i) {
+                    // bytes of two entries side by side: (dim 0, dim 1), (dim 2, dim 3)
+                    const uint32_t x0 = __byte_perm(v[0][i], v[1][i], 0x5140), x1 = __byte_perm(v[0][i], v[1][i], 0x7362);
+                    const uint32_t y0 = __byte_perm(v[2][i], v[3][i], 0x5140), y1 = __byte_perm(v[2][i], v[3][i], 0x7362);
+                    const uint32_t a0 = decode_lo(x0), a1 = decode_hi(x0), a2 = decode_lo(y0), a3 = decode_hi(y0);
+                    const uint32_t b0 = decode_lo(x1), b1 = decode_hi(x1), b2 = decode_lo(y1), b3 = decode_hi(y1);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    mma_f16(o[t][2 * i], a0, a1, a2, a3, pb[t][0], pb[t][1]);
-                    mma_f16(o[t][2 * i + 1], b0, b1, b2, b3, pb[t][0], pb[t][1]);
+                    for (int t = 0; t < NT; ++t) {
+                        mma_f16(o[t][2 * i], a0, a1, a2, a3, pb[xt][t][0], pb[xt][t][1]);
+                        mma_f16(o[t][2 * i + 1], b0, b1, b2, b3, pb[xt][t][0], pb[xt][t][1]);
+                    }
                 }
             }
         }
-        // ---- the warps' outputs, joined: warps 4 .. 7 hand theirs to 0 .. 3, whose four are added up in order
+        // ---- the warps' outputs, joined: of eight warps 4 .. 7 hand theirs to 0 .. 3, and four are added up in order
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -322,7 +413,7 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
                 }
             }
         float* my_o = join_s + (size_t)(warp & 3) * ROWS * DH;
-        float* my_ml = join_s + (size_t)(kFewWarps / 2) * ROWS * DH + (warp & 3) * ROWS * 2;
+        float* my_ml = join_s + (size_t)4 * ROWS * DH + (warp & 3) * ROWS * 2;
         auto leave = [&]() {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -336,10 +427,13 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
                     if (grp == 0) *reinterpret_cast<float2*>(my_ml + 2 * r) = make_float2(m[t][h], l[t][h]);
                 }
         };
-        if (NT == 1) __syncthreads();  // (every warp has its queries out of the joining memory)
-        if (warp >= 4) leave();
-        __syncthreads();
-        if (warp < 4) {
+        if (WARPS > 4) {
+            if (warp >= 4) leave();
+            __syncthreads();
+        }
+        if (WARPS == 4) {
+            leave();
+        } else if (warp < 4) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -367,8 +461,8 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(NT)) attn_few8_kernel(At
         float* part = reinterpret_cast<float*>(p.scratch + part_off) + ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
         if (it.begun() && threadIdx.x == 0)
             reinterpret_cast<SharedItem*>(p.scratch)[me] = {it.q0 + i0, rows, it.g, it.last_worker(piece[0])};
-        const float* ml = join_s + (size_t)(kFewWarps / 2) * ROWS * DH;
-        for (int i = threadIdx.x; i < rows * (DH / 4); i += kFewThreads) {
+        const float* ml = join_s + (size_t)4 * ROWS * DH;
+        for (int i = threadIdx.x; i < rows * (DH / 4); i += THREADS) {
             const int r = i / (DH / 4), d = i % (DH / 4) * 4;
             float2 e[4];
             float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};

@@ -13,7 +13,7 @@ template <int DH>
 cudaError_t append8_as(const AppendArgs& a, cudaStream_t s) {
     // pages that receive entries: a sequence with n new tokens spans at most n / 64 + 2
     const long long t = a.c.n_tokens, most = t / kPage + 2LL * a.c.batch, runs = t < most ? t : most;
-    const int pages = (int)(runs * a.c.n_kv);
+    const int pages = (int)(runs * a.c.n_kv * 2);
     const dim3 grid(pages + (a.q_out ? ceil_div(t, kAppendWarps) : 0));
     return a.in_bf16 ? launch_pdl(&kv_append8_kernel<DH, bf16_t>, grid, kAppendWarps * 32, 0, s, a, pages)
                      : launch_pdl(&kv_append8_kernel<DH, float>, grid, kAppendWarps * 32, 0, s, a, pages);
@@ -30,7 +30,7 @@ cudaError_t few8_as(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) 
         ready = pl.dev;
     }
     const ItemShape shape{pl.TP, a.window, 0};
-    const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kFewThreads, few_smem(DH, NT, a.c.batch), s, a, shape,
+    const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), few_threads(DH, NT), few_smem(DH, NT, a.c.batch), s, a, shape,
                                      pl.workers, pl.part_rows, pl.part_off);
     return e == cudaSuccess ? launch_combine<DH, bf16_t>(a, pl, s) : e;
 }
@@ -56,7 +56,7 @@ AttnPlan plan_attn8(const PagedArgs& c, int dev, int sms) {
         pl.TP = 8 * pl.rt / c.G;
     }
     pl.tiles = tiles_bound(c.n_tokens, c.batch, pl.TP);
-    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each, all = (long long)sms * (pl.pair ? 1 : few_ctas(pl.rt));
+    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each, all = (long long)sms * (pl.pair ? 1 : few_ctas(c.dh, pl.rt));
     pl.workers = pl.ctas = (int)(most < all ? most : all);
     pl.join = each > 1;
     pl.part_rows = (int)(mine < (long long)pl.TP * c.G ? mine : (long long)pl.TP * c.G);

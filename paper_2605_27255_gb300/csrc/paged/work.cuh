@@ -54,6 +54,11 @@ __device__ __forceinline__ RowTile row_tile(const ItemShape& s, int n, int len, 
     return {t0, (np + 1) / 2, np};
 }
 
+// a / b for a, b >= 0: in 32 bits where they fit (a 64-bit division takes some hundred instructions)
+__device__ __forceinline__ long long div_up_to_64(long long a, long long b) {
+    return ((unsigned long long)a | (unsigned long long)b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
+
 __device__ __forceinline__ int seq_new(const PagedArgs& c, int b) { return max(0, q_row(c, b + 1) - q_row(c, b)); }
 
 // The scratch: one record per worker, then the parts.  A worker leaves at most one
@@ -129,7 +134,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
     if (tid < NW) out[tid].left = 0;
     __syncthreads();
     // this thread's run of row tiles and its units
-    const int x0 = (int)((long long)tiles * tid / NT), x1 = (int)((long long)tiles * (tid + 1) / NT);
+    const int x0 = (int)((long long)tiles * tid / NT), x1 = (int)((long long)tiles * (tid + 1) / NT);  // (NT: a power of two)
     int lo = 0, hi = c.batch - 1;  // the last b with seq_tiles[b] <= x0 (it holds x0: an empty sequence's start is its successor's)
     while (lo < hi) {
         const int m = (lo + hi + 1) >> 1;
@@ -167,7 +172,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         if (w0 + w >= Sw) break;
-        const long long u0 = (long long)(w0 + w) * total / Sw, u1 = (long long)(w0 + w + 1) * total / Sw;
+        const long long u0 = div_up_to_64((w0 + w) * total, Sw), u1 = div_up_to_64((w0 + w + 1) * total, Sw);
         if (u0 >= before && u0 < before + mine) {
             long long at = before;
             walk([&](int b, int j, const RowTile& r) {
@@ -177,7 +182,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
                     at += n;
                     return false;
                 }
-                const int g = (int)((u0 - at) / len), off = (int)((u0 - at) % len) - kItemCost;
+                const int g = (int)div_up_to_64(u0 - at, len), off = (int)(u0 - at - (long long)g * len) - kItemCost;
                 // (a piece that starts before the item's first unit)
                 out[w] = {b, j, g, max(0, off), max(0, (int)(u1 - u0) + min(0, off)), u1, total, Sw};
                 return true;
@@ -188,7 +193,7 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
 }
 
 // the worker that holds place u of the line
-__device__ __forceinline__ int worker_of(long long u, long long total, int S) { return (int)(((u + 1) * S - 1) / total); }
+__device__ __forceinline__ int worker_of(long long u, long long total, int S) { return (int)div_up_to_64((u + 1) * S - 1, total); }
 
 // One worker's items in turn.  Every thread of a role keeps its own; what is only
 // asked of an item that starts here stays in the piece (shared memory).
