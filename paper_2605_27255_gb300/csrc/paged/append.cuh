@@ -66,7 +66,7 @@ __device__ __forceinline__ void load_gain(const T* gain, float (&g)[8]) {
 // this lane's part of a head, normalised and rotated in place (every lane of the head calls it)
 template <int DH>
 __device__ __forceinline__ void norm_turn(float (&a)[4], float (&b)[4], bool norm, const float (&g)[8], float eps,
-                                          const Angles& an, bool turn = true) {
+                                          const Angles& an) {
     if (norm) {
         float ss = 0.f;
 #pragma unroll
@@ -80,7 +80,6 @@ __device__ __forceinline__ void norm_turn(float (&a)[4], float (&b)[4], bool nor
             b[i] *= r * g[4 + i];
         }
     }
-    if (!turn) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float x = a[i], y = b[i];
@@ -119,46 +118,6 @@ __device__ __forceinline__ bool find_run(const PagedArgs& c, int r, int& b, int&
     return false;
 }
 
-// A warp: token t's queries, normalised and rotated.
-template <int DH, typename TI, typename T>
-__device__ __forceinline__ void append_queries(const AppendArgs& p, long long t) {
-    using HL = HeadLane<DH>;
-    const PagedArgs& c = p.c;
-    const int d = HL::dim(), hl = HL::head();
-    float gain[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-    if (t >= c.n_tokens) return;
-    load_gain<DH, T>(static_cast<const T*>(p.q_gain), gain);
-    const Tok k = find_token(c, (int)t);
-    if (k.b < 0) return;
-    const Angles an = load_angles<DH>(k.pos >= 0 ? p.rope : nullptr, k.pos);
-    const TI* src = static_cast<const TI*>(p.q) + (size_t)t * p.ld_q + d;
-    T* dst = static_cast<T*>(p.q_out) + (size_t)t * c.n_q * DH + d;
-    const float eps = k.pos >= 0 ? p.eps : 1.f;  // (a token without an entry: zeros, also where eps is 0)
-    constexpr int U = 4;  // heads in flight per lane
-    for (int h0 = 0; h0 < c.n_q; h0 += U * HL::H) {
-        float a[U][4], b[U][4];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * HL::H + hl;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[u][i] = b[u][i] = 0.f;
-            if (h < c.n_q && k.pos >= 0) {
-                load_f<TI, 4>(src + (size_t)h * DH, a[u]);
-                load_f<TI, 4>(src + (size_t)h * DH + DH / 2, b[u]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * HL::H + hl;
-            norm_turn<DH>(a[u], b[u], p.q_gain != nullptr, gain, eps, an);
-            if (h < c.n_q) {
-                store_f<T, 4>(dst + (size_t)h * DH, a[u]);
-                store_f<T, 4>(dst + (size_t)h * DH + DH / 2, b[u]);
-            }
-        }
-    }
-}
-
 // Four CTAs an SM (64 registers) keep enough loads in flight: 74 us for two 8191-token prompts,
 // 5.6 TB/s; with two entries per lane at a time 80, with the registers that take (three CTAs) 89, with 16
 // dims per lane 90.
@@ -172,8 +131,39 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append_kernel(AppendA
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     float gain[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-    if ((int)blockIdx.x >= page_ctas) {
-        append_queries<DH, TI, T>(p, ((long long)blockIdx.x - page_ctas) * kAppendWarps + warp);
+    if ((int)blockIdx.x >= page_ctas) {  // queries: a warp per token
+        const long long t = ((long long)blockIdx.x - page_ctas) * kAppendWarps + warp;
+        if (t >= c.n_tokens) return;
+        load_gain<DH, T>(static_cast<const T*>(p.q_gain), gain);
+        const Tok k = find_token(c, (int)t);
+        if (k.b < 0) return;
+        const Angles an = load_angles<DH>(k.pos >= 0 ? p.rope : nullptr, k.pos);
+        const TI* src = static_cast<const TI*>(p.q) + (size_t)t * p.ld_q + d;
+        T* dst = static_cast<T*>(p.q_out) + (size_t)t * c.n_q * DH + d;
+        const float eps = k.pos >= 0 ? p.eps : 1.f;  // (a token without an entry: zeros, also where eps is 0)
+        constexpr int U = 4;  // heads in flight per lane
+        for (int h0 = 0; h0 < c.n_q; h0 += U * HL::H) {
+            float a[U][4], b[U][4];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * HL::H + hl;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[u][i] = b[u][i] = 0.f;
+                if (h < c.n_q && k.pos >= 0) {
+                    load_f<TI, 4>(src + (size_t)h * DH, a[u]);
+                    load_f<TI, 4>(src + (size_t)h * DH + DH / 2, b[u]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * HL::H + hl;
+                norm_turn<DH>(a[u], b[u], p.q_gain != nullptr, gain, eps, an);
+                if (h < c.n_q) {
+                    store_f<T, 4>(dst + (size_t)h * DH, a[u]);
+                    store_f<T, 4>(dst + (size_t)h * DH + DH / 2, b[u]);
+                }
+            }
+        }
         return;
     }
     const int g = blockIdx.x % c.n_kv;
