@@ -590,46 +590,57 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             const int ch = wt % C, v0 = wt / C, rows = it.tokens(shape) * c.G - row0;
             const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + it.tile * shape.TP) * p.ld_q +
                               (size_t)it.g * c.G * DH + ch * 8;
-            uint4 x[NI];
+            auto load = [&](int v) {
+                const int t = div_g(row0 + v, g_magic);
+                return v < rows ? *reinterpret_cast<const uint4*>(q + (size_t)t * p.ld_q + (row0 + v - t * c.G) * DH)
+                                : make_uint4(0u, 0u, 0u, 0u);
+            };
+            if constexpr (E8) {
+                // two e4m3 parts, a power of two per row (the C lanes of a row are neighbours), eight rows at a time
+#pragma unroll 1
+                for (int i0 = 0; i0 < NI; i0 += 8) {
+                    uint4 x[8];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int v = v0 + i * RS, t = div_g(row0 + v, g_magic);
-                x[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (v < rows) x[i] = *reinterpret_cast<const uint4*>(q + (size_t)t * p.ld_q + (row0 + v - t * c.G) * DH);
-            }
-            if constexpr (E8) {  // two e4m3 parts, a power of two per row (the C lanes of a row are neighbours)
+                    for (int i = 0; i < 8; ++i) x[i] = load(v0 + (i0 + i) * RS);
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                    float y[8], most = 0.f;
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                        float y[8], most = 0.f;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        y[2 * k] = bf_lo(u[k]);
-                        y[2 * k + 1] = bf_hi(u[k]);
-                        most = fmaxf(most, fmaxf(finite_abs(y[2 * k]), finite_abs(y[2 * k + 1])));
+                        for (int k = 0; k < 4; ++k) {
+                            y[2 * k] = bf_lo(u[k]);
+                            y[2 * k + 1] = bf_hi(u[k]);
+                            most = max3(most, fabsf(y[2 * k]), fabsf(y[2 * k + 1]));
+                        }
+#pragma unroll
+                        for (int o = C / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                        // the largest magnitude ends in [128, 256), that of tiny rows below; an infinity makes the row
+                        // NaN, as its scores would be
+                        const bool inf = most > 3.402823466e38f;
+                        const float sc = inf ? 1.f : fmaxf(query_scale(most), 3.0092655e-36f), f = inf ? NAN : 128.f / sc;
+                        const int v = v0 + (i0 + i) * RS;
+                        if (ch == 0) row_scale[begun & 1][w][v] = sc * (1.f / 128.f);
+                        uint32_t a[2], b[2];
+#pragma unroll
+                        for (int k = 0; k < 8; k += 4) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) y[k + e] *= f;
+                            a[k / 4] = encode4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+                            const uint32_t lo = decode_lo(a[k / 4]), hi = decode_hi(a[k / 4]);
+                            const float2 l2 = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+                            const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                            b[k / 4] = encode4(y[k] - l2.x, y[k + 1] - l2.y, y[k + 2] - h2.x, y[k + 3] - h2.y);
+                        }
+                        unsigned char* d = q_s + w * kTile + v * DH + (((ch >> 1) ^ (DH == 128 ? v & 7 : v >> 1 & 3)) << 4) + (ch & 1) * 8;
+                        *reinterpret_cast<uint2*>(d) = make_uint2(a[0], a[1]);
+                        *reinterpret_cast<uint2*>(d + 128 * DH) = make_uint2(b[0], b[1]);
                     }
-#pragma unroll
-                    for (int o = C / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-                    const float sc = query_scale(most), f = 128.f / sc;  // the largest magnitude ends in [128, 256)
-                    const int v = v0 + i * RS;
-                    if (ch == 0) row_scale[begun & 1][w][v] = sc * (1.f / 128.f);
-                    uint32_t a[2], b[2];
-#pragma unroll
-                    for (int k = 0; k < 8; k += 4) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[k + e] *= f;
-                        a[k / 4] = encode4(y[k], y[k + 1], y[k + 2], y[k + 3]);
-                        const uint32_t lo = decode_lo(a[k / 4]), hi = decode_hi(a[k / 4]);
-                        const float2 l2 = __half22float2(*reinterpret_cast<const __half2*>(&lo));
-                        const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                        b[k / 4] = encode4(y[k] - l2.x, y[k + 1] - l2.y, y[k + 2] - h2.x, y[k + 3] - h2.y);
-                    }
-                    unsigned char* d = q_s + w * kTile + v * DH + (((ch >> 1) ^ (DH == 128 ? v & 7 : v >> 1 & 3)) << 4) + (ch & 1) * 8;
-                    *reinterpret_cast<uint2*>(d) = make_uint2(a[0], a[1]);
-                    *reinterpret_cast<uint2*>(d + 128 * DH) = make_uint2(b[0], b[1]);
                 }
                 ++begun;
             } else {
+                uint4 x[NI];
+#pragma unroll
+                for (int i = 0; i < NI; ++i) x[i] = load(v0 + i * RS);
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
                     const int v = v0 + i * RS;
@@ -705,7 +716,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     } else if ((j & 31) == 8) {
                         scales_at(next_blk);
                     }
-                    cs = fmaxf(c_row * __shfl_sync(0xffffffffu, k_sc, j & 31), 1.17549435e-38f);  // (never 0: masked scores are -infinity)
+                    // (never 0: masked scores are -infinity)
+                    cs = fmaxf(c_row * __shfl_sync(0xffffffffu, k_sc, j & 31), 1.17549435e-38f);
                     v_now = __shfl_sync(0xffffffffu, v_sc, j & 31);
                 }
                 ok = wait(&s_full[w][sn & 1], (uint32_t)((sn >> 1) & 1), 58, sn);
@@ -739,7 +751,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     const float top = SEL && !sel ? -INFINITY : fmaxf(max32(s[0]), max32(s[1])) * cs;
                     // the reference moves when the maximum has passed it by the slack (or it is the first one)
                     const bool move = top > m_ref + kAtSlack;
-                    if (__any_sync(0xffffffffu, move) || (E8 && v_now > v_ref)) {
+                    // 8-bit pools: scores so large that what a fused multiply-add keeps of the maximum itself, up to half a step,
+                    // is a power of two that matters are multiplied before the subtraction, which then leaves 0
+                    const bool large = E8 && fabsf(top) > 4194304.f && top > -INFINITY;
+                    if (__any_sync(0xffffffffu, move || large) || (E8 && v_now > v_ref)) {
+                        if (E8 && __any_sync(0xffffffffu, large)) {
+#pragma unroll
+                            for (int i = 0; i < kPage; ++i) s[i >> 5][i & 31] = __float_as_uint(__fmul_rn(__uint_as_float(s[i >> 5][i & 31]), cs));
+                            cs = 1.f;
+                        }
                         float f = move ? (m_ref == -INFINITY ? 0.f : ex2(m_ref - top)) : 1.f;
                         if (move) m_ref = top;
                         l *= f;

@@ -48,11 +48,15 @@ def verify(target: torch.Tensor, drafted: torch.Tensor, start: torch.Tensor, u: 
     if _current_device() != device.index:
         with torch.cuda.device(device.index):
             return verify(target, drafted, start, u, r, width=width, draft=draft)
-    n, batch = drafted.shape[0] if drafted.dim() == 1 else -1, r.shape[0] if r.dim() == 1 else -1
-    for name, t, shape, dtype in (("drafted", drafted, (n,), torch.int32), ("start", start, (batch + 1,), torch.int32),
-                                  ("u", u, (n,), torch.float32), ("r", r, (batch,), torch.float32)):
-        if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.device != device:
-            raise ValueError(f"{name} must be a contiguous {dtype} of shape {shape} on {device}")
+    if drafted.dim() != 1 or r.dim() != 1:
+        raise ValueError("drafted and r must have one dimension")
+    n, batch, i32, f32 = drafted.shape[0], r.shape[0], torch.int32, torch.float32
+    if drafted.dtype is not i32 or start.dtype is not i32 or u.dtype is not f32 or r.dtype is not f32 or \
+            start.shape != (batch + 1,) or u.shape != (n,) or drafted.device != device or start.device != device or \
+            u.device != device or r.device != device or not (drafted.is_contiguous() and start.is_contiguous() and
+                                                             u.is_contiguous() and r.is_contiguous()):
+        raise ValueError(f"drafted [{n}] and start [{batch + 1}] must be contiguous int32, u [{n}] and r [{batch}] "
+                         f"contiguous float32, all on {device}")
     if not 1 <= width <= 1 << 20:
         raise ValueError("width must lie between 1 and 2^20")
     ld = _rows(target, n + batch, vocab, target.dtype, device, "target")

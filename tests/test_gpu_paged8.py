@@ -176,6 +176,25 @@ def test_attend_every_code(d_h, new):
     run(x)
 
 
+@pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
+def test_attend_extreme_queries(new):
+    """Rows of the smallest and of very large queries (equal weights, one entry's values), of zeros, and rows with
+    an infinity or a NaN, which become NaN and leave the others alone."""
+    x = Batch8([500, 333], new, 8, 2, 64, seed=16)
+    size = torch.tensor([1e-39, 1e-37, 1e-34, 1e-20, 1e20, 1e28, 0.0, 1.0])[torch.arange(x.tokens * 8) * 5 % 8]
+    x.q = (x.q.float() * size.reshape(x.tokens, 8, 1)).bfloat16()
+    x.plain.q = x.q
+    run(x)
+    c, qs, kl = cache_of(x)
+    want = c.attend(x.q.cuda(), qs, kl)
+    odd = x.q.clone()
+    odd[0, 3, 7], odd[-1, 4, 0] = float("inf"), float("nan")
+    got = c.attend(odd.cuda(), qs, kl)
+    assert got[0, 3].isnan().all() and got[-1, 4].isnan().all()
+    got[0, 3], got[-1, 4] = want[0, 3], want[-1, 4]
+    assert torch.equal(got, want)
+
+
 def test_attend_long():
     run(Batch8([16000, 9000], [1, 1], 8, 2, 128, seed=31))
 
