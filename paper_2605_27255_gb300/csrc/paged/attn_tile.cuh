@@ -188,27 +188,48 @@ __device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
 
 // The codes of a page as an fp16 operand tile: rows of 64 entries, dims in blocks of 64, 128-byte
 // swizzle.  A quarter of the warp takes half of two neighbouring rows (128-dim rows: opposite halves), so that
-// neither its loads nor its stores meet in a bank.  (Two loads in flight: with four or eight unrolled the
-// kernel's warps wait for instructions, 550 us for the 2048-token chunk against 452.)
+// neither its loads nor its stores meet in a bank.  How much is unrolled decides over the whole kernel's time,
+// whose warps wait for instructions (1.6 of the 9 cycles between two of them, against 0.7 in the bf16 kernel): the
+// 2048-token chunk takes 488 us with one group of rows in flight, 472 with two, 449 with four, 517 with eight.
 template <int DH>
 __device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsigned char* src) {
-    constexpr int N = kPage * DH / 16 / 32, B = 2;  // 16-byte chunks of a lane, loads in flight
-    const int lane = threadIdx.x & 31, sub = lane >> 2 & 1, quad = lane & 3, q = lane >> 3;
-    auto row = [&](int i) { return (DH == 128 ? i >> 1 : i) * 8 + q * 2 + sub; };
-    auto half = [&](int i) { return DH == 128 ? sub ^ (i & 1) : 0; };
+    constexpr int U = 4, H = DH / 64;  // groups of eight rows in flight, halves of a row
+    const int lane = threadIdx.x & 31, sub = lane >> 2 & 1, quad = lane & 3, r = (lane >> 3) * 2 + sub;  // row of a group
+    uint32_t from[H], to[H][2];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const int half = DH == 128 ? sub ^ h : 0;
+        from[h] = smem_u32(src) + r * DH + half * 64 + quad * 16;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) to[h][k] = smem_u32(dst) + half * kPageHalf + r * 128 + (((2 * quad + k) ^ r) << 4);
+    }
 #pragma unroll 1
-    for (int i0 = 0; i0 < N; i0 += B) {
-        uint4 x[B];
+    for (int g = 0; g < kPage / 8; g += U) {
+        uint4 x[U][H];
 #pragma unroll
-        for (int i = 0; i < B; ++i) x[i] = *reinterpret_cast<const uint4*>(src + row(i0 + i) * DH + half(i0 + i) * 64 + quad * 16);
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < B; ++i) {
-            const int r = row(i0 + i);
-            unsigned char* d = dst + half(i0 + i) * kPageHalf + r * 128;
-            *reinterpret_cast<uint4*>(d + (((2 * quad) ^ (r & 7)) << 4)) =
-                make_uint4(decode_lo(x[i].x), decode_hi(x[i].x), decode_lo(x[i].y), decode_hi(x[i].y));
-            *reinterpret_cast<uint4*>(d + (((2 * quad + 1) ^ (r & 7)) << 4)) =
-                make_uint4(decode_lo(x[i].z), decode_hi(x[i].z), decode_lo(x[i].w), decode_hi(x[i].w));
+            for (int h = 0; h < H; ++h)
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(x[u][h].x), "=r"(x[u][h].y), "=r"(x[u][h].z), "=r"(x[u][h].w)
+                             : "r"(from[h] + u * 8 * DH));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                const uint4 y = x[u][h];
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to[h][0] + u * 1024), "r"(decode_lo(y.x)),
+                             "r"(decode_hi(y.x)), "r"(decode_lo(y.y)), "r"(decode_hi(y.y))
+                             : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to[h][1] + u * 1024), "r"(decode_lo(y.z)),
+                             "r"(decode_hi(y.z)), "r"(decode_lo(y.w)), "r"(decode_hi(y.w))
+                             : "memory");
+            }
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            from[h] += U * 8 * DH;
+            to[h][0] += U * 1024;
+            to[h][1] += U * 1024;
         }
     }
 }
@@ -224,9 +245,9 @@ __device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsign
 // (Weights as e4m3 parts, so that values need no conversion either, would lose the small ones: a
 // long tail of 2^-17 each next to one large weight.)  Measured for 2048 tokens behind 14336 entries, 32
 // query and 8 kv heads of 128: 2559 us with row tiles of 32 on mma.sync, 692 with keys converted too (by two
-// warps; 592 by three), 541 with key codes as operands, 452 with the scales by shuffles in place of a
-// barrier and a smaller conversion loop; the bf16 pools take 370.  What is left: the scales' part of
-// every page (20 us), key codes in two products' time (20), instruction fetch.
+// warps; 592 by three), 541 with key codes as operands, 465 with the scales by shuffles in place of a
+// barrier, 449 with fixed addresses in the conversion; the bf16 pools take 375.  What is left: instruction
+// fetch, the scales' part of every page (20 us), key codes in two products' time (20).
 template <int DH, bool PAIR, bool SEL, bool E8 = false>
 __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs p, ItemShape shape, int S,
                                                                   int part_rows, size_t part_off,
@@ -676,7 +697,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 if (kept > 0) pos = (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage : kPage - 1);
             }
             float m_ref = -INFINITY, l = 0.f;
-            float v_ref = 0.f, c_row = c2;  // 8-bit pools: the largest value scale so far, what the row's raw scores are worth
+            int v_ref = 0;      // 8-bit pools: the largest value scale so far, as an exponent (0: none)
+            float c_row = c2;   // what the row's raw scores are worth
             if (E8) {
                 ok = wait(q_full + w, (uint32_t)((begun - 1) & 1), 60, begun);
                 if (!ok) break;
@@ -686,17 +708,18 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             // scales eight pages later, so that no page waits for them
             const int pg0 = (it.t0 + it.kv0) * 2, gone = E8 ? first_seen(shape, it.n, it.len, it.tile) / kPage : 0;
             int next_blk = -1;
-            float k_sc = 1.f, v_sc = 0.f, next_k = 1.f, next_v = 0.f;
+            float k_sc = 1.f, next_k = 1.f;
+            int v_sc = 0, next_v = 0;  // (exponents)
             auto block_at = [&](int j) {  // (-1: gone, masked; scales of 1 and 0 change nothing)
                 const int i = pg0 + j + lane;
                 return j + lane < it.pages() && i * kPage < it.len && i >= gone ? page_block(c, it.b, i) : -1;
             };
             auto scales_at = [&](int blk) {
                 next_k = 1.f;
-                next_v = 0.f;
+                next_v = 0;
                 if (blk >= 0) {
                     next_k = p.k_scale[(size_t)blk * c.n_kv + it.g];
-                    next_v = p.v_scale[(size_t)blk * c.n_kv + it.g];
+                    next_v = (int)(__float_as_uint(p.v_scale[(size_t)blk * c.n_kv + it.g]) >> 23 & 255u);
                 }
             };
             if (E8) scales_at(block_at(0));
@@ -707,7 +730,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             const int np = it.pages();
             for (int j = 0; j < np; ++j, ++sn) {
                 const uint32_t s_buf = s_col + (uint32_t)((sn & 1) * 64);
-                float cs = c2, v_now = 0.f;
+                float cs = c2;
+                int v_now = 0;
                 if (E8) {
                     if ((j & 31) == 0) {
                         k_sc = next_k;
@@ -753,7 +777,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     const bool move = top > m_ref + kAtSlack;
                     // 8-bit pools: scores so large that what a fused multiply-add keeps of the maximum itself, up to half a step,
                     // is a power of two that matters are multiplied before the subtraction, which then leaves 0
-                    const bool large = E8 && fabsf(top) > 4194304.f && top > -INFINITY;
+                    const bool large = E8 && !(fabsf(top) <= 4194304.f);  // (or masked altogether)
                     if (__any_sync(0xffffffffu, move || large) || (E8 && v_now > v_ref)) {
                         if (E8 && __any_sync(0xffffffffu, large)) {
 #pragma unroll
@@ -764,7 +788,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         if (move) m_ref = top;
                         l *= f;
                         if (E8 && v_now > v_ref) {
-                            f *= v_ref / v_now;
+                            f *= v_ref > 0 && v_now - v_ref < 126 ? __uint_as_float((uint32_t)(127 + v_ref - v_now) << 23) : 0.f;
                             v_ref = v_now;
                         }
                         if (j > 0) {  // the output so far, once the values of the page before are in it
@@ -787,8 +811,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     float neg = SEL && !sel ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
                     int dv = 0;  // 8-bit pools: the page's value scale against the largest, as an exponent
                     if (E8) {
-                        dv = max((int)(__float_as_uint(v_now) >> 23) - (int)(__float_as_uint(v_ref) >> 23), -24);
-                        neg += (float)dv;
+                        dv = max(v_now - v_ref, -24);
+                        neg += __int_as_float(0x4b400000 + dv) - 12582912.f;  // (dv as fp32, without the conversion's wait)
                     }
                     // two columns at a time (paired fp32 instructions)
                     const uint64_t c22 = f32x2(cs, cs), neg2 = f32x2(neg, neg);
@@ -831,7 +855,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             if (!ok) break;
             tc_fence_after();
             if (live) {
-                const float unit = E8 ? v_ref : 1.f, inv = l > 0.f ? unit / l : 0.f;
+                const float unit = E8 ? __uint_as_float((uint32_t)v_ref << 23) : 1.f, inv = l > 0.f ? unit / l : 0.f;
 #pragma unroll
                 for (int h = 0; h < DH / 32; ++h) {
                     uint32_t v[32];
