@@ -499,10 +499,9 @@ PIPO_API pipo_status pipo_op_attn_pages(const pipo_paged *c, int32_t n_tokens, c
 
 /* ---- the same cache in 8 bits --------------------------------------------
  * Half the bytes of a bf16 cache: keys and values as e4m3 codes with one scale for every
- * block and kv head.  An entry stands for code * scale.  Scales are powers of two
- * between 2^-100 and 2^7 (fp32; magnitudes above 448 * 2^7 = 57344 saturate); the append
- * chooses them, and pools that something else has filled need such scales too.  Queries, gains
- * and outputs are bf16.  Everything else (layout, ragged batches, positions, what may
+ * block and kv head.  An entry stands for code * scale.  The append chooses powers of two
+ * between 2^-100 and 2^7 (fp32; magnitudes above 448 * 2^7 = 57344 saturate); pools that something
+ * else has filled may have any scales from 2^-100 to 2^100.  Queries, gains and outputs are bf16.  Everything else (layout, ragged batches, positions, what may
  * hold anything, what is refused) as for pipo_paged. */
 typedef struct {
     int32_t n_q_heads;

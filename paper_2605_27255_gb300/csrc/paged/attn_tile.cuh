@@ -138,6 +138,15 @@ __device__ __forceinline__ bool elect_one() {
     return e != 0;
 }
 
+// The logarithm of a scale: that of a power of two is exact (its fraction's is that of 1).
+constexpr float kNoScale = -1000.f;
+__device__ __forceinline__ float log2_scale(float x) {
+    const uint32_t u = __float_as_uint(x);
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(__uint_as_float((u & 0x007fffffu) | 0x3f800000u)));
+    return x > 0.f ? (float)((int)(u >> 23) - 127) + y : kNoScale;
+}
+
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -697,8 +706,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 if (kept > 0) pos = (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage : kPage - 1);
             }
             float m_ref = -INFINITY, l = 0.f;
-            int v_ref = 0;      // 8-bit pools: the largest value scale so far, as an exponent (0: none)
-            float c_row = c2;   // what the row's raw scores are worth
+            float v_ref = kNoScale;  // 8-bit pools: the largest value scale so far, as a logarithm
+            float c_row = c2;        // what the row's raw scores are worth
             if (E8) {
                 ok = wait(q_full + w, (uint32_t)((begun - 1) & 1), 60, begun);
                 if (!ok) break;
@@ -708,18 +717,17 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             // scales eight pages later, so that no page waits for them
             const int pg0 = (it.t0 + it.kv0) * 2, gone = E8 ? first_seen(shape, it.n, it.len, it.tile) / kPage : 0;
             int next_blk = -1;
-            float k_sc = 1.f, next_k = 1.f;
-            int v_sc = 0, next_v = 0;  // (exponents)
-            auto block_at = [&](int j) {  // (-1: gone, masked; scales of 1 and 0 change nothing)
+            float k_sc = 1.f, v_sc = kNoScale, next_k = 1.f, next_v = kNoScale;  // (values': logarithms)
+            auto block_at = [&](int j) {  // (-1: gone, masked)
                 const int i = pg0 + j + lane;
                 return j + lane < it.pages() && i * kPage < it.len && i >= gone ? page_block(c, it.b, i) : -1;
             };
             auto scales_at = [&](int blk) {
                 next_k = 1.f;
-                next_v = 0;
+                next_v = kNoScale;
                 if (blk >= 0) {
                     next_k = p.k_scale[(size_t)blk * c.n_kv + it.g];
-                    next_v = (int)(__float_as_uint(p.v_scale[(size_t)blk * c.n_kv + it.g]) >> 23 & 255u);
+                    next_v = log2_scale(p.v_scale[(size_t)blk * c.n_kv + it.g]);
                 }
             };
             if (E8) scales_at(block_at(0));
@@ -731,7 +739,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             for (int j = 0; j < np; ++j, ++sn) {
                 const uint32_t s_buf = s_col + (uint32_t)((sn & 1) * 64);
                 float cs = c2;
-                int v_now = 0;
+                float v_now = kNoScale;
                 if (E8) {
                     if ((j & 31) == 0) {
                         k_sc = next_k;
@@ -788,7 +796,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         if (move) m_ref = top;
                         l *= f;
                         if (E8 && v_now > v_ref) {
-                            f *= v_ref > 0 && v_now - v_ref < 126 ? __uint_as_float((uint32_t)(127 + v_ref - v_now) << 23) : 0.f;
+                            f *= ex2(v_ref - v_now);
                             v_ref = v_now;
                         }
                         if (j > 0) {  // the output so far, once the values of the page before are in it
@@ -809,10 +817,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     }
                     // (a page that the row has not selected: exponents of -infinity)
                     float neg = SEL && !sel ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
-                    int dv = 0;  // 8-bit pools: the page's value scale against the largest, as an exponent
+                    float dv = 0.f;  // 8-bit pools: the page's value scale against the largest, as an exponent
                     if (E8) {
-                        dv = max(v_now - v_ref, -24);
-                        neg += __int_as_float(0x4b400000 + dv) - 12582912.f;  // (dv as fp32, without the conversion's wait)
+                        dv = fmaxf(v_now - v_ref, -24.f);
+                        neg += dv;
                     }
                     // two columns at a time (paired fp32 instructions)
                     const uint64_t c22 = f32x2(cs, cs), neg2 = f32x2(neg, neg);
@@ -830,7 +838,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     if (PARTS == 2) tmem_st32(s_buf + 32, pl);
                     sum[0] = add_f32x2(sum[0], sum[1]);
                     float part = __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
-                    if (E8) part *= __uint_as_float((uint32_t)(127 - dv) << 23);
+                    if (E8) part *= ex2(-dv);
                     l += part;
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 }
@@ -855,7 +863,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             if (!ok) break;
             tc_fence_after();
             if (live) {
-                const float unit = E8 ? __uint_as_float((uint32_t)v_ref << 23) : 1.f, inv = l > 0.f ? unit / l : 0.f;
+                const float unit = E8 ? ex2(v_ref) : 1.f, inv = l > 0.f ? unit / l : 0.f;
 #pragma unroll
                 for (int h = 0; h < DH / 32; ++h) {
                     uint32_t v[32];

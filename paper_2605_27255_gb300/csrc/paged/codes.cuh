@@ -1,6 +1,6 @@
 // 8-bit cache entries: e4m3 codes and the scale that a block of a kv head has.
 //
-// A scale is a power of two between 2^-100 and 2^7, so that multiplying by it rounds
+// The append's scales are powers of two between 2^-100 and 2^7, so that multiplying by one rounds
 // nothing: codes move to a larger scale exactly, but for those that become
 // subnormal, and a code times its scale is a bf16 number.  (A scale from the block's
 // maximum over 448 would fit a little tighter, gain nothing for a floating-point code, and

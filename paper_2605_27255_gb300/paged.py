@@ -278,8 +278,8 @@ class PagedCache(_Cache):
 
 class PagedCache8(_Cache):
     """The same with half the bytes: pools of e4m3 codes (``torch.float8_e4m3fn``) and scales
-    ``k_scale``, ``v_scale`` [n_blocks, n_kv] (fp32, powers of two between 2^-100 and 2^7; ``append``
-    chooses them).  An entry is its code times its block's scale.  Queries, gains and
+    ``k_scale``, ``v_scale`` [n_blocks, n_kv] (fp32; ``append`` chooses powers of two between 2^-100
+    and 2^7, pools filled otherwise may have any from 2^-100 to 2^100).  An entry is its code times its block's scale.  Queries, gains and
     outputs are bf16.  ``append`` and ``attend`` are those of ``PagedCache``; there are no page
     scores.  ``encode`` makes pools from values."""
 
@@ -358,6 +358,8 @@ class BlockTables:
             with torch.cuda.device(self.index):
                 return self.advance(kept, added, tokens)
         n, i32 = self._seqs, torch.int32
+        if n == 0:
+            raise ValueError("tables without sequences")
         for t in (kept, added):
             if t.dtype is not i32 or t.shape != (n,) or not t.is_contiguous() or t.device != self.device:
                 raise ValueError(f"kept and added must be contiguous int32 [{n}] on the tables' device")

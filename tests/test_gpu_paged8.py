@@ -176,6 +176,23 @@ def test_attend_every_code(d_h, new):
     run(x)
 
 
+@pytest.mark.parametrize("d_h", [64, 128])
+@pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
+def test_attend_any_scales(d_h, new):
+    """Pools that were filled by something else: scales that are no powers of two, zeros in whole blocks, and keys
+    and values far from one in size."""
+    x = Batch8([900, 650], new, 8, 2, d_h, seed=18)
+    g = torch.Generator().manual_seed(19)
+    for name, size in (("k", 2.0 ** -30), ("v", 2.0 ** 40)):
+        scale = getattr(x, name + "_scale") * size * (0.5 + torch.rand(x.k_scale.shape, generator=g))
+        codes = getattr(x, name + "8")
+        if name == "v":
+            codes.view(torch.uint8)[x.table[0, 3].item()] = 0
+        setattr(x, name + "_scale", scale)
+        setattr(x.plain, name, codes.double() * scale[..., None, None].double())
+    run(x, scale=2.0 ** 30 * d_h ** -0.5)
+
+
 @pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
 def test_attend_extreme_queries(new):
     """Rows of the smallest and of very large queries (equal weights, one entry's values), of zeros, and rows with

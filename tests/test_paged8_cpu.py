@@ -97,6 +97,8 @@ def test_tensors_that_the_handles_refuse(host8):
             t.advance(kept, added, tokens)
     with pytest.raises(ValueError):
         paged.BlockTables(t.table, t.held, t.free[::2], t.n_free)
+    with pytest.raises(ValueError, match="sequences"):
+        paged.BlockTables.new(0, 3, 9, "cpu").advance(z[:0], z[:0], 4)
 
 
 def test_verify_checks_its_tensors(host8):
