@@ -173,28 +173,34 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
     ItemWalk it;
     it.start(c, shape, piece[0]);
     int slot = 0;
+    // (one column tile) an item's queries: a lane has row grp, 16 dims from 16 tig (and 64 + 16 tig) on, as its keys
+    uint4 x[NT == 1 ? DH / 64 : 1][2];
+    auto load_queries = [&]() {
+        if (NT > 1 || !it.more()) return;
+        const bool live = grp < it.tokens(shape) * c.G;
+        const int t = live ? grp / c.G : 0;
+        const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + it.tile * shape.TP + t) * p.ld_q +
+                          (size_t)(it.g * c.G + (live ? grp - t * c.G : 0)) * DH + tig * 16;
+#pragma unroll
+        for (int h = 0; h < DH / 64; ++h)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                x[NT == 1 ? h : 0][k] = live ? *reinterpret_cast<const uint4*>(q + h * 64 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    load_queries();
     while (it.more()) {
         const int rows = it.tokens(shape) * c.G, i0 = it.tile * shape.TP;
         // ---- queries
         uint2 qf[NT == 1 ? KS : 1];
         float scale_of_row[2] = {1.f, 1.f};  // (one column tile) of this lane's rows 2 tig, 2 tig + 1
         if constexpr (NT == 1) {
-            // every warp for itself: a lane has row grp, 16 dims from 16 tig (and 64 + 16 tig) on, as its keys
-            const int t = grp / c.G;
-            const bf16_t* q = static_cast<const bf16_t*>(p.q) + (size_t)(it.q0 + i0 + (grp < rows ? t : 0)) * p.ld_q +
-                              (size_t)(it.g * c.G + (grp < rows ? grp - t * c.G : 0)) * DH + tig * 16;
-            uint4 x[DH / 64][2];
+            // every warp for itself, loaded before the item that went before was joined
             float most = 0.f;
 #pragma unroll
             for (int h = 0; h < DH / 64; ++h)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    x[h][k] = grp < rows ? *reinterpret_cast<const uint4*>(q + h * 64 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int h = 0; h < DH / 64; ++h)
-#pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const uint32_t u[4] = {x[h][k].x, x[h][k].y, x[h][k].z, x[h][k].w};
+                    const uint32_t u[4] = {x[NT == 1 ? h : 0][k].x, x[NT == 1 ? h : 0][k].y, x[NT == 1 ? h : 0][k].z, x[NT == 1 ? h : 0][k].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(finite_abs(bf_lo(u[e])), finite_abs(bf_hi(u[e]))));
                 }
@@ -207,10 +213,10 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
             for (int h = 0; h < DH / 64; ++h)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    qf[NT == 1 ? h * 4 + 2 * k : 0] = make_uint2(half2_of(bf_lo(x[h][k].x) * f, bf_hi(x[h][k].x) * f),
-                                                                half2_of(bf_lo(x[h][k].y) * f, bf_hi(x[h][k].y) * f));
-                    qf[NT == 1 ? h * 4 + 2 * k + 1 : 0] = make_uint2(half2_of(bf_lo(x[h][k].z) * f, bf_hi(x[h][k].z) * f),
-                                                                    half2_of(bf_lo(x[h][k].w) * f, bf_hi(x[h][k].w) * f));
+                    qf[NT == 1 ? h * 4 + 2 * k : 0] = make_uint2(half2_of(bf_lo(x[NT == 1 ? h : 0][k].x) * f, bf_hi(x[NT == 1 ? h : 0][k].x) * f),
+                                                                half2_of(bf_lo(x[NT == 1 ? h : 0][k].y) * f, bf_hi(x[NT == 1 ? h : 0][k].y) * f));
+                    qf[NT == 1 ? h * 4 + 2 * k + 1 : 0] = make_uint2(half2_of(bf_lo(x[NT == 1 ? h : 0][k].z) * f, bf_hi(x[NT == 1 ? h : 0][k].z) * f),
+                                                                    half2_of(bf_lo(x[NT == 1 ? h : 0][k].w) * f, bf_hi(x[NT == 1 ? h : 0][k].w) * f));
                 }
         } else {
             // a warp per row, four dims a lane
@@ -412,6 +418,13 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
                     o[t][i][2 + h] *= v_ref;
                 }
             }
+        const bool whole = it.whole();
+        float* part = reinterpret_cast<float*>(p.scratch + part_off) + ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
+        const int first_row = it.q0 + i0, g = it.g;
+        if (it.begun() && threadIdx.x == 0)
+            reinterpret_cast<SharedItem*>(p.scratch)[me] = {first_row, rows, g, it.last_worker(piece[0])};
+        it.next(c, shape);
+        load_queries();
         float* my_o = join_s + (size_t)(warp & 3) * ROWS * DH;
         float* my_ml = join_s + (size_t)4 * ROWS * DH + (warp & 3) * ROWS * 2;
         auto leave = [&]() {
@@ -457,10 +470,6 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
             leave();
         }
         __syncthreads();
-        const bool whole = it.whole();
-        float* part = reinterpret_cast<float*>(p.scratch + part_off) + ((size_t)me * 2 + (it.kv0 == 0 ? 1 : 0)) * part_floats(part_rows, DH);
-        if (it.begun() && threadIdx.x == 0)
-            reinterpret_cast<SharedItem*>(p.scratch)[me] = {it.q0 + i0, rows, it.g, it.last_worker(piece[0])};
         const float* ml = join_s + (size_t)4 * ROWS * DH;
         for (int i = threadIdx.x; i < rows * (DH / 4); i += THREADS) {
             const int r = i / (DH / 4), d = i % (DH / 4) * 4;
@@ -487,15 +496,14 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
                 const int t = r / c.G;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) x[k] *= inv;
-                store_f<bf16_t, 4>(static_cast<bf16_t*>(p.out) + (size_t)(it.q0 + i0 + t) * p.ld_out +
-                                       (size_t)(it.g * c.G + r - t * c.G) * DH + d,
+                store_f<bf16_t, 4>(static_cast<bf16_t*>(p.out) + (size_t)(first_row + t) * p.ld_out +
+                                       (size_t)(g * c.G + r - t * c.G) * DH + d,
                                    x);
             } else {
                 *reinterpret_cast<float4*>(part + ((size_t)(d / 4) * part_rows + r) * 4) = make_float4(x[0], x[1], x[2], x[3]);
                 if (d == 0) *reinterpret_cast<float2*>(part + (size_t)part_rows * DH + 2 * r) = make_float2(M, L);
             }
         }
-        it.next(c, shape);
         __syncthreads();  // the joining memory is read
     }
     cp_async_wait<0>();

@@ -84,6 +84,7 @@ struct Piece {
     int left;            // of the line, from that unit on (0: nothing to do)
     long long end, total;  // end of the piece, length of the line
     int workers;         // S, or as many as the line is long
+    int n, len;          // of the sequence: new tokens, entries
 };
 
 // Ints of shared memory that find_pieces uses
@@ -184,7 +185,8 @@ __device__ __forceinline__ void find_pieces(const PagedArgs& c, const ItemShape&
                 }
                 const int g = (int)div_up_to_64(u0 - at, len), off = (int)(u0 - at - (long long)g * len) - kItemCost;
                 // (a piece that starts before the item's first unit)
-                out[w] = {b, j, g, max(0, off), max(0, (int)(u1 - u0) + min(0, off)), u1, total, Sw};
+                out[w] = {b, j, g, max(0, off), max(0, (int)(u1 - u0) + min(0, off)), u1, total, Sw,
+                          seq_n[b], seq_l[b]};
                 return true;
             });
         }
@@ -209,7 +211,11 @@ struct ItemWalk {
         g = p.g;
         left = p.left;
         kv0 = p.kv;
-        if (left > 0) load(c, s);
+        if (left == 0) return;
+        n = p.n;
+        len = p.len;
+        q0 = q_row(c, b);
+        shape(s);
     }
     __device__ __forceinline__ void load(const PagedArgs& c, const ItemShape& s) {
         n = seq_new(c, b);
