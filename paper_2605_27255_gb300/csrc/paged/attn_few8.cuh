@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
             slot = slot + 1 == ST ? 0 : slot + 1;
             const int e0 = (it.t0 + u) * kTileEnt + warp * EW;
             // (the sums of the two halves of the dims apart where registers allow: shorter chains)
-            constexpr int CH = DH == 128 && NT <= 2 ? 2 : 1;
+            constexpr int CH = DH == 128 && NT == 1 ? 2 : 1;
             float s[ET][NT][4], s2[CH][ET][NT][4];
 #pragma unroll
             for (int x = 0; x < ET; ++x)

@@ -32,6 +32,10 @@ cudaError_t few8_as(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) 
     const ItemShape shape{pl.TP, a.window, 0};
     const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), few_threads(DH, NT), few_smem(DH, NT, a.c.batch), s, a, shape,
                                      pl.workers, pl.part_rows, pl.part_off);
+    // (blocks of 32 rows would idle with tiles of 8: 64 sequences of five rows 36.6 us, so 33)
+    if (e == cudaSuccess && pl.join && NT == 1)
+        return launch_pdl(&combine_kernel<DH, bf16_t, 8>, dim3((unsigned)pl.workers, 1, DH / 16), 128, 0, s, a, pl.workers,
+                          pl.part_rows, pl.part_off);
     return e == cudaSuccess ? launch_combine<DH, bf16_t>(a, pl, s) : e;
 }
 

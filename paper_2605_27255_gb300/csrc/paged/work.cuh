@@ -265,12 +265,12 @@ struct ItemWalk {
 // A block takes 32 dims of 32 rows in 2 slices of the parts (a thread: one row, 16 dims; most
 // items of chunks are shared by two), or, where no tile has more than 4 rows, 16 dims in 8
 // slices (a thread: 4 dims), so that a few parts' loads are all in flight at once; the slices are
-// added up in order.  (One thread for all parts of a row: 12 us of the 59 of four decoding
+// added up in order.  (Eight rows, for tiles of as many over 8-bit pools: 16 dims in 4 slices.)  (One thread for all parts of a row: 12 us of the 59 of four decoding
 // sequences of 15.5 K entries.)
 template <int DH, typename T, int RP>
 __device__ __forceinline__ void join_rows(const AttnPagedArgs& a, const SharedItem& m, const float* parts, int part_rows,
                                           float* tmp) {
-    constexpr int PS = RP == 32 ? 2 : 8, NC = RP == 32 ? 4 : 1, V = NC * 4 + 2;  // slices; 4-dim groups; values passed on
+    constexpr int PS = RP == 32 ? 2 : RP == 8 ? 4 : 8, NC = RP == 32 ? 4 : 1, V = NC * 4 + 2;  // slices; 4-dim groups; values passed on
     constexpr int CG = 128 / (RP * PS);                                          // threads of a row and slice
     const int t = threadIdx.x, rl = t % RP, row = blockIdx.y * 32 + rl, ps = t * PS / 128;
     const int first = blockIdx.x, n = m.last - first + 1, c0 = (blockIdx.z * CG + t / RP % CG) * NC;
