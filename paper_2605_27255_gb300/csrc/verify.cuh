@@ -13,7 +13,9 @@
 // sums its slice of the vocabulary warp by warp, and learns the others' sums through
 // distributed shared memory; the one that holds the drawn place goes through the right
 // warp's slice once more.  Bound by the row's read (and the draft row's) and, for few sequences, by
-// the chain of start, drafted token, probabilities, row.
+// the chain of start, drafted token, probabilities, row.  Measured back to back with a vocabulary of 151936 in
+// fp32: 64 sequences 14.7 us (52 MB read), one 8.8 us.  Four loads of either row in flight take 50
+// registers, so that 512 CTAs need two rounds (16.8 and 8.0 us); CTAs of 256 threads 17.3 and 12.4.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -57,7 +59,7 @@ __device__ __forceinline__ void ver_load(const T* p, int i, int n, float (&x)[N]
 // even, as hi 2^22 + lo.  Adding 2^23 rounds a number below it to a whole one, whose bits lie
 // at the sum's low end; what is left over is exact and is rounded in the same way, at 2^22 times its
 // size (conversions to 64-bit integers, a few a cycle of an SM, took half of the kernel's time:
-// 33 us for 64 sequences of 151936 tokens).
+// 30 us for 64 sequences of 151936 tokens).
 struct VerWeight {
     int hi, lo;  // 0 .. 2^22, -2^21 .. 2^21
 };
