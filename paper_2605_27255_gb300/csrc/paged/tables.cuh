@@ -18,7 +18,8 @@
 namespace pipo {
 
 constexpr int kTabThreads = 1024, kTabPer = kPagedMaxBatch / kTabThreads;  // requests of a thread
-// Tokens up to which the same launch writes the slots too
+// Tokens up to which the same launch writes the slots too (16 requests, in a graph: 2048 tokens 6.8 us by one launch,
+// 7.7 by two; 4096 7.6 and 7.8; 8192 9.5 and 7.9)
 constexpr int kTabInline = 4096;
 
 __host__ __device__ constexpr size_t tables_smem(int batch) { return (size_t)(4 * batch + 3) * 4; }

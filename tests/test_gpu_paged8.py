@@ -241,6 +241,55 @@ def test_attend_on_another_stream_and_in_a_graph():
     check(out, ref_attend(x.plain, 128 ** -0.5), values_top(x))
 
 
+def test_attend_on_two_streams_and_in_two_graphs_at_once():
+    """One object, calls that overlap: scratch is a stream's, or a graph's, own."""
+    small, large = Batch8([900, 300], [1, 2], 32, 8, 128, seed=41), Batch8([900, 300], [300, 120], 32, 8, 128, seed=41)
+    c, _, kl = cache_of(small)
+    work = [(x.q.cuda(), x.q_start.cuda()) for x in (small, large)]
+    want = [c.attend(q, qs, kl).clone() for q, qs in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    got = [[], []]
+    for _ in range(5):
+        for i, (q, qs) in enumerate(work):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(c.attend(q, qs, kl))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(want[i], y) for y in got[i])
+    graphs, out = [], []
+    for q, qs in work:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out.append(c.attend(q, qs, kl))
+        graphs.append(g)
+    for o in out:
+        o.zero_()
+    for _ in range(5):
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, out))
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [1, 200, 70]])
+def test_attend_empty_wide_and_clamped(new):
+    """Sequences without entries, a table far wider than they need, lengths beyond it and below zero."""
+    x = Batch8([130, 300, 64], new, 8, 2, 64, seed=42, width=5000)
+    c, qs, kl = cache_of(x)
+    q = x.q.cuda()
+    check(c.attend(q, qs, kl), ref_attend(x.plain, 64 ** -0.5), values_top(x))
+    for n in (0, -5, -2 ** 31):
+        assert (c.attend(q, qs, torch.full_like(kl, n)) == 0).all()
+    x = Batch8([128, 320, 64], new, 8, 2, 64, seed=43, width=5)
+    c, qs, kl = cache_of(x)
+    blocks = [t for row in x.table.tolist() for t in row if 0 <= t < x.x.blocks]
+    c.table.copy_(torch.tensor((blocks * 5)[:15], dtype=torch.int32).reshape(3, 5))  # (every page is some block)
+    top = torch.full_like(kl, 320)
+    assert torch.equal(c.attend(q, qs, torch.full_like(kl, 2 ** 31 - 1)), c.attend(q, qs, top))
+
+
 @pytest.mark.parametrize("new", [[1, 1, 3], [200, 1, 64]])
 def test_attend_same_inputs_same_bits(new):
     x = Batch8([1500, 300, 2000], new, 32, 8, 128, seed=9)
