@@ -534,7 +534,10 @@ PIPO_API pipo_status pipo_op_kv_append8(const pipo_paged8 *c, int32_t n_tokens, 
                                         int32_t n_rope, void *d_q_out, void *stream);
 
 /* Causal attention over an 8-bit cache, as pipo_op_attn_paged, with scratch of
- * pipo_op_attn_paged8_scratch(c, n_tokens) bytes.  Scores, softmax and sums are fp32. */
+ * pipo_op_attn_paged8_scratch(c, n_tokens) bytes.  Scores, softmax and sums are fp32;
+ * the softmax weights meet the values in fp16 (an error of an eighth of the output's own rounding).
+ * Which kernel runs goes by the batch's average of rows per sequence, so the low bits of a sequence's
+ * outputs depend on what shares its batch; the same call gives the same bits. */
 PIPO_API pipo_status pipo_op_attn_paged8(const pipo_paged8 *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
                                          float scale, int32_t window, void *d_out, int64_t ld_out, void *d_scratch,
                                          size_t scratch_bytes, void *stream);

@@ -78,15 +78,18 @@ __host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
            (size_t)at_page_bytes(dh) * (at_k_pages(dh, pair) + at_v_pages(dh, pair)) * (pair ? 1 : 2);
 }
 
-// 8-bit pools: pages of key codes, of value operands and of value codes on their way to those
-__host__ __device__ constexpr int at8_k_pages(int dh) { return dh == 128 ? 5 : 8; }
-__host__ __device__ constexpr int at8_v_pages(int dh) { return dh == 128 ? 4 : 6; }
-__host__ __device__ constexpr int at8_raw_pages(int dh) { return dh == 128 ? 5 : 8; }
-constexpr int kAt8Convert = 3;  // converting warps: 2, 12 and 14
+// 8-bit pools: pages of key codes, of value operands and of value codes on their way to those, in a ring each
+// (single: per pipeline)
+__host__ __device__ constexpr int at8_k_pages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 3 : 6); }
+__host__ __device__ constexpr int at8_v_pages(int dh, bool pair) { return pair ? (dh == 128 ? 4 : 6) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr int at8_raw_pages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr int at8_convert(bool pair) { return pair ? 3 : 1; }  // converting warps of a ring
 __host__ __device__ constexpr int at8_codes(int dh) { return kPage * dh; }
-__host__ __device__ constexpr size_t at8_smem(int dh) {
-    return 1024 + 2 * (size_t)at_q_bytes(dh) + (size_t)at_page_bytes(dh) * at8_v_pages(dh) +
-           (size_t)at8_codes(dh) * (at8_k_pages(dh) + at8_raw_pages(dh));
+__host__ __device__ constexpr int at8_ring_bytes(int dh, bool pair) {
+    return at_page_bytes(dh) * at8_v_pages(dh, pair) + at8_codes(dh) * (at8_k_pages(dh, pair) + at8_raw_pages(dh, pair));
+}
+__host__ __device__ constexpr size_t at8_smem(int dh, bool pair) {
+    return 1024 + 2 * (size_t)at_q_bytes(dh) + (size_t)at8_ring_bytes(dh, pair) * (pair ? 1 : 2);
 }
 
 // B operand [entries][dims] of a page (MN-major, 128-byte swizzle): 64-dim blocks kPageHalf apart,
@@ -244,11 +247,12 @@ __device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsign
 }
 
 // SEL: whole tiles over selected pages (AttnPagedArgs::bits), PAIR only.
-// E8: pools of e4m3 codes, PAIR only.  Key codes are operands as they are (kind::f8f6f4): queries are scaled
+// E8: pools of e4m3 codes.  Key codes are operands as they are (kind::f8f6f4): queries are scaled
 // by a power of two per row to below 256 and meet them as two e4m3 parts, which hold all digits of
 // a bf16 number down to 2^-10 of the row's largest (below that 2^-18 of the largest are lost).  The two
 // parts cost what one bf16 operand does.  The row's and the block's scale meet the
-// scores in fp32.  Value codes become fp16 tiles (a code is an fp16 number) by warps 2, 12 and 14; their
+// scores in fp32.  Value codes become fp16 tiles (a code is an fp16 number) by warps 2, 12 and 14 (single: 12 and
+// 14, one per pipeline); their
 // scales go into the weights, relative to the largest so far (2^-24 at least: what that
 // adds to an output is below 2^-20 of its largest value), and weights keep fp16's 11 digits.
 // (Weights as e4m3 parts, so that values need no conversion either, would lose the small ones: a
@@ -263,10 +267,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                                                   const __grid_constant__ CUtensorMap tmK,
                                                                   const __grid_constant__ CUtensorMap tmV) {
     constexpr int kTile = at_q_bytes(DH), kPg = at_page_bytes(DH), NR = PAIR ? 1 : 2;  // NR: pairs of rings
-    constexpr int PARTS = PAIR ? 1 : 2;  // bf16 parts of the weights
-    constexpr int SK = E8 ? at8_k_pages(DH) : at_k_pages(DH, PAIR), SV = E8 ? at8_v_pages(DH) : at_v_pages(DH, PAIR);
-    constexpr int SR = at8_raw_pages(DH), kCodes = at8_codes(DH);
-    static_assert(!E8 || (PAIR && !SEL), "8-bit pools: chunks");
+    constexpr int PARTS = PAIR || E8 ? 1 : 2;  // parts of the weights
+    constexpr int SK = E8 ? at8_k_pages(DH, PAIR) : at_k_pages(DH, PAIR), SV = E8 ? at8_v_pages(DH, PAIR) : at_v_pages(DH, PAIR);
+    constexpr int SR = at8_raw_pages(DH, PAIR), kCodes = at8_codes(DH);
+    static_assert(!E8 || !SEL, "selected pages: bf16 pools");
     extern __shared__ __align__(1024) unsigned char at_smem_raw[];
     __shared__ uint32_t tmem_base;
     __shared__ __align__(8) uint64_t k_full[NR][SK], k_empty[NR][SK], v_full[NR][SV], v_empty[NR][SV];
@@ -274,8 +278,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
     __shared__ Piece pieces[NR];
     __shared__ int give_up;
     // 8-bit pools: ring of value codes, the queries' row scales
-    __shared__ __align__(8) uint64_t raw_full[E8 ? SR : 1], raw_empty[E8 ? SR : 1];
-    __shared__ bool raw_live[E8 ? SR : 1];
+    __shared__ __align__(8) uint64_t raw_full[E8 ? NR : 1][E8 ? SR : 1], raw_empty[E8 ? NR : 1][E8 ? SR : 1];
+    __shared__ bool raw_live[E8 ? NR : 1][E8 ? SR : 1];
     __shared__ float row_scale[E8 ? 2 : 1][E8 ? 2 : 1][E8 ? 128 : 1];  // [item's parity][pipeline][row]
 
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -309,10 +313,11 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             mbar_init(drained + 2 * w + 1, 1);
         }
         if (E8) {
-            for (int i = 0; i < SR; ++i) {
-                mbar_init(raw_full + i, 1);
-                mbar_init(raw_empty + i, 1);
-            }
+            for (int r = 0; r < NR; ++r)
+                for (int i = 0; i < SR; ++i) {
+                    mbar_init(&raw_full[r][i], 1);
+                    mbar_init(&raw_empty[r][i], 1);
+                }
         }
         give_up = 0;
         mbar_init_fence();
@@ -343,8 +348,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             ItemWalk it;
             it.start(c, shape, pieces[ring]);
             // (8-bit pools: value operands, key codes, value codes)
-            unsigned char* k_s = E8 ? ring_s + SV * kPg : ring_s + (size_t)ring * (SK + SV) * kPg;
-            unsigned char* v_s = E8 ? ring_s : k_s + SK * kPg;
+            unsigned char* k_s = E8 ? ring_s + ring * at8_ring_bytes(DH, PAIR) + SV * kPg : ring_s + (size_t)ring * (SK + SV) * kPg;
+            unsigned char* v_s = E8 ? k_s - SV * kPg : k_s + SK * kPg;
             if (E8 && (warp & 1) == 0) {
                 // ---- copies of codes: the keys one page ahead of the values
                 unsigned char* raw_s = k_s + SK * kCodes;
@@ -364,14 +369,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             }
                             blk = __shfl_sync(0xffffffffu, mine, j - held);
                             const int st = kn % SK;
-                            ok = kn < SK || wait(&k_empty[0][st], (uint32_t)(((kn / SK) & 1) ^ 1), 51, kn);
+                            ok = kn < SK || wait(&k_empty[ring][st], (uint32_t)(((kn / SK) & 1) ^ 1), 51, kn);
                             if (!ok) break;
                             if (lane == 0) {
                                 if (blk < 0) {
-                                    mbar_arrive(&k_full[0][st]);
+                                    mbar_arrive(&k_full[ring][st]);
                                 } else {
-                                    mbar_arrive_expect_tx(&k_full[0][st], (uint32_t)kCodes);
-                                    tma_load_2d(k_s + st * kCodes, &tmK, 0, (blk * c.n_kv + it.g) * kPage, &k_full[0][st]);
+                                    mbar_arrive_expect_tx(&k_full[ring][st], (uint32_t)kCodes);
+                                    tma_load_2d(k_s + st * kCodes, &tmK, 0, (blk * c.n_kv + it.g) * kPage, &k_full[ring][st]);
                                 }
                             }
                             ++kn;
@@ -379,15 +384,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         }
                         if (j > 0) {
                             const int st = vn % SR;
-                            ok = vn < SR || wait(raw_empty + st, (uint32_t)(((vn / SR) & 1) ^ 1), 51, vn);
+                            ok = vn < SR || wait(&raw_empty[ring][st], (uint32_t)(((vn / SR) & 1) ^ 1), 51, vn);
                             if (!ok) break;
                             if (lane == 0) {
-                                raw_live[st] = prev >= 0;
+                                raw_live[ring][st] = prev >= 0;
                                 if (prev < 0) {
-                                    mbar_arrive(raw_full + st);
+                                    mbar_arrive(&raw_full[ring][st]);
                                 } else {
-                                    mbar_arrive_expect_tx(raw_full + st, (uint32_t)kCodes);
-                                    tma_load_2d(raw_s + st * kCodes, &tmV, 0, (prev * c.n_kv + it.g) * kPage, raw_full + st);
+                                    mbar_arrive_expect_tx(&raw_full[ring][st], (uint32_t)kCodes);
+                                    tma_load_2d(raw_s + st * kCodes, &tmV, 0, (prev * c.n_kv + it.g) * kPage, &raw_full[ring][st]);
                                 }
                             }
                             ++vn;
@@ -397,8 +402,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     }
                 }
                 if (lane == 0) {
-                    ring_drain<SK>(kn, [&](int st, uint32_t ph, int i) { mbar_wait(&k_full[0][st], ph, 52, (unsigned)i); });
-                    ring_drain<SR>(vn, [&](int st, uint32_t ph, int i) { mbar_wait(raw_full + st, ph, 52, (unsigned)i); });
+                    ring_drain<SK>(kn, [&](int st, uint32_t ph, int i) { mbar_wait(&k_full[ring][st], ph, 52, (unsigned)i); });
+                    ring_drain<SR>(vn, [&](int st, uint32_t ph, int i) { mbar_wait(&raw_full[ring][st], ph, 52, (unsigned)i); });
                 }
             } else if ((warp & 1) == 0) {
                 // ---- copies: the keys one page ahead of the values
@@ -571,24 +576,25 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
         } else if (E8) {
             // ---- value codes to operands: the converting warps take the pages in turn
             ItemWalk it;
-            it.start(c, shape, pieces[0]);
-            const int me = warp == 2 ? 2 : (warp - 12) >> 1;
-            unsigned char *v_s = ring_s, *raw_s = ring_s + SV * kPg + SK * kCodes;
+            const int rg = PAIR ? 0 : (warp - 12) >> 1, me = PAIR ? (warp == 2 ? 2 : (warp - 12) >> 1) : 0;
+            constexpr int W = at8_convert(PAIR);
+            it.start(c, shape, pieces[rg]);
+            unsigned char *v_s = ring_s + rg * at8_ring_bytes(DH, PAIR), *raw_s = v_s + SV * kPg + SK * kCodes;
             int n = 0;  // pages before the present item
             bool ok = true;
             for (; it.more() && ok; it.next(c, shape)) {
                 const int end = n + it.pages();
-                for (int i = n + (me + kAt8Convert - n % kAt8Convert) % kAt8Convert; i < end; i += kAt8Convert) {
+                for (int i = n + (me + W - n % W) % W; i < end; i += W) {
                     const int st = i % SR, to = i % SV;
-                    ok = wait(raw_full + st, (uint32_t)((i / SR) & 1), 61, i) &&
-                         (i < SV || wait(&v_empty[0][to], (uint32_t)(((i / SV) & 1) ^ 1), 62, i));
+                    ok = wait(&raw_full[rg][st], (uint32_t)((i / SR) & 1), 61, i) &&
+                         (i < SV || wait(&v_empty[rg][to], (uint32_t)(((i / SV) & 1) ^ 1), 62, i));
                     if (!ok) break;
-                    if (raw_live[st]) page_from_codes<DH>(v_s + to * kPg, raw_s + st * kCodes);
+                    if (raw_live[rg][st]) page_from_codes<DH>(v_s + to * kPg, raw_s + st * kCodes);
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(&v_full[0][to]);
-                        mbar_arrive(raw_empty + st);
+                        mbar_arrive(&v_full[rg][to]);
+                        mbar_arrive(&raw_empty[rg][st]);
                     }
                     __syncwarp();
                 }

@@ -46,24 +46,38 @@ cudaError_t launch_kv_append8(const AppendArgs& a, cudaStream_t s) {
 }
 
 // The plan of attention over 8-bit pools by the rows (new tokens times query heads of a kv head) that the
-// batch's sequences have on average: row tiles of 8, 16 or 32 rows, and above kFewRows pairs of 128 on tcgen05.
-// (16 sequences of 2000 entries, 32 query and 8 kv heads of 128 / 16 and 16 of 64: 64 rows 60 / 79 us with few rows,
-// 66 / 99 with pairs; 96 rows 83 / 112 and 66 / 109; one sequence of 4000: 64 rows 19 / 21 and 24 / 22.)
-constexpr int kFewRows = 64;
+// batch's sequences have on average: row tiles of 8, 16 or 32 rows on mma.sync; tiles of 128 on tcgen05, two
+// pipelines with items of their own; above 128 rows pairs of tiles that share a pipeline's pages.  Where mma.sync
+// would read the cache twice (33 to 64 rows) it goes by the work: with few sequences and heads its short start
+// counts.  Measured in us, 32 query and 8 kv heads of 128 / 16 and 16 of 64, mma.sync, single tiles, pairs:
+//   one sequence of 4000 entries, 64 rows   19 / 21    27 / 22    24 / 22
+//   4 of 2000, 64 rows                      26 / 29    26 / 25    28 / 36
+//   16 of 2000, 32 rows                     37 / 44    53 / 63    65 / 87
+//   16 of 2000, 64 rows                     60 / 80    55 / 68    66 / 99
+//   16 of 2000, 128 rows                   105 / 145   58 / 73    73 / 116
+constexpr int kFewRows = 32, kFewRowsStart = 64, kManyItems = 32;
 AttnPlan plan_attn8(const PagedArgs& c, int dev, int sms) {
     AttnPlan pl{};
     pl.dev = dev;
     const long long mine = (long long)c.n_tokens * c.G;
-    if (mine > (long long)kFewRows * c.batch) {
-        pl.pair = true;
-        pl.TP = 256 / c.G;
+    int per = 1;  // workers of an SM
+    const int few = (long long)c.batch * c.n_kv >= kManyItems ? kFewRows : kFewRowsStart;
+    if (mine > (long long)few * c.batch) {
+        pl.pair = mine > 128LL * c.batch;
+        pl.TP = (pl.pair ? 256 : 128) / c.G;
+        per = pl.pair ? 1 : 2;
     } else {
         pl.rt = c.G <= 8 && mine <= 8LL * c.batch ? 1 : mine <= 16LL * c.batch ? 2 : 4;
         pl.TP = 8 * pl.rt / c.G;
+        per = few_ctas(c.dh, pl.rt);
     }
     pl.tiles = tiles_bound(c.n_tokens, c.batch, pl.TP);
-    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each, all = (long long)sms * (pl.pair ? 1 : few_ctas(c.dh, pl.rt));
+    const long long each = (c.max_pages + 1) / 2, most = pl.tiles * c.n_kv * each, all = (long long)sms * per;
     pl.workers = pl.ctas = (int)(most < all ? most : all);
+    if (!pl.rt && !pl.pair) {  // two workers of a CTA
+        pl.ctas = (pl.workers + 1) / 2;
+        pl.workers = 2 * pl.ctas;
+    }
     pl.join = each > 1;
     pl.part_rows = (int)(mine < (long long)pl.TP * c.G ? mine : (long long)pl.TP * c.G);
     pl.part_rows += pl.part_rows & 1;

@@ -22,20 +22,20 @@ cudaError_t tile_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMa
     return e == cudaSuccess ? launch_combine<DH, bf16_t>(a, pl, s) : e;
 }
 
-template <int DH>
+template <int DH, bool PAIR>
 cudaError_t tile8_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
                      cudaStream_t s) {
-    auto* fn = &attn_tile_kernel<DH, true, false, true>;
+    auto* fn = &attn_tile_kernel<DH, PAIR, false, true>;
     static thread_local int ready_dev = -1;  // the shared-memory limit is set per device
-    static_assert(at8_smem(DH) >= 1024 + 2 * (size_t)at_q_bytes(DH) + find_ints(kPagedMaxBatch) * 4,
+    static_assert(at8_smem(DH, PAIR) >= 1024 + 2 * (size_t)at_q_bytes(DH) + find_ints(kPagedMaxBatch) * 4,
                   "the search for the pieces uses the rings' memory");
     if (ready_dev != pl.dev) {
-        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at8_smem(DH));
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at8_smem(DH, PAIR));
         if (e != cudaSuccess) return e;
         ready_dev = pl.dev;
     }
     const ItemShape shape{pl.TP, a.window, 0};
-    const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kAtThreads, at8_smem(DH), s, a, shape, pl.workers,
+    const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), kAtThreads, at8_smem(DH, PAIR), s, a, shape, pl.workers,
                                      pl.part_rows, pl.part_off, tk, tv);
     return e == cudaSuccess ? launch_combine<DH, bf16_t>(a, pl, s) : e;
 }
@@ -105,7 +105,8 @@ cudaError_t launch_attn_tile(const AttnPagedArgs& a, const AttnPlan& pl, const C
 
 cudaError_t launch_attn_tile8(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorMap& tk, const CUtensorMap& tv,
                               cudaStream_t s) {
-    return a.c.dh == 64 ? tile8_as<64>(a, pl, tk, tv, s) : tile8_as<128>(a, pl, tk, tv, s);
+    if (a.c.dh == 64) return pl.pair ? tile8_as<64, true>(a, pl, tk, tv, s) : tile8_as<64, false>(a, pl, tk, tv, s);
+    return pl.pair ? tile8_as<128, true>(a, pl, tk, tv, s) : tile8_as<128, false>(a, pl, tk, tv, s);
 }
 
 cudaError_t take_error_paged(unsigned* code, unsigned* info) { return take_unit_error(code, info); }

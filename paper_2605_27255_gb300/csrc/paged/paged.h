@@ -71,7 +71,7 @@ inline __host__ __device__ int bit_words(int max_pages) { return (max_pages + 31
 struct AttnPlan {
     int dev;
     bool pair;          // bf16: two 128-row tiles per item share the copies
-    int rt;             // fp32: rows of a tile / 16; 8-bit pools, few rows: rows of a tile / 8
+    int rt;             // fp32: rows of a tile / 16; 8-bit pools: rows of a tile / 8 for few rows, else 0
     bool join;          // items may be shared between workers
     bool listed;        // selected pages: a token's own list; else whole tiles with bits
     int TP;             // tokens per row tile

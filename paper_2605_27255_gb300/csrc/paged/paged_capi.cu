@@ -357,7 +357,7 @@ pipo_status pipo_op_attn_paged8(const pipo_paged8* c8, int32_t n_tokens, const v
     a.k_scale = c8->k_scale;
     a.v_scale = c8->v_scale;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (!pl.pair) return cuda_status("pipo_op_attn_paged8", launch_attn_few8(a, pl, s));
+    if (pl.rt) return cuda_status("pipo_op_attn_paged8", launch_attn_few8(a, pl, s));
     CUtensorMap tk, tv;
     pipo_status st = pool_map("pipo_op_attn_paged8", &tk, a.c.k, a.c, PoolKind::kKeyCodes);
     if (st == PIPO_OK) st = pool_map("pipo_op_attn_paged8", &tv, a.c.v, a.c, PoolKind::kValueCodes);

@@ -60,6 +60,8 @@ SHAPES = {
     "long": ([2500, 1900], [1, 2]),
     "drafts": ([640, 641, 130], [4, 4, 4]),
     "few": ([300, 17, 129], [9, 8, 7]),
+    "middle": ([700, 90, 333, 0], [20, 30, 16, 0]),
+    "middle-64": ([64, 128, 65, 1], [23, 22, 21, 1]),
 }
 
 
@@ -71,13 +73,13 @@ def test_attend_matches_float64(heads, shape):
 
 
 @pytest.mark.parametrize("d_h", [64, 128])
-@pytest.mark.parametrize("new", [[1, 1, 1, 1], [3, 1, 1, 9], [90, 1, 1, 300]])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [3, 1, 1, 9], [20, 1, 1, 60], [90, 1, 1, 300]])
 @pytest.mark.parametrize("window", [1, 2, 63, 64, 65, 200, 100000, 2 ** 31 - 1])
 def test_attend_window(d_h, new, window):
     run(Batch8([400, 70, 1, 300], new, 8, 2, d_h, seed=window % 1000), window)
 
 
-@pytest.mark.parametrize("new", [[5, 2, 1], [150, 2, 1]])
+@pytest.mark.parametrize("new", [[5, 2, 1], [60, 2, 1], [150, 2, 1]])
 def test_tokens_without_an_entry_and_rows_of_no_sequence(new):
     """More new tokens than entries: zero outputs and nothing appended; rows
     outside every sequence stay as they were."""
@@ -120,7 +122,7 @@ def test_attend_strided_rows(new):
 
 
 @pytest.mark.parametrize("d_h", [64, 128])
-@pytest.mark.parametrize("new", [[1, 1, 1, 1], [7, 1, 3, 4], [7, 1, 130, 40], [200, 300, 5, 333]])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [7, 1, 3, 4], [30, 20, 10, 22], [7, 1, 130, 40], [200, 300, 5, 333]])
 @pytest.mark.parametrize("window", [1, 50, 64, 200])
 def test_attend_window_over_pages_that_are_gone(d_h, new, window):
     """What the window has passed for all of a sequence's new tokens may be NaN, codes and scales,
@@ -142,13 +144,13 @@ def test_attend_window_over_pages_that_are_gone(d_h, new, window):
 
 
 @pytest.mark.parametrize("d_h", [64, 128])
-@pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
+@pytest.mark.parametrize("new", [[1, 1], [6, 5], [20, 18], [60, 200]])
 def test_attend_blocks_of_different_scales(d_h, new):
     """Values of blocks that differ by up to 2^20, keys by up to 2^3: scales differ block by block."""
     run(Batch8([900, 650], new, 8, 2, d_h, seed=4, v_mult=(-18, 2), k_mult=(-2, 1)))
 
 
-@pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
+@pytest.mark.parametrize("new", [[1, 1], [6, 5], [20, 18], [60, 200]])
 def test_attend_sharp_flat_and_tiny(new):
     """Queries of very different size in one tile: scores that single out one entry, or none."""
     x = Batch8([500, 333], new, 8, 2, 128, seed=6)
@@ -160,7 +162,7 @@ def test_attend_sharp_flat_and_tiny(new):
 
 
 @pytest.mark.parametrize("d_h", [64, 128])
-@pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
+@pytest.mark.parametrize("new", [[1, 1], [6, 5], [20, 18], [60, 200]])
 def test_attend_every_code(d_h, new):
     """Pools of random bytes (all but NaN), subnormal codes among them, and blocks of subnormal codes alone."""
     x = Batch8([900, 650], new, 8, 2, d_h, seed=14)
@@ -177,7 +179,7 @@ def test_attend_every_code(d_h, new):
 
 
 @pytest.mark.parametrize("d_h", [64, 128])
-@pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
+@pytest.mark.parametrize("new", [[1, 1], [6, 5], [20, 18], [60, 200]])
 def test_attend_any_scales(d_h, new):
     """Pools that were filled by something else: scales that are no powers of two, zeros in whole blocks, and keys
     and values far from one in size."""
@@ -193,7 +195,7 @@ def test_attend_any_scales(d_h, new):
     run(x, scale=2.0 ** 30 * d_h ** -0.5)
 
 
-@pytest.mark.parametrize("new", [[1, 1], [6, 5], [60, 200]])
+@pytest.mark.parametrize("new", [[1, 1], [6, 5], [20, 18], [60, 200]])
 def test_attend_extreme_queries(new):
     """Rows of the smallest and of very large queries (equal weights, one entry's values), of zeros, and rows with
     an infinity or a NaN, which become NaN and leave the others alone."""
@@ -273,7 +275,7 @@ def test_attend_on_two_streams_and_in_two_graphs_at_once():
     assert all(torch.equal(a, b) for a, b in zip(want, out))
 
 
-@pytest.mark.parametrize("new", [[1, 1, 1], [1, 200, 70]])
+@pytest.mark.parametrize("new", [[1, 1, 1], [1, 40, 20], [1, 200, 70]])
 def test_attend_empty_wide_and_clamped(new):
     """Sequences without entries, a table far wider than they need, lengths beyond it and below zero."""
     x = Batch8([130, 300, 64], new, 8, 2, 64, seed=42, width=5000)
@@ -290,7 +292,7 @@ def test_attend_empty_wide_and_clamped(new):
     assert torch.equal(c.attend(q, qs, torch.full_like(kl, 2 ** 31 - 1)), c.attend(q, qs, top))
 
 
-@pytest.mark.parametrize("new", [[1, 1, 3], [200, 1, 64]])
+@pytest.mark.parametrize("new", [[1, 1, 3], [30, 1, 35], [200, 1, 64]])
 def test_attend_same_inputs_same_bits(new):
     x = Batch8([1500, 300, 2000], new, 32, 8, 128, seed=9)
     c, qs, kl = cache_of(x)
@@ -300,7 +302,7 @@ def test_attend_same_inputs_same_bits(new):
         assert torch.equal(first, c.attend(q, qs, kl))
 
 
-@pytest.mark.parametrize("new", [[1, 1, 3], [200, 1, 64]])
+@pytest.mark.parametrize("new", [[1, 1, 3], [30, 1, 35], [200, 1, 64]])
 def test_scratch_may_hold_anything(new):
     x = Batch8([1500, 300, 2000], new, 32, 8, 128, seed=9)
     c, qs, kl = cache_of(x)
@@ -321,7 +323,7 @@ def test_many_sequences():
     run(Batch8(lens, new, 4, 2, 64, seed=17))
 
 
-@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("new", [1, 20, 40])
 def test_blocks_past_32_bit_offsets(new):
     """Blocks whose entries lie more than 2^32 bytes into the pools."""
     x = Batch8([150], [new], 32, 8, 128, seed=40)
