@@ -165,6 +165,8 @@ _lock = threading.Lock()
 def load(path: str = LIB_PATH):
     """Load the CUDA library (raises if it is missing: no fallback)."""
     global _lib
+    if _lib is not None:  # (set once, complete)
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(path):

@@ -265,8 +265,8 @@ struct ItemWalk {
 // A block takes 32 dims of 32 rows in 2 slices of the parts (a thread: one row, 16 dims; most
 // items of chunks are shared by two), or, where no tile has more than 4 rows, 16 dims in 8
 // slices (a thread: 4 dims), so that a few parts' loads are all in flight at once; the slices are
-// added up in order.  (Eight rows, for tiles of as many over 8-bit pools: 16 dims in 4 slices.)  (One thread for all parts of a row: 12 us of the 59 of four decoding
-// sequences of 15.5 K entries.)
+// added up in order.  (Eight rows, for tiles of as many over 8-bit pools: 16 dims in 4 slices.  One thread for
+// all parts of a row: 12 us of the 59 of four decoding sequences of 15.5 K entries.)
 template <int DH, typename T, int RP>
 __device__ __forceinline__ void join_rows(const AttnPagedArgs& a, const SharedItem& m, const float* parts, int part_rows,
                                           float* tmp) {

@@ -42,9 +42,9 @@ def verify(target: torch.Tensor, drafted: torch.Tensor, start: torch.Tensor, u: 
 
     Returns int32 ``tokens`` [batch, width], the kept drafts and the drawn token, -1 behind,
     and ``count`` [batch], how many there are."""
-    device, vocab = target.device, target.shape[-1]
     if not target.is_cuda or target.dtype not in _TYPES or target.dim() != 2:
         raise ValueError("target must be [rows, vocab] float32 or bfloat16 on a CUDA device")
+    device, vocab = target.device, target.shape[1]
     if _current_device() != device.index:
         with torch.cuda.device(device.index):
             return verify(target, drafted, start, u, r, width=width, draft=draft)

@@ -89,7 +89,8 @@ class _Cache:
         if len(shape) != 3 or shape[1] != heads or shape[2] != self.d_h or x.dtype is not dtype or \
                 x.device != self.device or (shape[0] and (stride[2] != 1 or (heads > 1 and stride[1] != self.d_h))):
             raise ValueError(f"{name} must be [tokens, {heads}, {self.d_h}] {dtype} with whole rows")
-        _no_backward(name, x)
+        if x.requires_grad:
+            _no_backward(name, x)
         return stride[0] if shape[0] > 1 else heads * self.d_h
 
     def _work(self, tokens: int, stream: int) -> torch.Tensor:
@@ -139,7 +140,8 @@ class _Cache:
             if gain.dtype != self.dtype or gain.shape != (self.d_h,) or not gain.is_contiguous() or \
                     gain.device != self.device:
                 raise ValueError("gains must be [d_h] of the pools' type")
-            _no_backward("a gain", gain)
+            if gain.requires_grad:
+                _no_backward("a gain", gain)
         if rope is not None:
             if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1] != self.d_h // 2 or \
                     rope.shape[2] != 2 or not rope.is_contiguous() or rope.device != self.device:
@@ -152,11 +154,12 @@ class _Cache:
         elif out.shape != (tokens, self.n_q, self.d_h) or out.dtype != self.dtype or not out.is_contiguous() or \
                 out.device != self.device:
             raise ValueError("out must be a contiguous [tokens, n_q, d_h] of the pools' type")
-        p = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
         with self._lock:
             self._batch(q_start, kv_len)
-            self._kv_append(tokens, _TYPES[k.dtype], p(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, p(q_gain),
-                            p(k_gain), eps, p(rope), 0 if rope is None else rope.shape[0], p(out),
+            self._kv_append(tokens, _TYPES[k.dtype], 0 if q is None else q.data_ptr(), ld_q, k.data_ptr(), ld_k,
+                            v.data_ptr(), ld_v, 0 if q_gain is None else q_gain.data_ptr(),
+                            0 if k_gain is None else k_gain.data_ptr(), eps, 0 if rope is None else rope.data_ptr(),
+                            0 if rope is None else rope.shape[0], 0 if out is None else out.data_ptr(),
                             _raw_stream(self.index))
         return out
 

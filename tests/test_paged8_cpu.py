@@ -9,6 +9,7 @@ import torch
 import paged8_util
 from paged_util import PAGE
 from paper_2605_27255_gb300 import capi, drafts, paged
+from test_capi_cpu import struct_fields
 from test_paged_handle_cpu import host  # noqa: F401
 
 
@@ -108,7 +109,8 @@ def test_verify_checks_its_tensors(host8):
     assert tokens.shape == (2, 3) and count.shape == (2,)
     for k, v in (("target", torch.rand(4, 7)), ("target", torch.rand(5, 7).double()), ("target", torch.rand(7, 5).t()),
                  ("drafted", x["drafted"].long()), ("start", x["start"][:2]), ("u", torch.rand(2)),
-                 ("r", torch.rand(2).double()), ("u", torch.rand(6)[::2]), ("drafted", x["drafted"][None])):
+                 ("r", torch.rand(2).double()), ("u", torch.rand(6)[::2]), ("drafted", x["drafted"][None]),
+                 ("target", torch.tensor(1.0)), ("r", torch.tensor(0.5)), ("start", torch.tensor(0, dtype=torch.int32))):
         with pytest.raises(ValueError):
             drafts.verify(**{**x, k: v}, width=3)
     for draft in (torch.rand(2, 7), torch.rand(3, 6), torch.rand(3, 7).bfloat16(), torch.rand(3, 7).requires_grad_()):
@@ -192,7 +194,9 @@ def test_what_the_library_refuses_of_a_verification():
 
 
 def test_structures_match_the_header():
-    """Sizes as a C compiler lays them out (pointers after the 32-bit fields)."""
+    """Names in the header's order, sizes as a C compiler lays them out (pointers after the 32-bit fields)."""
+    for c in (capi.pipo_paged8, capi.pipo_page_tables):
+        assert [f for f, _ in c._fields_] == struct_fields(c.__name__)
     assert ctypes.sizeof(capi.pipo_paged8) == 32 + 7 * 8 and capi.pipo_paged8.k.offset == 32
     assert ctypes.sizeof(capi.pipo_page_tables) == 16 + 4 * 8 and capi.pipo_page_tables.table.offset == 16
 
