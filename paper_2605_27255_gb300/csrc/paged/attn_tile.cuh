@@ -259,7 +259,7 @@ __device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsign
 // long tail of 2^-17 each next to one large weight.)  Measured for 2048 tokens behind 14336 entries, 32
 // query and 8 kv heads of 128: 2559 us with row tiles of 32 on mma.sync, 692 with keys converted too (by two
 // warps; 592 by three), 541 with key codes as operands, 465 with the scales by shuffles in place of a
-// barrier, 449 with fixed addresses in the conversion; the bf16 pools take 375.  What is left: instruction
+// barrier, 445 with fixed addresses in the conversion; the bf16 pools take 375.  What is left: instruction
 // fetch, the scales' part of every page (20 us), key codes in two products' time (20).
 template <int DH, bool PAIR, bool SEL, bool E8 = false>
 __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs p, ItemShape shape, int S,
@@ -791,7 +791,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     const bool move = top > m_ref + kAtSlack;
                     // 8-bit pools: scores so large that what a fused multiply-add keeps of the maximum itself, up to half a step,
                     // is a power of two that matters are multiplied before the subtraction, which then leaves 0
-                    const bool large = E8 && !(fabsf(top) <= 4194304.f);  // (or masked altogether)
+                    const bool large = E8 && fabsf(top) > 4194304.f && top > -INFINITY;
                     if (__any_sync(0xffffffffu, move || large) || (E8 && v_now > v_ref)) {
                         if (E8 && __any_sync(0xffffffffu, large)) {
 #pragma unroll
