@@ -34,50 +34,10 @@ __device__ __forceinline__ void move_codes(uint8_t* block, int n, float f) {
     }
 }
 
-// A warp: token t's queries, normalised and rotated (gain: ones; d, hl: the lane's place in its head).  The text is
-// kv_append_kernel's: called from there too it makes that kernel 8 % slower (78 against 72.5 us for two
-// 8191-token prompts; the same registers, another schedule).
-template <int DH, typename TI>
-__device__ __forceinline__ void append_queries(const AppendArgs& p, long long t, float (&gain)[8], int d, int hl) {
-    using HL = HeadLane<DH>;
-    const PagedArgs& c = p.c;
-    if (t >= c.n_tokens) return;
-    load_gain<DH, bf16_t>(static_cast<const bf16_t*>(p.q_gain), gain);
-    const Tok k = find_token(c, (int)t);
-    if (k.b < 0) return;
-    const Angles an = load_angles<DH>(k.pos >= 0 ? p.rope : nullptr, k.pos);
-    const TI* src = static_cast<const TI*>(p.q) + (size_t)t * p.ld_q + d;
-    bf16_t* dst = static_cast<bf16_t*>(p.q_out) + (size_t)t * c.n_q * DH + d;
-    const float eps = k.pos >= 0 ? p.eps : 1.f;  // (a token without an entry: zeros, also where eps is 0)
-    constexpr int U = 4;  // heads in flight per lane
-    for (int h0 = 0; h0 < c.n_q; h0 += U * HL::H) {
-        float a[U][4], b[U][4];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * HL::H + hl;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[u][i] = b[u][i] = 0.f;
-            if (h < c.n_q && k.pos >= 0) {
-                load_f<TI, 4>(src + (size_t)h * DH, a[u]);
-                load_f<TI, 4>(src + (size_t)h * DH + DH / 2, b[u]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * HL::H + hl;
-            norm_turn<DH>(a[u], b[u], p.q_gain != nullptr, gain, eps, an);
-            if (h < c.n_q) {
-                store_f<bf16_t, 4>(dst + (size_t)h * DH, a[u]);
-                store_f<bf16_t, 4>(dst + (size_t)h * DH + DH / 2, b[u]);
-            }
-        }
-    }
-}
-
 // grid: CTAs of kAppendWarps tokens' queries each, then page_ctas = runs * n_kv * 2 of (page, kv head, keys or
 // values).  Keys and values apart, so that 64 registers hold a block's entries and four CTAs fit an SM: two
 // 8191-token prompts with 32 query and 8 kv heads of 128 in bf16 117 us with both in one CTA (128 registers, two
-// CTAs), 81 apart, 78 with the queries first (the other order ends in a tail of long CTAs).
+// CTAs), 81 apart, 78 with the queries first (the other order ends in a tail of long CTAs), 72.4 now.
 template <int DH, typename TI>
 __global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append8_kernel(AppendArgs p, int page_ctas) {
     using HL = HeadLane<DH>;
@@ -89,8 +49,41 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append8_kernel(Append
     pdl_wait();
     float gain[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     const int query_ctas = (int)gridDim.x - page_ctas, x0 = (int)blockIdx.x - query_ctas;
+    // Queries: a warp per token, the text of kv_append_kernel's (as a function that both call it compiles to a slower
+    // schedule in either: 78 against 72.5 us there, 77 against 72.4 here)
     if (x0 < 0) {
-        append_queries<DH, TI>(p, (long long)blockIdx.x * kAppendWarps + warp, gain, d, hl);
+        const long long t = (long long)blockIdx.x * kAppendWarps + warp;
+        if (t >= c.n_tokens) return;
+        load_gain<DH, bf16_t>(static_cast<const bf16_t*>(p.q_gain), gain);
+        const Tok k = find_token(c, (int)t);
+        if (k.b < 0) return;
+        const Angles an = load_angles<DH>(k.pos >= 0 ? p.rope : nullptr, k.pos);
+        const TI* src = static_cast<const TI*>(p.q) + (size_t)t * p.ld_q + d;
+        bf16_t* dst = static_cast<bf16_t*>(p.q_out) + (size_t)t * c.n_q * DH + d;
+        const float eps = k.pos >= 0 ? p.eps : 1.f;  // (a token without an entry: zeros, also where eps is 0)
+        constexpr int U = 4;  // heads in flight per lane
+        for (int h0 = 0; h0 < c.n_q; h0 += U * HL::H) {
+            float a[U][4], b[U][4];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * HL::H + hl;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[u][i] = b[u][i] = 0.f;
+                if (h < c.n_q && k.pos >= 0) {
+                    load_f<TI, 4>(src + (size_t)h * DH, a[u]);
+                    load_f<TI, 4>(src + (size_t)h * DH + DH / 2, b[u]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * HL::H + hl;
+                norm_turn<DH>(a[u], b[u], p.q_gain != nullptr, gain, eps, an);
+                if (h < c.n_q) {
+                    store_f<bf16_t, 4>(dst + (size_t)h * DH, a[u]);
+                    store_f<bf16_t, 4>(dst + (size_t)h * DH + DH / 2, b[u]);
+                }
+            }
+        }
         return;
     }
     const bool keys = (x0 & 1) == 0;
