@@ -12,7 +12,8 @@
 // A cluster of CTAs per sequence.  Each finds the row by itself (a warp looks at 32 drafts at a time),
 // sums its slice of the vocabulary warp by warp, and learns the others' sums through
 // distributed shared memory; the one that holds the drawn place goes through the right
-// warp's slice once more.  Bound by the row's read (and the draft row's) and, for few sequences, by
+// warp's slice once more.  Another CTA's shared memory may be written only once that CTA has started: every
+// CTA arrives at the cluster's barrier when it starts and waits there, under the sums, before its first such write.  Bound by the row's read (and the draft row's) and, for few sequences, by
 // the chain of start, drafted token, probabilities, row.  Measured back to back with a vocabulary of 151936 in
 // fp32: 64 sequences 14.7 us (52 MB read), one 8.8 us.  Four loads of either row in flight take 50
 // registers, so that 512 CTAs need two rounds (16.8 and 8.0 us); CTAs of 256 threads 17.3 and 12.4.
@@ -82,6 +83,7 @@ __global__ void __launch_bounds__(kVerThreads) __cluster_dims__(kVerCluster, 1, 
     cg::cluster_group cluster = cg::this_cluster();
     const int b = (int)(blockIdx.x / kVerCluster), rank = (int)cluster.block_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // this CTA has started
     pdl_launch();
     pdl_wait();
     const int s0 = min(max(a.start[b], 0), a.n_drafted), s1 = min(max(a.start[b + 1], s0), a.n_drafted);
@@ -153,6 +155,7 @@ __global__ void __launch_bounds__(kVerThreads) __cluster_dims__(kVerCluster, 1, 
         for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
         if (lane == 0) warp_sum[warp] = mine;
         __syncthreads();
+        if (pass == 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // all have
         if (threadIdx.x < kVerCluster) {
             unsigned long long all = 0;
 #pragma unroll
