@@ -75,6 +75,15 @@ __device__ __forceinline__ unsigned long long ver_sum(int hi, int lo) {
 // a warp's slice has at most 2^19 / 128 tokens, a lane 128 of them: 32 bits hold the sums of either part
 static_assert((kVerMaxVocab / (kVerCluster * kVerWarps * 32) + 8LL) * (1 << 22) < (1LL << 31), "a lane's sums");
 
+// floor(r W), 0 <= r < 1: r is m 2^-s with a whole m below 2^24 (s >= 24), m W has 87 bits at most.  (As a product of
+// doubles it can end on the next whole number: rows of many ones have a W past 2^53.)
+__device__ __forceinline__ unsigned long long ver_place(float r, unsigned long long W) {
+    const uint32_t u = __float_as_uint(r), e = max(u >> 23, 1u), m = (u & 0x7fffffu) | (u >> 23 ? 0x800000u : 0u);
+    const int s = 150 - (int)e;
+    const unsigned long long lo = m * W, hi = __umul64hi(m, W);
+    return s < 64 ? lo >> s | hi << (64 - s) : s < 128 ? hi >> (s - 64) : 0ull;
+}
+
 template <typename T, int N>
 __global__ void __launch_bounds__(kVerThreads) __cluster_dims__(kVerCluster, 1, 1) verify_kernel(VerifyArgs a) {
     namespace cg = cooperative_groups;
@@ -174,8 +183,7 @@ __global__ void __launch_bounds__(kVerThreads) __cluster_dims__(kVerCluster, 1, 
             if (rank == 0 && threadIdx.x == 0) out[kept] = a.vocab - 1;
             return;
         }
-        const float r = fminf(fmaxf(a.r[b], 0.f), 0.99999994f);
-        const unsigned long long goal = (unsigned long long)((double)r * (double)total);
+        const unsigned long long goal = ver_place(fminf(fmaxf(a.r[b], 0.f), 0.99999994f), total);
         if (goal < before) return;
         for (int w = 0; w < warp; ++w) before += warp_sum[w];
         if (goal < before || goal >= before + warp_sum[warp]) return;

@@ -48,3 +48,30 @@ def test_short_rows_without_weight(vocab):
         count = count.cpu()
         assert torch.equal(count, torch.where(odd, 2, 1).to(torch.int32))
         assert torch.equal(tokens.cpu()[torch.arange(n), count - 1], want)
+
+
+def place(r: float, weights) -> int:
+    """The first token whose running weight exceeds floor(r W), in whole numbers (r = m / 2^s exactly)."""
+    m, d = r.as_integer_ratio()
+    goal, total = m * sum(weights) // d, 0
+    for v, w in enumerate(weights):
+        total += w
+        if total > goal:
+            return v
+
+
+@pytest.mark.parametrize("n", [1025, 2049, 65537, 1 << 19])
+@pytest.mark.parametrize("r", [0.5, 0.25, 1 - 2.0 ** -24, 0.75 + 2.0 ** -24, 2.0 ** -9, 2.0 ** -30, 2.0 ** -140, 0.0])
+def test_places_that_53_bits_do_not_hold(n, r):
+    """Rows of ones (they need not add up to one): W = n 2^44 - 1 in units of 2^-44, so that r W ends just below whole
+    tokens, and a product rounded to 53 bits on them."""
+    row = torch.ones(1, n)
+    row[0, n - 2] = 1 - 2.0 ** -24  # 2^20 units less
+    row[0, n - 1] = (2 ** 20 - 1) * 2.0 ** -44  # 2^20 - 1 more
+    one = 1 << 44
+    weights = [one] * (n - 2) + [one - (1 << 20), (1 << 20) - 1]
+    assert sum(weights) == (n - 1) * one - 1
+    none_i, none_f = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, device="cuda")
+    tokens, _ = drafts.verify(row.cuda(), none_i, torch.zeros(2, dtype=torch.int32, device="cuda"), none_f,
+                              torch.tensor([r], device="cuda"), width=1)
+    assert tokens.item() == place(r, weights)
