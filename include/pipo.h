@@ -525,9 +525,12 @@ typedef struct {
  * the power of two that leaves the largest finite magnitude of its new entries in [32, 64).
  * Later entries keep a scale while they fit 448 times it; else it is chosen from
  * them in the same way, and the codes held before move by the ratio (exactly, but for those
- * that become subnormal).  So a block's codes depend on how its entries were cut
- * into calls by at most a power of two and the subnormals' rounding.  Infinities saturate,
- * NaN is stored as NaN.  Blocks that two sequences share must not receive entries. */
+ * that become subnormal, where the scale before was a power of two too; else they are rounded
+ * once more).  A scale never falls while its block is held: one above 2^7, of a pool that something else has
+ * filled, stays, and entries beyond 448 times it saturate.  So the codes of entries depend on how they
+ * were cut into calls, and on entries that came after them (also those of drafts that were given up
+ * since: the scale they raised stays up), by at most a power of two and the subnormals' rounding.
+ * Infinities saturate, NaN is stored as NaN.  Blocks that two sequences share must not receive entries. */
 PIPO_API pipo_status pipo_op_kv_append8(const pipo_paged8 *c, int32_t n_tokens, int32_t in_dtype, const void *d_q,
                                         int64_t ld_q, const void *d_k, int64_t ld_k, const void *d_v, int64_t ld_v,
                                         const void *d_q_gain, const void *d_k_gain, float eps, const float *d_rope,

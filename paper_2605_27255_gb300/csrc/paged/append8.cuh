@@ -5,7 +5,8 @@
 // scale, and they are rounded once.  A block's first entry (slot 0 among the new ones)
 // starts a new scale.  Later entries keep it while they fit (up to 448 times the scale);
 // else it is chosen anew from them, and the codes that the block holds move by the
-// ratio, a power of two.
+// ratio, a power of two.  It never falls: where the chosen one, capped at 2^7, would be below that of a pool
+// which something else has filled, that one stays, new entries beyond it saturate, and no held code is touched.
 //
 // Bound by HBM: every new value is read once and written once.
 #pragma once
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 4) kv_append8_kernel(Append
 #pragma unroll
     for (int w = 0; w < kAppendWarps; ++w) m = fmaxf(m, most[w]);
     const int slot0 = j0 - page * kPage;  // entries held before
-    const float now = slot0 == 0 || m > kCodeMax * old ? scale_of(m) : old, f = 1.f / now;
+    const float now = slot0 == 0 ? scale_of(m) : m > kCodeMax * old ? fmaxf(scale_of(m), old) : old, f = 1.f / now;
     uint8_t* dst = static_cast<uint8_t*>(keys ? c.k : c.v) + head * kPage * DH;
     if (slot0 > 0 && now != old) move_codes<DH>(dst, slot0, old / now);
     if (threadIdx.x == 0) *scale = now;  // (every thread has read the old one before the barrier)
