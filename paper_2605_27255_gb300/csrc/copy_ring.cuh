@@ -10,8 +10,10 @@
 
 #ifdef __CUDACC__
 #define PIPO_RING_FN __device__ __forceinline__
+#define PIPO_RING_RULE __host__ __device__ constexpr
 #else
 #define PIPO_RING_FN inline
+#define PIPO_RING_RULE constexpr
 #endif
 
 namespace pipo {
@@ -56,5 +58,15 @@ PIPO_RING_FN void pair_drain(int n, bool leader, Full full, Empty empty) {
     bool ok = true;
     ring_drain<ST>(n, [&](int st, uint32_t ph, int i) { ok = ok && empty(st, ph, i); });
 }
+
+// Consumers that take the pages of a ring in turn, page i the consumer i % W, and wait for their own alone: a barrier's
+// parity tells its present phase from the one before, so a wait that comes while the fill BEFORE the wanted one is still
+// under way passes at once.  (Copies may arrive in any order, and a page without a copy arrives at once.)  The
+// fill before is known to be over where the same consumer took it: stages must be a multiple of consumers.
+PIPO_RING_RULE bool ring_turns_ok(int stages, int consumers) { return stages % consumers == 0; }
+// Producers that fill the slots of a ring in turn, each after a wait for its own slot to be free, where slots are freed in
+// order: a producer's page before, W back, was free to be filled, so that all pages up to W + S back have left
+// their slots; that must reach the one that was two laps ago in this page's slot.
+PIPO_RING_RULE bool ring_fillers_ok(int slots, int producers) { return producers <= slots; }
 
 }  // namespace pipo

@@ -82,7 +82,7 @@ __host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
 // (single: per pipeline)
 __host__ __device__ constexpr int at8_k_pages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 3 : 6); }
 __host__ __device__ constexpr int at8_v_pages(int dh, bool pair) { return pair ? (dh == 128 ? 4 : 6) : (dh == 128 ? 2 : 4); }
-__host__ __device__ constexpr int at8_raw_pages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr int at8_raw_pages(int dh, bool pair) { return pair ? (dh == 128 ? 6 : 9) : (dh == 128 ? 2 : 4); }
 __host__ __device__ constexpr int at8_convert(bool pair) { return pair ? 3 : 1; }  // converting warps of a ring
 __host__ __device__ constexpr int at8_codes(int dh) { return kPage * dh; }
 __host__ __device__ constexpr int at8_ring_bytes(int dh, bool pair) {
@@ -574,10 +574,11 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 }
             }
         } else if (E8) {
-            // ---- value codes to operands: the converting warps take the pages in turn
+            // ---- value codes to operands: the converting warps take the pages in turn, each from stages of its own
             ItemWalk it;
             const int rg = PAIR ? 0 : (warp - 12) >> 1, me = PAIR ? (warp == 2 ? 2 : (warp - 12) >> 1) : 0;
             constexpr int W = at8_convert(PAIR);
+            static_assert(ring_turns_ok(SR, W) && ring_fillers_ok(SV, W), "parities of the rings that the converting warps share");
             it.start(c, shape, pieces[rg]);
             unsigned char *v_s = ring_s + rg * at8_ring_bytes(DH, PAIR), *raw_s = v_s + SV * kPg + SK * kCodes;
             int n = 0;  // pages before the present item
