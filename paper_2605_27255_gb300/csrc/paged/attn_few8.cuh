@@ -10,8 +10,8 @@
 //                   at a time;
 //   O^T += C_v^T P^T  16 dims x 8 rows; a lane reads 16 dims of four entries and pairs the
 //                   entries' bytes.  P^T comes from S^T's registers by movmatrix.
-// The queries are scaled by a power of two per row to fp16 (bf16's digits fit; what is below
-// 2^-24 of a row's largest is lost), scores get it back with the block's scale in fp32.  The values'
+// The queries are scaled by a power of two per row to fp16, the largest below 2^15 (bf16's digits fit down to 2^-31 of
+// it, what is below 2^-39 is lost), scores get it back with the block's scale in fp32.  The values'
 // scales go into the weights, relative to the largest one so far: weights stay below
 // 2^8 and keep fp16's 11 digits (2^-25 below 2^-14).
 //
@@ -211,7 +211,8 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
                 }
             most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
             most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            const float sc = query_scale(most), f = 1.f / sc;
+            const int ex = query_exponent(most);
+            const float sc = exp2_int(ex), f = exp2_int(-ex);
             scale_of_row[0] = __shfl_sync(0xffffffffu, sc, 8 * tig);
             scale_of_row[1] = __shfl_sync(0xffffffffu, sc, 8 * tig + 4);
 #pragma unroll
@@ -237,8 +238,9 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, finite_abs(x[i]));
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-                const float sc = query_scale(most), f = 1.f / sc;
-                if (lane == 0) row_scale[r] = sc;
+                const int ex = query_exponent(most);
+                const float f = exp2_int(-ex);
+                if (lane == 0) row_scale[r] = exp2_int(ex);
                 if (lane < DH / 4) {  // dims 4 lane ..: chunk lane / 4, word lane % 4 of it
                     const int step = (lane >> 4) * 4 + (lane & 3), quad = (lane >> 2) & 3;
                     q_s[((r >> 3) * KS + step) * 32 + (r & 7) * 4 + quad] = make_uint2(half2_of(x[0] * f, x[1] * f), half2_of(x[2] * f, x[3] * f));

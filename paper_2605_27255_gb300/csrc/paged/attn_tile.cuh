@@ -80,16 +80,17 @@ __host__ __device__ constexpr size_t at_smem(int dh, bool pair) {
 
 // 8-bit pools: pages of key codes, of value operands and of value codes on their way to those, in a ring each
 // (single: per pipeline)
-__host__ __device__ constexpr int at8_k_pages(int dh, bool pair) { return pair ? (dh == 128 ? 5 : 8) : (dh == 128 ? 3 : 6); }
-__host__ __device__ constexpr int at8_v_pages(int dh, bool pair) { return pair ? (dh == 128 ? 4 : 6) : (dh == 128 ? 2 : 4); }
-__host__ __device__ constexpr int at8_raw_pages(int dh, bool pair) { return pair ? (dh == 128 ? 6 : 9) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr int at8_k_pages(int dh, bool pair) { return pair ? (dh == 128 ? 7 : 8) : (dh == 128 ? 2 : 6); }
+__host__ __device__ constexpr int at8_v_pages(int dh, bool pair) { return pair ? (dh == 128 ? 3 : 6) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr int at8_raw_pages(int dh, bool pair) { return pair ? (dh == 128 ? 3 : 9) : (dh == 128 ? 2 : 4); }
+__host__ __device__ constexpr int at8_q_bytes(int dh) { return 3 * 128 * dh; }  // three parts of a query tile
 __host__ __device__ constexpr int at8_convert(bool pair) { return pair ? 3 : 1; }  // converting warps of a ring
 __host__ __device__ constexpr int at8_codes(int dh) { return kPage * dh; }
 __host__ __device__ constexpr int at8_ring_bytes(int dh, bool pair) {
     return at_page_bytes(dh) * at8_v_pages(dh, pair) + at8_codes(dh) * (at8_k_pages(dh, pair) + at8_raw_pages(dh, pair));
 }
 __host__ __device__ constexpr size_t at8_smem(int dh, bool pair) {
-    return 1024 + 2 * (size_t)at_q_bytes(dh) + (size_t)at8_ring_bytes(dh, pair) * (pair ? 1 : 2);
+    return 1024 + 2 * (size_t)at8_q_bytes(dh) + (size_t)at8_ring_bytes(dh, pair) * (pair ? 1 : 2);
 }
 
 // B operand [entries][dims] of a page (MN-major, 128-byte swizzle): 64-dim blocks kPageHalf apart,
@@ -248,9 +249,11 @@ __device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsign
 
 // SEL: whole tiles over selected pages (AttnPagedArgs::bits), PAIR only.
 // E8: pools of e4m3 codes.  Key codes are operands as they are (kind::f8f6f4): queries are scaled
-// by a power of two per row to below 256 and meet them as two e4m3 parts, which hold all digits of
-// a bf16 number down to 2^-10 of the row's largest (below that 2^-18 of the largest are lost).  The two
-// parts cost what one bf16 operand does.  The row's and the block's scale meet the
+// by a power of two per row to below 2^15 and meet them as three e5m2 parts of three digits each (the
+// rest of the one before, so that its sign is a digit too): all digits of a bf16 number down to 2^-24 of the row's
+// largest, and what is below 2^-31 of that is lost.  (Two e4m3 parts cost a third less and hold 2^-10 and 2^-18: a row
+// whose other dims lie 2^10 below one that the keys do not have is then off by more than the output's
+// rounding.)  The row's and the block's scale meet the
 // scores in fp32.  Value codes become fp16 tiles (a code is an fp16 number) by warps 2, 12 and 14 (single: 12 and
 // 14, one per pipeline); their
 // scales go into the weights, relative to the largest so far (2^-24 at least: what that
@@ -259,14 +262,16 @@ __device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsign
 // long tail of 2^-17 each next to one large weight.)  Measured for 2048 tokens behind 14336 entries, 32
 // query and 8 kv heads of 128: 2559 us with row tiles of 32 on mma.sync, 692 with keys converted too (by two
 // warps; 592 by three), 541 with key codes as operands, 465 with the scales by shuffles in place of a
-// barrier, 445 with fixed addresses in the conversion; the bf16 pools take 375.  What is left: instruction
-// fetch, the scales' part of every page (20 us), key codes in two products' time (20).
+// barrier, 445 with fixed addresses in the conversion, 475 with the queries' third part (492 with rings of 5, 4 and 3
+// pages of keys, values and value codes in the shared memory it leaves, 484 with 4, 3 and 6; 7, 3 and 3 are taken); the
+// bf16 pools take 375.  What is left: instruction fetch, the scales' part of every page (20 us), the key products (three
+// parts take half as long again as the bf16 kernel's).
 template <int DH, bool PAIR, bool SEL, bool E8 = false>
 __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs p, ItemShape shape, int S,
                                                                   int part_rows, size_t part_off,
                                                                   const __grid_constant__ CUtensorMap tmK,
                                                                   const __grid_constant__ CUtensorMap tmV) {
-    constexpr int kTile = at_q_bytes(DH), kPg = at_page_bytes(DH), NR = PAIR ? 1 : 2;  // NR: pairs of rings
+    constexpr int kTile = E8 ? at8_q_bytes(DH) : at_q_bytes(DH), kPg = at_page_bytes(DH), NR = PAIR ? 1 : 2;  // NR: pairs of rings
     constexpr int PARTS = PAIR || E8 ? 1 : 2;  // parts of the weights
     constexpr int SK = E8 ? at8_k_pages(DH, PAIR) : at_k_pages(DH, PAIR), SV = E8 ? at8_v_pages(DH, PAIR) : at_v_pages(DH, PAIR);
     constexpr int SR = at8_raw_pages(DH, PAIR), kCodes = at8_codes(DH);
@@ -280,7 +285,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
     // 8-bit pools: ring of value codes, the queries' row scales
     __shared__ __align__(8) uint64_t raw_full[E8 ? NR : 1][E8 ? SR : 1], raw_empty[E8 ? NR : 1][E8 ? SR : 1];
     __shared__ bool raw_live[E8 ? NR : 1][E8 ? SR : 1];
-    __shared__ float row_scale[E8 ? 2 : 1][E8 ? 2 : 1][E8 ? 128 : 1];  // [item's parity][pipeline][row]
+    __shared__ int8_t row_scale[E8 ? 2 : 1][E8 ? 2 : 1][E8 ? 128 : 1];  // [item's parity][pipeline][row], exponents of two
 
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* q_s = sm;              // two query tiles
@@ -484,7 +489,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         continue;
                     }
                     if (!values) {
-                        constexpr uint32_t id_s = E8 ? umma_idesc_e4m3(128, kPage) : umma_idesc_bf16(128, kPage);
+                        constexpr uint32_t id_s = E8 ? umma_idesc_e5m2_e4m3(128, kPage) : umma_idesc_bf16(128, kPage);
                         // descriptors count in 16 bytes: a step along a tile is an addition
                         constexpr int kPgK = E8 ? kCodes : kPg;
                         const uint32_t q_at = smem_u32(q_s) + chain * kTile, k_at = smem_u32(k_s);
@@ -500,9 +505,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             if (elect_one()) {
                                 uint32_t qb = (uint32_t)dq, kb = (uint32_t)dk + (uint32_t)((st * kPgK) >> 4);
                                 asm volatile("" : "+r"(qb), "+r"(kb));  // eight sums now, not sixteen kept over the loop
-                                if constexpr (E8) {  // 32 dims a step; the queries' second part lies behind the first
+                                if constexpr (E8) {  // 32 dims a step; the queries' parts lie one behind the other
 #pragma unroll
-                                    for (int i = 0; i < 2 * DH / 32; ++i)
+                                    for (int i = 0; i < 3 * DH / 32; ++i)
                                         umma_f8(s_at + buf * 64,
                                                 u32x2(qb + ((i / (DH / 32) * 128 * DH + i % (DH / 32) * 32) >> 4), (uint32_t)(dq >> 32)),
                                                 u32x2(kb + ((i % (DH / 32) * 32) >> 4), (uint32_t)(dk >> 32)), id_s, i > 0 ? 1u : 0u);
@@ -633,7 +638,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                                 : make_uint4(0u, 0u, 0u, 0u);
             };
             if constexpr (E8) {
-                // two e4m3 parts, a power of two per row (the C lanes of a row are neighbours), eight rows at a time
+                // three e5m2 parts, a power of two per row (the C lanes of a row are neighbours), eight rows at a time
 #pragma unroll 1
                 for (int i0 = 0; i0 < NI; i0 += 8) {
                     uint4 x[8];
@@ -651,26 +656,30 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         }
 #pragma unroll
                         for (int o = C / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-                        // the largest magnitude ends in [128, 256), that of tiny rows below; an infinity makes the row
-                        // NaN, as its scores would be
+                        // (an infinity makes the row NaN, as its scores would be)
                         const bool inf = most > 3.402823466e38f;
-                        const float sc = inf ? 1.f : fmaxf(query_scale(most), 3.0092655e-36f), f = inf ? NAN : 128.f / sc;
+                        const int e = inf ? 0 : query_exponent(most);
+                        const float f = inf ? NAN : exp2_int(-e);
                         const int v = v0 + (i0 + i) * RS;
-                        if (ch == 0) row_scale[begun & 1][w][v] = sc * (1.f / 128.f);
-                        uint32_t a[2], b[2];
-#pragma unroll
-                        for (int k = 0; k < 8; k += 4) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[k + e] *= f;
-                            a[k / 4] = encode4(y[k], y[k + 1], y[k + 2], y[k + 3]);
-                            const uint32_t lo = decode_lo(a[k / 4]), hi = decode_hi(a[k / 4]);
-                            const float2 l2 = __half22float2(*reinterpret_cast<const __half2*>(&lo));
-                            const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                            b[k / 4] = encode4(y[k] - l2.x, y[k + 1] - l2.y, y[k + 2] - h2.x, y[k + 3] - h2.y);
-                        }
+                        if (ch == 0) row_scale[begun & 1][w][v] = (int8_t)e;
                         unsigned char* d = q_s + w * kTile + v * DH + (((ch >> 1) ^ (DH == 128 ? v & 7 : v >> 1 & 3)) << 4) + (ch & 1) * 8;
-                        *reinterpret_cast<uint2*>(d) = make_uint2(a[0], a[1]);
-                        *reinterpret_cast<uint2*>(d + 128 * DH) = make_uint2(b[0], b[1]);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) y[k] *= f;
+#pragma unroll
+                        for (int part = 0; part < 3; ++part) {
+                            uint32_t a[2];
+#pragma unroll
+                            for (int k = 0; k < 8; k += 4) {
+                                a[k / 4] = encode4_e5m2(y[k], y[k + 1], y[k + 2], y[k + 3]);
+                                if (part == 2) continue;
+                                const float2 lo = decode2_e5m2((uint16_t)a[k / 4]), hi = decode2_e5m2((uint16_t)(a[k / 4] >> 16));
+                                y[k] -= lo.x;
+                                y[k + 1] -= lo.y;
+                                y[k + 2] -= hi.x;
+                                y[k + 3] -= hi.y;
+                            }
+                            *reinterpret_cast<uint2*>(d + part * 128 * DH) = make_uint2(a[0], a[1]);
+                        }
                     }
                 }
                 ++begun;
@@ -718,7 +727,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             if (E8) {
                 ok = wait(q_full + w, (uint32_t)((begun - 1) & 1), 60, begun);
                 if (!ok) break;
-                c_row = c2 * row_scale[(begun - 1) & 1][w][r];
+                c_row = c2 * exp2_int(row_scale[(begun - 1) & 1][w][r]);
             }
             // 8-bit pools: lane l holds the scales of page l of 32, those of the next 32 are on their way: blocks first,
             // scales eight pages later, so that no page waits for them

@@ -50,10 +50,27 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The power of two that queries of largest magnitude `most` are divided by on their way to fp16: they end below
-// 2 and above 2^-126 of themselves (1 for zeros)
-__device__ __forceinline__ float query_scale(float most) {
-    return most > 0.f ? __uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)) : 1.f;
+// four values as e5m2, the first one in the low byte, and two of them back
+__device__ __forceinline__ uint32_t encode4_e5m2(float a, float b, float c, float d) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (uint32_t)hi << 16 | lo;
+}
+__device__ __forceinline__ float2 decode2_e5m2(uint16_t x) {
+    uint32_t y;
+    asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(y) : "h"(x));
+    return __half22float2(*reinterpret_cast<const __half2*>(&y));
+}
+
+// 2^e, -126 <= e <= 127
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// The exponent of the power of two that queries of largest magnitude `most` are divided by on their way to formats with
+// 5 exponent bits: the largest ends in [2^14, 2^15), a row of tiny ones (below 2^-112) lower, but no further than that
+// a bf16 number's last digit, 2^-133, is still 2^-7 (0 for zeros)
+__device__ __forceinline__ int query_exponent(float most) {
+    return most > 0.f ? max((int)(__float_as_uint(most) >> 23) - 127, -112) - 14 : 0;
 }
 
 }  // namespace pipo

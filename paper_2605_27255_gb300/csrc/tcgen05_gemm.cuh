@@ -80,11 +80,11 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16(int M, int N) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// The same with A and B fp16, and of kind::f8f6f4 with A and B e4m3 (both formats have number 0).
+// The same with A and B fp16, and of kind::f8f6f4 with A e5m2 (number 1) and B e4m3 (0).
 __host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) {
     return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
-__host__ __device__ constexpr uint32_t umma_idesc_e4m3(int M, int N) { return umma_idesc_f16(M, N); }
+__host__ __device__ constexpr uint32_t umma_idesc_e5m2_e4m3(int M, int N) { return umma_idesc_f16(M, N) | (1u << 7); }
 
 __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
     asm volatile(
