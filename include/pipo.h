@@ -538,7 +538,9 @@ PIPO_API pipo_status pipo_op_kv_append8(const pipo_paged8 *c, int32_t n_tokens, 
 
 /* Causal attention over an 8-bit cache, as pipo_op_attn_paged, with scratch of
  * pipo_op_attn_paged8_scratch(c, n_tokens) bytes.  Scores, softmax and sums are fp32;
- * the softmax weights meet the values in fp16 (an error of an eighth of the output's own rounding).  Queries keep all
+ * the softmax weights meet the values in fp16 (an error of an eighth of the output's own rounding; a weight times its
+ * block's scale that is 2^-32 of the row's largest or less may be lost).  Blocks that a row does not see do not
+ * touch it, whatever their scales are.  Queries keep all
  * their digits down to 2^-24 of their row's largest; what is below 2^-31 of that may be lost.
  * Which kernel runs goes by the batch's average of rows per sequence, so the low bits of a sequence's
  * outputs depend on what shares its batch; the same call gives the same bits. */

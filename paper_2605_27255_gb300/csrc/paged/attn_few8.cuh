@@ -12,8 +12,7 @@
 //                   entries' bytes.  P^T comes from S^T's registers by movmatrix.
 // The queries are scaled by a power of two per row to fp16, the largest below 2^15 (bf16's digits fit down to 2^-31 of
 // it, what is below 2^-39 is lost), scores get it back with the block's scale in fp32.  The values'
-// scales go into the weights, relative to the largest one so far: weights stay below
-// 2^8 and keep fp16's 11 digits (2^-25 below 2^-14).
+// scales go into the weights (codes.cuh), which keep fp16's 11 digits.
 //
 // A warp takes 16 (or 32) entries of a 128-entry unit, with its own ring of copies, running maximum
 // and output; warps meet only at the end of an item, where their outputs are joined in
@@ -33,8 +32,6 @@
 #include "work.cuh"
 
 namespace pipo {
-
-constexpr float kFewSlack = 8.f;  // exponents above the reference before it moves
 
 // Entries of a warp's step: 16 fill an MMA's rows, 32 share a step's other work (eight sequences of 15.5 K
 // entries 49.1 -> 47.7 us); with more than one column tile their scores would not fit the registers.
@@ -74,12 +71,7 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, uint32_t n) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
 }
-__device__ __forceinline__ float few_ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
+__device__ __forceinline__ bool few_large(float m) { return fabsf(m) > kLargeScore && m > kNoScore; }
 // byte offsets of 16-byte chunk c of entry r (0 .. 15) in a stage's keys or values: swizzled so that the
 // lanes' reads hit different banks (keys: lanes take neighbouring entries; values: every other one)
 template <int DH>
@@ -249,7 +241,7 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
             __syncthreads();
         }
         // ---- this lane's rows: 2 tig and 2 tig + 1 of every column tile
-        float cs[NT][2], m[NT][2], l[NT][2], o[NT][MT][4];
+        float cs[NT][2], m[NT][2], l[NT][2], v_ref[NT][2], o[NT][MT][4];  // (references m + v_ref: codes.cuh)
         int pos[NT][2], lo[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -259,7 +251,8 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
                 cs[t][h] = c2 * (NT == 1 ? scale_of_row[h] : row_scale[NT > 1 ? t * 8 + 2 * tig + h : 0]);
                 pos[t][h] = it.len - it.n + i0 + r / c.G;
                 lo[t][h] = p.window > 0 ? pos[t][h] - p.window + 1 : 0;
-                m[t][h] = -INFINITY;
+                m[t][h] = kNoScore;
+                v_ref[t][h] = 0.f;
                 l[t][h] = 0.f;
             }
 #pragma unroll
@@ -271,14 +264,15 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
         // entries that every row sees: all before `free_to`, from `free_from` on
         const int free_to = it.len - it.n + i0 + 1;
         const int free_from = p.window > 0 ? it.len - it.n + i0 + it.tokens(shape) - p.window : 0;
-        float v_ref = 0.f, v_inv = 0.f;  // the largest value scale so far
+        bool large = false;      // (the same for the warp) large scores among its rows' references
+        float v_top = kNoScale;  // the largest scale so far
         for (int u = it.kv0; u < it.kv1; ++u) {
             cp_async_wait<ST - 2>();
             __syncwarp();
             issue();
             const unsigned char* ks_s = mine_s + slot * SB;
             const unsigned char* vs_s = ks_s + VS;
-            const float k_scale = scales[warp][slot][0], v_scale = scales[warp][slot][1];
+            const float k_scale = scales[warp][slot][0], v_now = log2_scale(scales[warp][slot][1]);
             slot = slot + 1 == ST ? 0 : slot + 1;
             const int e0 = (it.t0 + u) * kTileEnt + warp * EW;
             // (the sums of the two halves of the dims apart where registers allow: shorter chains)
@@ -317,66 +311,101 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
                         }
                     }
             // ---- softmax: s[.][t][0], s[.][t][1] are entry grp's scores for the lane's two rows, [2], [3] entry
-            // grp + 8's.  The reference of the exponents moves when a score has passed it by 2^8 (as in the tile
-            // kernel); only then the warp agrees on its maxima.
+            // grp + 8's, in the raw (times f).  The references of the exponents move when a score (with its scale) has passed
+            // one by 2^8 (as in the tile kernel); only then the warp agrees on its maxima.
             const bool edge = e0 + EW > free_to || e0 < free_from;
-            bool move = v_scale > v_ref;
+            const float v_up = v_now + kWeightUp;
+            const bool far = v_now < v_top - kFarScale;  // (the same for the warp)
+            bool move = large || far;
+            float down = code_ex2(-v_up);  // from weights to the sum's
+            v_top = fmaxf(v_top, v_now);
+            float top[NT][2], f[NT][2], neg[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float f = cs[t][h] * k_scale;
+                    f[t][h] = fmaxf(cs[t][h] * k_scale, 1.17549435e-38f);  // (never 0: masked scores are -infinity)
+                    neg[t][h] = v_up - (m[t][h] + v_ref[t][h]);
+                    top[t][h] = -INFINITY;
 #pragma unroll
                     for (int x = 0; x < ET; ++x) {
 #pragma unroll
-                        for (int e = h; e < 4; e += 2)
-                            s[x][t][e] = (CH == 2 ? s2[0][x][t][e] + s2[CH - 1][x][t][e] : s2[0][x][t][e]) * f;
+                        for (int e = h; e < 4; e += 2) s[x][t][e] = CH == 2 ? s2[0][x][t][e] + s2[CH - 1][x][t][e] : s2[0][x][t][e];
                         if (edge) {
                             const int a = e0 + 16 * x + grp;
                             if (a > pos[t][h] || a < lo[t][h]) s[x][t][h] = -INFINITY;
                             if (a + 8 > pos[t][h] || a + 8 < lo[t][h]) s[x][t][2 + h] = -INFINITY;
                         }
-                        move |= fmaxf(s[x][t][h], s[x][t][2 + h]) > m[t][h] + kFewSlack;
+                        top[t][h] = fmaxf(top[t][h], fmaxf(s[x][t][h], s[x][t][2 + h]));
                     }
+                    top[t][h] *= f[t][h];
+                    move |= top[t][h] + neg[t][h] > kWeightTop;
                 }
             if (__any_sync(0xffffffffu, move)) {
-                const float v_new = fmaxf(v_ref, v_scale), fv = v_ref > 0.f ? v_ref / v_new : 0.f;
+                bool big = false;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float now = m[t][h];
 #pragma unroll
-                        for (int x = 0; x < ET; ++x) now = fmaxf(now, fmaxf(s[x][t][h], s[x][t][2 + h]));
+                        for (int w = 4; w < 32; w <<= 1) top[t][h] = fmaxf(top[t][h], __shfl_xor_sync(0xffffffffu, top[t][h], w));
+                        const float by = (m[t][h] - top[t][h]) + (v_ref[t][h] - v_now);
+                        if (by < 0.f) {
+                            m[t][h] = top[t][h];
+                            v_ref[t][h] = v_now;
+                            l[t][h] = times_ex2(l[t][h], by);
+                            const float y = code_ex2(by);
 #pragma unroll
-                        for (int w = 4; w < 32; w <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, w));
-                        const float f = now == -INFINITY ? 1.f : few_ex2(m[t][h] - now);
-                        m[t][h] = now;
-                        l[t][h] *= f;
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            o[t][i][h] *= f * fv;
-                            o[t][i][2 + h] *= f * fv;
+                            for (int i = 0; i < MT; ++i) {
+                                o[t][i][h] *= y;
+                                o[t][i][2 + h] *= y;
+                            }
                         }
+                        neg[t][h] = v_up - (m[t][h] + v_ref[t][h]);
+                        big |= few_large(m[t][h]);
                     }
-                v_ref = v_new;
-                v_inv = v_new > 0.f ? 1.f / v_new : 0.f;
+                large = __any_sync(0xffffffffu, big);
+                if (large) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                            for (int x = 0; x < ET; ++x)
+#pragma unroll
+                                for (int e = h; e < 4; e += 2) s[x][t][e] = __fsub_rn(__fmul_rn(s[x][t][e], f[t][h]), m[t][h]);
+                            f[t][h] = 1.f;
+                            neg[t][h] = v_up - v_ref[t][h];
+                        }
+                }
+                if (far) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int x = 0; x < ET; ++x)
+#pragma unroll
+                                for (int e = h; e < 4; e += 2) l[t][h] += code_ex2(fmaf(s[x][t][e], f[t][h], neg[t][h] - v_up));
+                    down = 0.f;
+                }
             }
-            const float vr = v_scale * v_inv;
             uint32_t pb[ET][NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const float ref[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
+                float sum[2] = {0.f, 0.f};
 #pragma unroll
                 for (int x = 0; x < ET; ++x) {
                     float w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = few_ex2(s[x][t][e] - ref[e & 1]);
+                    for (int e = 0; e < 4; ++e) w[e] = code_ex2(fmaf(s[x][t][e], f[t][e & 1], neg[t][e & 1]));
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) l[t][h] += w[h] + w[2 + h];
-                    pb[x][t][0] = turn8x8(half2_of(w[0] * vr, w[1] * vr));
-                    pb[x][t][1] = turn8x8(half2_of(w[2] * vr, w[3] * vr));
+                    for (int h = 0; h < 2; ++h) sum[h] += w[h] + w[2 + h];
+                    pb[x][t][0] = turn8x8(half2_of(w[0], w[1]));
+                    pb[x][t][1] = turn8x8(half2_of(w[2], w[3]));
                 }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) l[t][h] = fmaf(sum[h], down, l[t][h]);
             }
             // ---- values: dims 16 grp .. (8 grp .. for 64) of entries 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9
 #pragma unroll
@@ -419,10 +448,13 @@ __global__ void __launch_bounds__(few_threads(DH, NT), few_ctas(DH, NT)) attn_fe
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int w = 4; w < 32; w <<= 1) l[t][h] += __shfl_xor_sync(0xffffffffu, l[t][h], w);
+                const PartRef ref = part_ref(m[t][h], v_ref[t][h], l[t][h]);
+                m[t][h] = ref.m;
+                l[t][h] = ref.l;
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    o[t][i][h] *= v_ref;
-                    o[t][i][2 + h] *= v_ref;
+                    o[t][i][h] *= ref.by;
+                    o[t][i][2 + h] *= ref.by;
                 }
             }
         const bool whole = it.whole();

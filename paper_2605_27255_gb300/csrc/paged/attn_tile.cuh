@@ -142,15 +142,6 @@ __device__ __forceinline__ bool elect_one() {
     return e != 0;
 }
 
-// The logarithm of a scale: that of a power of two is exact (its fraction's is that of 1).
-constexpr float kNoScale = -1000.f;
-__device__ __forceinline__ float log2_scale(float x) {
-    const uint32_t u = __float_as_uint(x);
-    float y;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(__uint_as_float((u & 0x007fffffu) | 0x3f800000u)));
-    return x > 0.f ? (float)((int)(u >> 23) - 127) + y : kNoScale;
-}
-
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -255,9 +246,7 @@ __device__ __forceinline__ void page_from_codes(unsigned char* dst, const unsign
 // whose other dims lie 2^10 below one that the keys do not have is then off by more than the output's
 // rounding.)  The row's and the block's scale meet the
 // scores in fp32.  Value codes become fp16 tiles (a code is an fp16 number) by warps 2, 12 and 14 (single: 12 and
-// 14, one per pipeline); their
-// scales go into the weights, relative to the largest so far (2^-24 at least: what that
-// adds to an output is below 2^-20 of its largest value), and weights keep fp16's 11 digits.
+// 14, one per pipeline); their scales go into the weights (codes.cuh), which keep fp16's 11 digits.
 // (Weights as e4m3 parts, so that values need no conversion either, would lose the small ones: a
 // long tail of 2^-17 each next to one large weight.)  Measured for 2048 tokens behind 14336 entries, 32
 // query and 8 kv heads of 128: 2559 us with row tiles of 32 on mma.sync, 692 with keys converted too (by two
@@ -721,8 +710,10 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                 const int32_t* list = p.pages + ((size_t)(it.q0 + tok) * c.n_kv + it.g) * shape.n_top;
                 if (kept > 0) pos = (kept - 1) * kPage + (list[kept - 1] == pos / kPage ? pos % kPage : kPage - 1);
             }
-            float m_ref = -INFINITY, l = 0.f;
-            float v_ref = kNoScale;  // 8-bit pools: the largest value scale so far, as a logarithm
+            float m_ref = E8 ? kNoScore : -INFINITY, l = 0.f;
+            // 8-bit pools (codes.cuh): the reference is m_ref + v_ref; large: of m_ref; v_top: the largest scale so far
+            float v_ref = 0.f, v_top = kNoScale;
+            bool large = false;
             float c_row = c2;        // what the row's raw scores are worth
             if (E8) {
                 ok = wait(q_full + w, (uint32_t)((begun - 1) & 1), 60, begun);
@@ -733,14 +724,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             // scales eight pages later, so that no page waits for them
             const int pg0 = (it.t0 + it.kv0) * 2, gone = E8 ? first_seen(shape, it.n, it.len, it.tile) / kPage : 0;
             int next_blk = -1;
-            float k_sc = 1.f, v_sc = kNoScale, next_k = 1.f, next_v = kNoScale;  // (values': logarithms)
+            float k_sc = 1.f, v_sc = 0.f, next_k = 1.f, next_v = 0.f;  // (values': logarithms)
             auto block_at = [&](int j) {  // (-1: gone, masked)
                 const int i = pg0 + j + lane;
                 return j + lane < it.pages() && i * kPage < it.len && i >= gone ? page_block(c, it.b, i) : -1;
             };
             auto scales_at = [&](int blk) {
                 next_k = 1.f;
-                next_v = kNoScale;
+                next_v = 0.f;
                 if (blk >= 0) {
                     next_k = p.k_scale[(size_t)blk * c.n_kv + it.g];
                     next_v = log2_scale(p.v_scale[(size_t)blk * c.n_kv + it.g]);
@@ -755,7 +746,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             for (int j = 0; j < np; ++j, ++sn) {
                 const uint32_t s_buf = s_col + (uint32_t)((sn & 1) * 64);
                 float cs = c2;
-                float v_now = kNoScale;
+                float v_now = 0.f;
                 if (E8) {
                     if ((j & 31) == 0) {
                         k_sc = next_k;
@@ -797,25 +788,53 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                             if (e0 + i > pos || e0 + i < lo) s[i >> 5][i & 31] = 0xff800000u;
                     }
                     const float top = SEL && !sel ? -INFINITY : fmaxf(max32(s[0]), max32(s[1])) * cs;
-                    // the reference moves when the maximum has passed it by the slack (or it is the first one)
-                    const bool move = top > m_ref + kAtSlack;
-                    // 8-bit pools: scores so large that what a fused multiply-add keeps of the maximum itself, up to half a step,
-                    // is a power of two that matters are multiplied before the subtraction, which then leaves 0
-                    const bool large = E8 && fabsf(top) > 4194304.f && top > -INFINITY;
-                    if (__any_sync(0xffffffffu, move || large) || (E8 && v_now > v_ref)) {
-                        if (E8 && __any_sync(0xffffffffu, large)) {
+                    // the reference moves when the maximum (8-bit pools: with the page's scale) has passed it by the slack,
+                    // or it is the first one
+                    const float v_up = v_now + kWeightUp;
+                    float neg = E8 ? v_up - (m_ref + v_ref) : 0.f;
+                    const bool move = E8 ? top + neg > kWeightTop : top > m_ref + kAtSlack;
+                    const bool far = E8 && v_now < v_top - kFarScale;  // (the same for the warp)
+                    float down = -v_up;                                // from weights to the sum's, as an exponent
+                    v_top = fmaxf(v_top, v_now);
+                    bool dead = false;
+                    if (__any_sync(0xffffffffu, E8 ? move || large || far : move)) {
+                        float f = 1.f;
+                        bool scaled = true;
+                        if (!E8) {
+                            if (move) f = m_ref == -INFINITY ? 0.f : ex2(m_ref - top);
+                            if (move) m_ref = top;
+                            l *= f;
+                        } else {
+                            // (exact beside large scores too)
+                            const float by = (m_ref - top) + (v_ref - v_now);
+                            const bool move = by < -kAtSlack;
+                            if (move) {
+                                l = times_ex2(l, by);
+                                f = ex2(by);
+                                m_ref = top;
+                                v_ref = v_now;
+                                large = fabsf(m_ref) > kLargeScore;
+                            }
+                            neg = v_up - (m_ref + v_ref);
+                            scaled = __any_sync(0xffffffffu, move);
+                            const bool any_large = __any_sync(0xffffffffu, large);
+                            if (any_large) {
 #pragma unroll
-                            for (int i = 0; i < kPage; ++i) s[i >> 5][i & 31] = __float_as_uint(__fmul_rn(__uint_as_float(s[i >> 5][i & 31]), cs));
-                            cs = 1.f;
+                                for (int i = 0; i < kPage; ++i)
+                                    s[i >> 5][i & 31] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(s[i >> 5][i & 31]), cs), m_ref));
+                                cs = 1.f;
+                                neg = v_up - v_ref;
+                            }
+                            if (far) {  // (relative to the page's own largest score; fp16 would have 0 for the weights)
+                                const float up = (any_large ? top - m_ref : top) + neg;
+                                dead = up < -40.f && top > -INFINITY;
+                                if (dead) {
+                                    neg -= up;
+                                    down = up - v_up;
+                                }
+                            }
                         }
-                        float f = move ? (m_ref == -INFINITY ? 0.f : ex2(m_ref - top)) : 1.f;
-                        if (move) m_ref = top;
-                        l *= f;
-                        if (E8 && v_now > v_ref) {
-                            f *= ex2(v_ref - v_now);
-                            v_ref = v_now;
-                        }
-                        if (j > 0) {  // the output so far, once the values of the page before are in it
+                        if (j > 0 && scaled) {  // the output so far, once the values of the page before are in it
                             ok = wait(&o_full[w][(sn - 1) & 1], (uint32_t)(((sn - 1) >> 1) & 1), 59, sn);
                             if (!ok) break;
                             tc_fence_after();
@@ -832,12 +851,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         }
                     }
                     // (a page that the row has not selected: exponents of -infinity)
-                    float neg = SEL && !sel ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
-                    float dv = 0.f;  // 8-bit pools: the page's value scale against the largest, as an exponent
-                    if (E8) {
-                        dv = fmaxf(v_now - v_ref, -24.f);
-                        neg += dv;
-                    }
+                    if (!E8) neg = SEL && !sel ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
                     // two columns at a time (paired fp32 instructions)
                     const uint64_t c22 = f32x2(cs, cs), neg2 = f32x2(neg, neg);
                     uint64_t sum[2] = {0ull, 0ull};
@@ -850,11 +864,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                         pk[i] = E8 ? half2_of(p0, p1) : pack_bf16x2(p0, p1);
                         if (PARTS == 2) pl[i] = pack_bf16x2(p0 - bf_lo(pk[i]), p1 - bf_hi(pk[i]));
                     }
+                    if (far) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) pk[i] = dead ? 0u : pk[i];
+                    }
                     tmem_st32(s_buf, pk);
                     if (PARTS == 2) tmem_st32(s_buf + 32, pl);
                     sum[0] = add_f32x2(sum[0], sum[1]);
                     float part = __uint_as_float((uint32_t)sum[0]) + __uint_as_float((uint32_t)(sum[0] >> 32));
-                    if (E8) part *= ex2(-dv);
+                    if (E8) part = far ? times_ex2(part, down) : part * ex2(down);
                     l += part;
                     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 }
@@ -879,7 +897,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
             if (!ok) break;
             tc_fence_after();
             if (live) {
-                const float unit = E8 ? ex2(v_ref) : 1.f, inv = l > 0.f ? unit / l : 0.f;
+                // (8-bit pools: weights are held up, and parts are left as codes.cuh says)
+                const float inv = l > 0.f ? (E8 ? 1.f / (1 << (int)kWeightUp) : 1.f) / l : 0.f;
+                const PartRef ref = E8 && !whole ? part_ref(m_ref, v_ref, l) : PartRef{m_ref, l, 1.f};
 #pragma unroll
                 for (int h = 0; h < DH / 32; ++h) {
                     uint32_t v[32];
@@ -888,7 +908,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     pin32(v);
                     if (E8 && !whole) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * unit);
+                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * ref.by);
                     }
                     if (r < rows && whole) {
 #pragma unroll
@@ -908,7 +928,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) attn_tile_kernel(AttnPagedArgs 
                     __syncwarp();
                 }
                 if (!whole && r < rows)
-                    *reinterpret_cast<float2*>(part + (size_t)part_rows * DH + 2 * (row0 + r)) = make_float2(m_ref, l);
+                    *reinterpret_cast<float2*>(part + (size_t)part_rows * DH + 2 * (row0 + r)) = make_float2(ref.m, ref.l);
             }
             tc_fence_before();  // the output is read, before the next item's values overwrite it
         }
