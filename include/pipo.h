@@ -567,14 +567,15 @@ typedef struct {
 } pipo_page_tables;
 
 /* The tables of a step in one call.  Sequence b keeps its first d_kept[b] entries (fewer than
- * it holds after rejected drafts, 0 when it has ended) and gets d_added[b] new
+ * it holds after rejected drafts, 0 when it has ended; clamped to 0 .. 64 held[b]) and gets d_added[b] new
  * tokens (negative counts as 0).  Blocks past the kept entries go back onto the stack, in the order of the
  * sequences and pages; then b is served if its row has room, and the stack has the blocks
  * and n_tokens the room that all sequences up to b (but those without room in their row) ask for;
  * a sequence that needs no new block waits for tokens only.  The blocks handed out are
- * the last ones on the stack, in order, so that the same call on its own result changes nothing.
+ * the last ones on the stack, in order, so that the same call on its own result changes nothing if no d_kept[b] was
+ * clamped from above (a clamped one may reach further after the call than before it: every repeat then takes blocks).
  * Pages given back and not handed out again are -1 in the table.
- *   d_kv_len[b]      entries of b with its new ones (d_kept[b] alone if it was not served);
+ *   d_kv_len[b]      entries of b with its new ones (the clamped d_kept[b] alone if it was not served);
  *   d_q_start[b]     rows of the tokens before b's, [batch + 1]: the difference is
  *                    d_added[b], or 0 for a sequence that was not served;
  *   d_slots[t]       block * 64 + slot of token row t, [n_tokens], -1 behind the last;

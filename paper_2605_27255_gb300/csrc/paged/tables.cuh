@@ -6,7 +6,7 @@
 // has room, and if the stack holds the wanted pages of all requests up to b, and the
 // token arrays their tokens (b with w_b = 0 needs only the latter).  The pages of all served
 // requests are the last ones of the stack, in their order; so the same call on its own result
-// changes nothing.
+// changes nothing (unless kept entries were clamped: what is held has grown).
 //
 // Bound by latency: three prefix sums over the requests in one CTA (every request has its
 // sums in shared memory), then a thread per page given back, per page taken and

@@ -351,12 +351,13 @@ class BlockTables:
                    torch.full((1,), n_blocks, **i32))
 
     def advance(self, kept: torch.Tensor, added: torch.Tensor, tokens: int) -> Tuple[torch.Tensor, ...]:
-        """Keep the first ``kept[b]`` entries of every sequence and make room for ``added[b]``
-        more.  Blocks past the kept entries become free, then sequences are served in order while
+        """Keep the first ``kept[b]`` entries of every sequence (clamped to what it holds) and make room for
+        ``added[b]`` more.  Blocks past the kept entries become free, then sequences are served in order while
         blocks, their rows and ``tokens`` token rows last.  Returns int32 ``q_start`` [batch + 1] and
         ``kv_len`` [batch] for the cache's calls, and of every token row ``slots`` (block * 64 +
         slot) and ``positions`` [tokens], -1 behind the last.  A sequence that was not served has no
-        rows, and ``kv_len[b]`` is ``kept[b]``."""
+        rows, and ``kv_len[b]`` is the clamped ``kept[b]``.  The same call again changes nothing if nothing was
+        clamped from above."""
         if _current_device() != self.index:
             with torch.cuda.device(self.index):
                 return self.advance(kept, added, tokens)
