@@ -542,8 +542,8 @@ PIPO_API pipo_status pipo_op_kv_append8(const pipo_paged8 *c, int32_t n_tokens, 
  * block's scale that is 2^-32 of the row's largest or less may be lost).  Blocks that a row does not see do not
  * touch it, whatever their scales are.  Queries keep all
  * their digits down to 2^-24 of their row's largest; what is below 2^-31 of that may be lost.
- * Which kernel runs goes by the batch's average of rows per sequence, so the low bits of a sequence's
- * outputs depend on what shares its batch; the same call gives the same bits. */
+ * Which kernel runs goes by the batch's average of rows per sequence (those without new tokens count), so the low bits
+ * of a sequence's outputs depend on what shares its batch; the same call gives the same bits. */
 PIPO_API pipo_status pipo_op_attn_paged8(const pipo_paged8 *c, int32_t n_tokens, const void *d_q, int64_t ld_q,
                                          float scale, int32_t window, void *d_out, int64_t ld_out, void *d_scratch,
                                          size_t scratch_bytes, void *stream);

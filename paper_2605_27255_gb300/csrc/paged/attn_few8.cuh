@@ -22,8 +22,8 @@
 //
 // Bound by HBM while it streams, else by its start (lengths, piece, block table, one after the other: 5 us) and the
 // joining.  Measured with the joining, back to back: eight sequences of 15.5 K entries with one token each, 32 query
-// and 8 kv heads of 128, 47 us, 5.4 TB/s; 64 sequences of five tokens with a window of 1024, 16 heads of 64, 32 to
-// 38 us (by the GPU), 3.6 to 4.2 TB/s; one token over 1155 entries 8.8 us.
+// and 8 kv heads of 128, 47 us, 5.4 TB/s (49 with two such caches in turn); 64 sequences of five tokens with a window of
+// 1024, 16 heads of 64, 32 to 39 us (by the GPU), 3.5 to 4.2 TB/s; one token over 1155 entries 9.0 us.
 #pragma once
 
 #include <cuda_fp16.h>

@@ -32,7 +32,8 @@ cudaError_t few8_as(const AttnPagedArgs& a, const AttnPlan& pl, cudaStream_t s) 
     const ItemShape shape{pl.TP, a.window, 0};
     const cudaError_t e = launch_pdl(fn, dim3((unsigned)pl.ctas), few_threads(DH, NT), few_smem(DH, NT, a.c.batch), s, a, shape,
                                      pl.workers, pl.part_rows, pl.part_off);
-    // (blocks of 32 rows would idle with tiles of 8: 64 sequences of five rows 36.6 us, so 33)
+    // (blocks of 32 rows idle with tiles of 8.  Two builds in turn on one GPU: 16 sequences of 2000 entries and five rows 18.1
+    // us with them, 16.5 so, eight of 15.5 K entries 48.6 and 47.6; 64 of five rows with a window of 1024 37.5 and 38.5)
     if (e == cudaSuccess && pl.join && NT == 1)
         return launch_pdl(&combine_kernel<DH, bf16_t, 8>, dim3((unsigned)pl.workers, 1, DH / 16), 128, 0, s, a, pl.workers,
                           pl.part_rows, pl.part_off);
@@ -50,11 +51,13 @@ cudaError_t launch_kv_append8(const AppendArgs& a, cudaStream_t s) {
 // pipelines with items of their own; above 128 rows pairs of tiles that share a pipeline's pages.  Where mma.sync
 // would read the cache twice (33 to 64 rows) it goes by the work: with few sequences and heads its short start
 // counts.  Measured in us, 32 query and 8 kv heads of 128 / 16 and 16 of 64, mma.sync, single tiles, pairs:
-//   one sequence of 4000 entries, 64 rows   19 / 21    27 / 22    24 / 22
-//   4 of 2000, 64 rows                      26 / 29    26 / 25    28 / 36
-//   16 of 2000, 32 rows                     37 / 44    53 / 63    65 / 87
-//   16 of 2000, 64 rows                     60 / 80    55 / 68    66 / 99
-//   16 of 2000, 128 rows                   105 / 145   58 / 73    73 / 116
+//   one sequence of 4000 entries, 64 rows   20 / 24    27 / 21    23 / 21
+//   4 of 2000, 64 rows                      27 / 30    25 / 23    26 / 34
+//   16 of 2000, 32 rows                     39 / 48    51 / 66    62 / 95
+//   16 of 2000, 64 rows                     63 / 83    55 / 69    64 / 97
+//   16 of 2000, 128 rows                   111 / 151   59 / 70    76 / 110
+// (Uniform batches, no idle sequences: the average counts those too, so a chunk among many idle places takes tiles of
+// few rows.)
 constexpr int kFewRows = 32, kFewRowsStart = 64, kManyItems = 32;
 AttnPlan plan_attn8(const PagedArgs& c, int dev, int sms) {
     AttnPlan pl{};

@@ -27,7 +27,7 @@ cudaError_t tile8_as(const AttnPagedArgs& a, const AttnPlan& pl, const CUtensorM
                      cudaStream_t s) {
     auto* fn = &attn_tile_kernel<DH, PAIR, false, true>;
     static thread_local int ready_dev = -1;  // the shared-memory limit is set per device
-    static_assert(at8_smem(DH, PAIR) >= 1024 + 2 * (size_t)at_q_bytes(DH) + find_ints(kPagedMaxBatch) * 4,
+    static_assert(at8_smem(DH, PAIR) >= 1024 + 2 * (size_t)at8_q_bytes(DH) + find_ints(kPagedMaxBatch) * 4,
                   "the search for the pieces uses the rings' memory");
     if (ready_dev != pl.dev) {
         const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at8_smem(DH, PAIR));

@@ -15,8 +15,8 @@
 // warp's slice once more.  Another CTA's shared memory may be written only once that CTA has started: every
 // CTA arrives at the cluster's barrier when it starts and waits there, under the sums, before its first such write.  Bound by the row's read (and the draft row's) and, for few sequences, by
 // the chain of start, drafted token, probabilities, row.  Measured back to back with a vocabulary of 151936 in
-// fp32: 64 sequences 14.7 us (52 MB read), one 8.8 us.  Four loads of either row in flight take 50
-// registers, so that 512 CTAs need two rounds (16.8 and 8.0 us); CTAs of 256 threads 17.3 and 12.4.
+// fp32: 64 sequences 14.7 us with their 52 MB in L2, 17.9 with rows that are not, one 8.6 us.  Four loads of either row
+// in flight take 50 registers, so that 512 CTAs need two rounds (16.8 and 8.0 us in L2); CTAs of 256 threads 17.3 and 12.4.
 #pragma once
 
 #include <cooperative_groups.h>

@@ -78,3 +78,27 @@ def test_any_scale_below_grows_as_its_own_do(scale, size, d_h):
             off = (new_now - want).abs()
             assert (off <= torch.maximum(2.0 ** -4 * want.abs(), torch.tensor(2.0 ** -10 * now)) * (1 + 2.0 ** -20)).all()
             assert math.isfinite(now) and now >= old
+
+
+@pytest.mark.parametrize("d_h", [64, 128])
+@pytest.mark.parametrize("large", [100.0, 3000.0, 5e4])
+def test_a_draft_that_is_given_up_leaves_its_scale(d_h, large):
+    """Entries kept before a large draft, and those appended in its place: the scale stays as high as the draft needed,
+    every entry is within its half step and a subnormal step of it (half of one each time it is rounded, and scales at
+    least double)."""
+    pool = lambda: torch.zeros(1, 2, PAGE, d_h, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)  # noqa: E731
+    s = lambda: torch.ones(1, 2, device="cuda")  # noqa: E731
+    c = paged.PagedCache8(pool(), pool(), s(), s(), torch.zeros(1, 1, dtype=torch.int32, device="cuda"), n_q=2)
+    g = torch.Generator().manual_seed(9)
+    x = torch.randn(12, 2, d_h, generator=g)
+    add(c, x[:8], 0)
+    first = c.k_scale.clone()
+    add(c, torch.full((2, 2, d_h), large), 8)  # two drafts, given up
+    raised = c.k_scale.clone()
+    assert (raised == scale_of(large)).all() and (raised > first).all()
+    add(c, x[8:], 8)
+    for pool, scales, sign in ((c.k, c.k_scale, 1), (c.v, c.v_scale, -1)):
+        assert torch.equal(scales, raised)
+        got = pool[0, :, :12].double().cpu().transpose(0, 1) * scale_of(large)
+        want = sign * x.double()
+        assert ((got - want).abs() <= 2.0 ** -4 * want.abs() * (1 + 2.0 ** -4) + 2.0 ** -9 * scale_of(large)).all()

@@ -138,3 +138,13 @@ def test_large_scores_keep_the_scales(d_h, n, size):
             want = v[s.argmax()]
             assert ((got[t, h] - want).abs() <= (2.0 ** -8 + 2.0 ** -10) * want.abs() + 2.0 ** -65).all()
     assert seen > 0.9 * 16 * n
+
+
+@pytest.mark.parametrize("d_h", [64, 128])
+@pytest.mark.parametrize("n", TOKENS)
+@pytest.mark.parametrize("small_first", [True, False])
+def test_parts_whose_scales_lie_at_the_ends(d_h, n, small_first):
+    """Items that many workers share, half of their entries with values near 2^-96 and half near 2^91: all weights
+    count below the fraction line, whichever part they come from."""
+    x = Batch8([4500, 3800], [n, n], 8, 2, d_h, seed=56)
+    run(lift(x, lambda b, p: -95 if (p < 34) == small_first else 94))
